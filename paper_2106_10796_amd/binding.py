@@ -53,6 +53,12 @@ class cdsgd_cost(ctypes.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_}
 
 
+class cdsgd_adamw_tensor(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("weight16", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n", ctypes.c_size_t), ("weight_decay", ctypes.c_float)]
+
+
 class _Declines:
     """In the place of the native calls: every call declines."""
 
@@ -169,9 +175,29 @@ def lib():
                                            ctypes.POINTER(cdsgd_cost)]
         L.cdsgd_cost_period_mean.restype = i
         L.cdsgd_cost_period_mean.argtypes = [ctypes.POINTER(cdsgd_cost_params), ctypes.POINTER(cdsgd_cost)]
+        _declare_ops(L)
         _calls = _load_calls(L)
         _lib = L                       # last: another thread that sees it finds the calls bound
     return _lib
+
+
+def _declare_ops(L):
+    """The entry points of include/cdsgd_ops.h."""
+    vp, sz, f, i, d = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float, ctypes.c_int, ctypes.c_double
+    pvp = ctypes.POINTER(vp)
+    for name, restype, argtypes in (
+            ("cdsgd_grad_norm_create", i, [pvp, ctypes.POINTER(sz), i, i, pvp]),
+            ("cdsgd_grad_norm_compute", i, [vp, d, d, vp, vp]),
+            ("cdsgd_grad_norm_destroy", i, [vp]),
+            ("cdsgd_state_blocks", sz, [sz]),
+            ("cdsgd_adamw_plan_create", i, [ctypes.POINTER(cdsgd_adamw_tensor), i, i, i, pvp]),
+            ("cdsgd_adamw_plan_destroy", i, [vp]),
+            ("cdsgd_adamw_step", i, [vp, ctypes.c_long, d, d, d, d, d, ctypes.c_uint64, vp, vp]),
+            ("cdsgd_adamw_grad_norm", i, [vp, d, d, vp, vp]),
+            ("cdsgd_adamw_bind_readout", i, [vp, pvp, pvp, i]),
+            ("cdsgd_adamw_read_states", i, [vp, vp])):
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = restype, argtypes
 
 
 def packed_words(n: int) -> int:
@@ -538,6 +564,139 @@ class Trainer:
         if self._handle is not None and self._handle.value:
             lib().cdsgd_trainer_destroy(self._handle)
         self._handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+# ---------------------------------------------------------------------------
+# include/cdsgd_ops.h: norms of gradients, AdamW
+# ---------------------------------------------------------------------------
+STATE_BLOCK = 256   # CDSGD_STATE_BLOCK
+
+
+def state_blocks(n: int) -> int:
+    return int(lib().cdsgd_state_blocks(int(n)))
+
+
+def _same_device(tensors):
+    """A handle works on the device of its tensors, which is the current one when it is made."""
+    for t in tensors:
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError("a tensor is not on the current device")
+
+
+class GradNorm:
+    """The norm of a list of gradients (cdsgd_grad_norm_*): contiguous CUDA tensors of one type.  Keeps references to them."""
+
+    def __init__(self, grads):
+        self._handle = None
+        dtype = grads[0].dtype if len(grads) else torch.float32
+        if dtype not in GRAD_DTYPES:
+            raise TypeError("gradients must be float32, bfloat16 or float16")
+        arr = (ctypes.c_void_p * max(len(grads), 1))(*[_dev(g, dtype, None, "grads[%d]" % i) for i, g in enumerate(grads)])
+        sizes = (ctypes.c_size_t * max(len(grads), 1))(*[g.numel() for g in grads])
+        _same_device(grads)
+        handle = ctypes.c_void_p()
+        st = lib().cdsgd_grad_norm_create(arr, sizes, len(grads), GRAD_DTYPES[dtype], ctypes.byref(handle))
+        _check(st, "cdsgd_grad_norm_create")
+        self._handle, self._keep = handle, list(grads)
+
+    def compute(self, out, grad_scale=1.0, max_norm=float("inf")):
+        """out (float32, 2 elements) receives the norm and the factor that brings it down to max_norm."""
+        st = lib().cdsgd_grad_norm_compute(self._handle, float(grad_scale), float(max_norm), _dev(out, torch.float32, 2, "out"),
+                                           _stream())
+        if st != OK:
+            _check(st, "cdsgd_grad_norm_compute")
+
+    def destroy(self):
+        if self._handle is not None and self._handle.value:
+            lib().cdsgd_grad_norm_destroy(self._handle)
+        self._handle = self._keep = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+class AdamWPlan:
+    """AdamW over a list of tensors, one launch a step (cdsgd_adamw_*).
+
+    tensors: list of dicts with keys weight (float32), grad (grad_dtype), m and v (float32, or uint8 with state_bits=8),
+    m_scale and v_scale (uint8, state_blocks(n) of them, with state_bits=8), and optionally weight16 (grad_dtype, receives
+    a copy of the new weights; for all tensors or none) and weight_decay (0 if absent).  Contiguous CUDA tensors of any shape, of which the
+    plan keeps references.  States that are all zero bytes are the start of training.
+    """
+
+    def __init__(self, tensors, grad_dtype=torch.float32, state_bits=32):
+        self._handle = self._at = None
+        if grad_dtype not in GRAD_DTYPES:
+            raise TypeError("gradients must be float32, bfloat16 or float16")
+        state = torch.uint8 if state_bits == 8 else torch.float32
+        T = len(tensors)
+        arr = (cdsgd_adamw_tensor * max(T, 1))()
+        for i, t in enumerate(tensors):
+            n = t["weight"].numel()
+            arr[i].weight = _dev(t["weight"], torch.float32, None, "weight")
+            arr[i].weight16 = _dev(t.get("weight16"), grad_dtype, n, "weight16")
+            arr[i].grad = _dev(t["grad"], grad_dtype, n, "grad")
+            for name in ("m", "v"):
+                setattr(arr[i], name, _dev(t[name], state, n, name))
+                setattr(arr[i], name + "_scale", _dev(t.get(name + "_scale"), torch.uint8, state_blocks(n), name + "_scale"))
+            arr[i].n = n
+            arr[i].weight_decay = float(t.get("weight_decay", 0.0))
+        _same_device([x for t in tensors for x in t.values() if isinstance(x, torch.Tensor)])
+        handle = ctypes.c_void_p()
+        st = lib().cdsgd_adamw_plan_create(arr, T, GRAD_DTYPES[grad_dtype], int(state_bits), ctypes.byref(handle))
+        _check(st, "cdsgd_adamw_plan_create")
+        self._handle, self._at = handle, handle.value
+        self._sizes = [t["weight"].numel() for t in tensors]
+        self._keep, self._keep_out = [dict(t) for t in tensors], None
+
+    def step(self, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, seed=0, clip=None):
+        """Step number `step` (from 1 on).  clip: the out of grad_norm, or None.  seed: another one for every step with 8-bit states."""
+        st = lib().cdsgd_adamw_step(self._handle, int(step), float(lr), float(beta1), float(beta2), float(eps), float(grad_scale),
+                                    int(seed) & 0xFFFFFFFFFFFFFFFF, _dev(clip, torch.float32, 2, "clip"), _stream())
+        if st != OK:
+            _check(st, "cdsgd_adamw_step")
+
+    def grad_norm(self, out, grad_scale=1.0, max_norm=float("inf")):
+        """The norm of the plan's gradients and the factor for clipping, into out (float32, 2 elements)."""
+        st = lib().cdsgd_adamw_grad_norm(self._handle, float(grad_scale), float(max_norm), _dev(out, torch.float32, 2, "out"),
+                                         _stream())
+        if st != OK:
+            _check(st, "cdsgd_adamw_grad_norm")
+
+    def bind_readout(self, m_out, v_out):
+        """Where read_states puts the values of 8-bit states: lists of float32 or of bfloat16 tensors, one for each tensor."""
+        if len(m_out) != len(self._sizes) or len(v_out) != len(self._sizes):
+            raise ValueError("need one output for each tensor")
+        dtype = m_out[0].dtype
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("states are read out as float32 or bfloat16")
+        rows = []
+        for name, outs in (("m_out", m_out), ("v_out", v_out)):
+            rows.append((ctypes.c_void_p * len(outs))(*[_dev(t, dtype, n, "%s[%d]" % (name, i))
+                                                       for i, (t, n) in enumerate(zip(outs, self._sizes))]))
+        _same_device([*m_out, *v_out])
+        _check(lib().cdsgd_adamw_bind_readout(self._handle, rows[0], rows[1], GRAD_DTYPES[dtype]), "cdsgd_adamw_bind_readout")
+        self._keep_out = (list(m_out), list(v_out))
+
+    def read_states(self):
+        """The values that 8-bit states stand for, into the tensors of bind_readout."""
+        st = lib().cdsgd_adamw_read_states(self._handle, _stream())
+        if st != OK:
+            _check(st, "cdsgd_adamw_read_states")
+
+    def destroy(self):
+        if self._handle is not None and self._handle.value:
+            lib().cdsgd_adamw_plan_destroy(self._handle)
+        self._handle = self._at = self._keep = self._keep_out = None
 
     def __del__(self):
         try:

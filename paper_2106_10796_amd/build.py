@@ -11,6 +11,7 @@ import sysconfig
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "cdsgd.hip")
+SRC_OPS = [os.path.join(PKG, "csrc", name) for name in ("adamw.hip",)]          # translation units of their own
 SRC_HOST = [os.path.join(PKG, "csrc", "cdsgd_cost_model.cpp")]   # host-only parts of the library
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcdsgd.so")
@@ -115,7 +116,7 @@ def build(extra_flags=(), out=LIB, verbose=False) -> str:
     library = source_id(extra_flags)
     tmp = out + ".tmp%d" % os.getpid()
     _compile([hipcc_path(), *HIPCC_FLAGS, *extra_flags, '-DCDSGD_BUILD_ID_HEX="%s"' % library,
-              "-I", INCLUDE, SRC, *SRC_HOST, "-o", tmp], out, tmp, verbose)
+              "-I", INCLUDE, SRC, *SRC_OPS, *SRC_HOST, "-o", tmp], out, tmp, verbose)
     if out == LIB:
         _build_calls_if_possible(library, verbose)
     return out

@@ -1,5 +1,6 @@
 // CD-SGD per-step data-parallel hot path for gfx950 (MI355X): the C ABI and the host side of every
 // entry point.  One translation unit; the kernels are in the .hpp files beside this one:
+//   host_common.hpp     argument checks that the translation units share
 //   tuning.hpp          build-time knobs (launch shapes, cache policy)
 //   device_common.hpp   chunk geometry, 128-bit loads / stores, 16-bit widening, the quantiser
 //   device_tables.hpp   extents, tensor descriptors, chunk table
@@ -44,6 +45,7 @@
 
 #include "cdsgd.h"
 
+#include "host_common.hpp"
 #include "tuning.hpp"
 #include "device_common.hpp"
 #include "device_tables.hpp"
@@ -82,24 +84,6 @@ namespace {
 constexpr unsigned kLdsFor20Waves = 8192;
 constexpr unsigned kLdsFor22Waves = 7168;
 constexpr unsigned kLdsFor26Waves = 6144;
-
-inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-// Do [a, a + na) and [b, b + nb) share a byte?  (NULL never overlaps.)
-inline bool overlap2(const void *a, size_t na, const void *b, size_t nb)
-{
-    if (!a || !b) return false;
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y ? y - x < na : x - y < nb;
-}
-
-// Do the byte ranges [a, a + bytes) and [b, b + bytes) share a byte?  (NULL never overlaps.)
-inline bool overlap(const void *a, const void *b, size_t bytes)
-{
-    if (!a || !b) return false;
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y ? y - x < bytes : x - y < bytes;
-}
 
 inline unsigned long long packed_bytes_of(size_t n) { return 4ull * ((n + 15) / 16); }
 
@@ -161,11 +145,6 @@ inline bool good_threshold(float t) { return std::isfinite(t) && t > 0.0f; }
 inline bool good_step_params(long step, int k, float threshold, float lr_local, float lr_global)
 {
     return k >= 1 && step >= 0 && good_threshold(threshold) && std::isfinite(lr_local) && std::isfinite(lr_global);
-}
-
-inline int launch_status()
-{
-    return hipGetLastError() == hipSuccess ? CDSGD_OK : CDSGD_ERR_DEVICE;
 }
 
 }  // namespace

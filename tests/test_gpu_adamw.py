@@ -1,0 +1,439 @@
+"""AdamW over a layer list and norms of gradients on the GPU, against plain implementations in 64 bits and, for the codes of
+8-bit states, against the same operations in 32 bits, which the definition fixes bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2106_10796_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZES = [[1], [3], [255], [256, 1, 257], [511, 512, 513], [4095, 4096, 4097], [10007, 2, 65536, 31, 8193]]
+HYPER = dict(lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8)
+GUARD = 64          # elements around every buffer that nothing may write
+
+
+# ---- plain implementations ------------------------------------------------------------------------------------------------
+
+def plain_step(w, m, v, g, decay, step, lr, beta1, beta2, eps, factor=1.0):
+    """64 bits."""
+    g = g * factor
+    m = beta1 * m + (1 - beta1) * g
+    v = beta2 * v + (1 - beta2) * g * g
+    mhat, vhat = m / (1 - beta1 ** step), v / (1 - beta2 ** step)
+    return w - lr * decay * w - lr * mhat / (np.sqrt(vhat) + eps), m, v
+
+
+def moments32(m, v, g, beta1, beta2, gs):
+    """The two moments as the definition rounds them."""
+    f = np.float32
+    with np.errstate(all="ignore"):
+        g = g.astype(f) * f(gs)
+        return m * f(beta1) + g * f(1 - beta1), v * f(beta2) + (g * g) * f(1 - beta2)
+
+
+def dither(n, seed, first=0):
+    mask = (1 << 64) - 1
+    z = (seed + 0x9E3779B97F4A7C15) & mask
+    z = ((z ^ (z >> 32)) * 0xD6E8FEB86659FD93) & mask
+    s = (z ^ (z >> 32)) & 0xFFFFFFFF
+    x = (np.arange(first, first + n, dtype=np.uint64) * np.uint64(0x9E3779B9) + np.uint64(s)) & np.uint64(0xFFFFFFFF)
+    x = ((x ^ (x >> np.uint64(15))) * np.uint64(0xBB67AE85)) & np.uint64(0xFFFFFFFF)
+    x = ((x ^ (x >> np.uint64(13))) * np.uint64(0x6A09E667)) & np.uint64(0xFFFFFFFF)
+    x = x ^ (x >> np.uint64(16))
+    return (x & np.uint64(0xFFFF)).astype(np.int64), (x >> np.uint64(16)).astype(np.int64)
+
+
+def blocks_of(x):
+    n = x.size
+    padded = np.zeros(-(-n // 256) * 256, dtype=x.dtype)
+    padded[:n] = x
+    return padded.reshape(-1, 256)
+
+
+def encode(x, top, d):
+    """Codes and scale bytes of fp32 values; blocks that hold a NaN or an infinity get scale 255 and codes that mean nothing."""
+    x = x.astype(np.float32)
+    b = ((blocks_of(x).view(np.uint32) & 0x7FFFFFFF).max(1) >> 23).astype(np.int64)
+    with np.errstate(all="ignore"):
+        y = np.ldexp(np.abs(x).astype(np.float64), (top - np.repeat(b, 256)[:x.size])).astype(np.float32)
+    code = (y.view(np.uint32).astype(np.int64) + 16 * d) >> 20
+    code = np.where(np.signbit(x), code | 128, code) if top == 14 else np.where((code == 0) & (x > 0), 1, code)
+    return (code & 255).astype(np.uint8), b.astype(np.uint8)
+
+
+def decode(code, scale, top):
+    c = code.astype(np.int64)
+    sign = np.where(c >= 128, -1.0, 1.0) if top == 14 else 1.0
+    c = c & 127 if top == 14 else c
+    mag = np.where(c >= 8, np.ldexp(1 + (c & 7) / 8, (c >> 3) - 127), np.ldexp((c & 7) / 8, -126))
+    s = np.repeat(scale.astype(np.int64), 256)[:code.size]
+    return np.where(s == 255, np.nan, sign * np.ldexp(mag, s - top))
+
+
+# ---- a list on the GPU ----------------------------------------------------------------------------------------------------
+
+class Guarded:
+    """A buffer between two guards."""
+
+    def __init__(self, values, dtype):
+        self.n, self.dtype = values.size, dtype
+        self.all = torch.full((self.n + 2 * GUARD,), 77, dtype=dtype, device="cuda")
+        self.t = self.all[GUARD:GUARD + self.n]
+        self.t.copy_(torch.from_numpy(np.ascontiguousarray(values)).to(dtype))
+
+    def get(self):
+        rest = torch.cat((self.all[:GUARD], self.all[GUARD + self.n:]))
+        assert bool((rest.float() == 77).all()), "written outside the tensor"
+        t = self.t.cpu()
+        return t.float().numpy() if self.dtype in (torch.bfloat16, torch.float16) else t.numpy()
+
+
+def make(sizes, grad, bits, copy=False, seed=0, spread=1e-3, decays=(0.0, 0.1)):
+    r = np.random.default_rng(seed)
+    out = []
+    for i, n in enumerate(sizes):
+        w, g = r.normal(0, 0.1, n).astype(np.float32), r.normal(0, spread, n).astype(np.float32)
+        g[r.random(n) < 0.02] *= 100
+        g[r.random(n) < 0.1] = 0
+        m, v = (r.normal(0, spread, n) * r.choice([1, 1e-3], n)).astype(np.float32), (spread ** 2 * r.random(n) ** 4).astype(np.float32)
+        t = {"weight": Guarded(w, torch.float32), "grad": Guarded(g, TYPES[grad]), "decay": decays[i % len(decays)]}
+        if bits == 32:
+            t["m"], t["v"] = Guarded(m, torch.float32), Guarded(v, torch.float32)
+        else:
+            half = np.full(n, 32768)
+            for name, x, top in (("m", m, 14), ("v", v, 30)):
+                codes, scale = encode(x, top, half)
+                t[name], t[name + "_scale"] = Guarded(codes, torch.uint8), Guarded(scale, torch.uint8)
+        if copy:
+            t["weight16"] = Guarded(np.zeros(n, np.float32), TYPES[grad])
+        out.append(t)
+    return out
+
+
+def plan_of(tensors, grad, bits):
+    return B.AdamWPlan([{k: (x.t if isinstance(x, Guarded) else x) for k, x in t.items() if k != "decay"} | {"weight_decay": t["decay"]}
+                        for t in tensors], grad_dtype=TYPES[grad], state_bits=bits)
+
+
+def values(t, bits):
+    """(w, m, v, g) in 64 bits."""
+    w, g = t["weight"].get().astype(np.float64), t["grad"].get().astype(np.float64)
+    if bits == 32:
+        return w, t["m"].get().astype(np.float64), t["v"].get().astype(np.float64), g
+    return w, decode(t["m"].get(), t["m_scale"].get(), 14), decode(t["v"].get(), t["v_scale"].get(), 30), g
+
+
+def weight_bound(w, m, g, new_m, new_v, step, lr, beta1, beta2, eps, **_):
+    """What the roundings of the definition can add up to.  The moment: two products, a sum, and the factors' own rounding, of
+    terms that may cancel; the update: ten operations of a unit each (2 for square root and reciprocal); the weight: 4."""
+    denom = np.sqrt(new_v / (1 - beta2 ** step)) + eps
+    each = lr / (1 - beta1 ** step) / denom
+    terms = beta1 * np.abs(m) + (1 - beta1) * np.abs(g)
+    return U * (4 * np.abs(w) + each * (6 * terms + 14 * np.abs(new_m))) * 1.01 + 1e-40
+
+
+# ---- tests ----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "+".join(map(str, s)))
+@pytest.mark.parametrize("grad,copy", [("f32", False), ("bf16", True), ("f16", True), ("bf16", False), ("f16", False)])
+def test_step_with_32_bit_states(sizes, grad, copy):
+    tensors = make(sizes, grad, 32, copy, seed=sum(sizes))
+    plan = plan_of(tensors, grad, 32)
+    for step in (1, 2, 1000):
+        before = [values(t, 32) for t in tensors]
+        plan.step(step, **HYPER)
+        for t, (w, m, v, g) in zip(tensors, before):
+            want_w, want_m, want_v = plain_step(w, m, v, g, t["decay"], step, **HYPER)
+            got_w, got_m, got_v, _ = values(t, 32)
+            m32, v32 = moments32(m.astype(np.float32), v.astype(np.float32), g, 0.9, 0.999, 1.0)
+            assert np.array_equal(got_m.astype(np.float32), m32) and np.array_equal(got_v.astype(np.float32), v32)
+            assert np.all(np.abs(got_m - want_m) <= 5 * U * (0.9 * np.abs(m) + 0.1 * np.abs(g)) + 1e-44)
+            assert np.all(np.abs(got_v - want_v) <= 6 * U * want_v + 1e-44)
+            assert np.all(np.abs(got_w - want_w) <= weight_bound(w, m, g, want_m, want_v, step, **HYPER))
+            if copy:
+                assert np.array_equal(t["weight16"].get(), torch.from_numpy(t["weight"].get()).to(TYPES[grad]).float().numpy())
+
+
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "+".join(map(str, s)))
+@pytest.mark.parametrize("grad,copy", [("f32", False), ("bf16", True), ("f16", False), ("bf16", False), ("f16", True)])
+def test_step_with_8_bit_states(sizes, grad, copy):
+    tensors = make(sizes, grad, 8, copy, seed=sum(sizes))
+    plan = plan_of(tensors, grad, 8)
+    for step, seed in ((1, 0), (2, 12345678901234567890), (1000, 7)):
+        before = [values(t, 8) for t in tensors]
+        plan.step(step, seed=seed, **HYPER)
+        first = 0
+        for t, (w, m, v, g) in zip(tensors, before):
+            n = w.size
+            want_w, want_m, want_v = plain_step(w, m, v, g, t["decay"], step, **HYPER)
+            m32, v32 = moments32(m.astype(np.float32), v.astype(np.float32), g, 0.9, 0.999, 1.0)
+            dm, dv = dither(n, seed, first)
+            first += -(-n // 256) * 256
+            for name, x, top, d in (("m", m32, 14, dm), ("v", v32, 30, dv)):
+                codes, scale = encode(x, top, d)
+                assert np.array_equal(t[name + "_scale"].get(), scale), name
+                assert np.array_equal(t[name].get(), codes), name
+                held = decode(codes, scale, top)
+                # within a step of the code's own grid: an eighth of the value, or of the lowest binade under the block's scale
+                lowest = np.ldexp(1.0, np.repeat(scale.astype(int), 256)[:n] - 127 - (top - 1))
+                assert np.all(np.abs(held - x) <= np.maximum(np.abs(x), lowest) / 8)
+            got_w = t["weight"].get().astype(np.float64)
+            assert np.all(np.abs(got_w - want_w) <= weight_bound(w, m, g, want_m, want_v, step, **HYPER))
+            if copy:
+                assert np.array_equal(t["weight16"].get(), torch.from_numpy(t["weight"].get()).to(TYPES[grad]).float().numpy())
+
+
+@pytest.mark.parametrize("n", [1, 7, 256, 300, 513, 5000])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_states_read_out(n, out):
+    r = np.random.default_rng(n)
+    t = make([n, n], "f32", 8, seed=n)
+    for x in t:      # every code there is
+        for name in ("m", "v"):
+            x[name].t.copy_(torch.from_numpy(r.integers(0, 256, n).astype(np.uint8)))
+            x[name + "_scale"].t.copy_(torch.from_numpy(r.integers(60, 200, -(-n // 256)).astype(np.uint8)))
+    t[1]["m_scale"].t[-1] = 255
+    plan = plan_of(t, "f32", 8)
+    with pytest.raises(B.CdsgdError) as e:
+        plan.read_states()
+    assert e.value.status == B.ERR_NULL
+    outs = [[Guarded(np.zeros(n, np.float32), TYPES[out]) for _ in t] for _ in range(2)]
+    plan.bind_readout([o.t for o in outs[0]], [o.t for o in outs[1]])
+    plan.read_states()
+    for i, x in enumerate(t):
+        for got, name, top in ((outs[0][i], "m", 14), (outs[1][i], "v", 30)):
+            want = decode(x[name].get(), x[name + "_scale"].get(), top)
+            assert np.array_equal(got.get().astype(np.float64), want, equal_nan=True), name
+
+
+def test_readout_refuses():
+    t = make([300], "f32", 8)
+    plan = plan_of(t, "f32", 8)
+    f = lambda n=300, d=torch.float32: torch.zeros(n, device="cuda", dtype=d)  # noqa: E731
+    with pytest.raises(ValueError):
+        plan.bind_readout([], [])
+    with pytest.raises(TypeError, match="float32 or bfloat16"):
+        plan.bind_readout([f(d=torch.float16)], [f(d=torch.float16)])
+    with pytest.raises(ValueError, match="m_out"):
+        plan.bind_readout([f(299)], [f()])
+    same = f()
+    for m, v, want in ((same, same, B.ERR_ALIAS), (t[0]["weight"].t, f(), B.ERR_ALIAS), (f(301)[1:], f(), B.ERR_ALIGN)):
+        with pytest.raises(B.CdsgdError) as e:
+            plan.bind_readout([m], [v])
+        assert e.value.status == want
+    plan32 = plan_of(make([300], "f32", 32), "f32", 32)
+    for call in (lambda: plan32.bind_readout([f()], [f()]), plan32.read_states):
+        with pytest.raises(B.CdsgdError) as e:
+            call()
+        assert e.value.status == B.ERR_PARAM
+
+
+@pytest.mark.parametrize("over", [dict(step=0), dict(step=-1), dict(lr=-1.0), dict(lr=float("nan")), dict(lr=1e300), dict(beta1=1.0),
+                                  dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=float("nan")), dict(eps=0.0), dict(eps=-1e-8),
+                                  dict(eps=float("inf")), dict(grad_scale=float("inf"))])
+def test_step_refuses(over):
+    t = make([300], "f32", 32)
+    plan = plan_of(t, "f32", 32)
+    before = values(t[0], 32)
+    with pytest.raises(B.CdsgdError) as e:
+        plan.step(**({"step": 1, **HYPER} | over))
+    assert e.value.status == B.ERR_PARAM
+    for a, b in zip(before, values(t[0], 32)):
+        assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_clip_and_scale(bits):
+    """The factor of a clip and the gradients' scale are one factor on the gradient; it comes from the device."""
+    t = make([1000, 5001], "bf16", bits, seed=3, spread=0.1)
+    plan = plan_of(t, "bf16", bits)
+    out = torch.zeros(2, device="cuda")
+    before = [values(x, bits) for x in t]
+    plan.grad_norm(out, grad_scale=0.5, max_norm=0.25)
+    norm = 0.5 * np.sqrt(sum(np.sum(x[3] ** 2) for x in before))
+    got = out.cpu().numpy().astype(np.float64)
+    assert abs(got[0] - norm) <= 2 * U * norm and abs(got[1] - 0.25 / norm) <= 2 * U * 0.25 / norm and norm > 0.25
+    plan.step(5, grad_scale=0.5, clip=out, seed=9, **HYPER)
+    gs = np.float32(0.5) * np.float32(got[1])
+    for x, (w, m, v, g) in zip(t, before):
+        want_w, want_m, want_v = plain_step(w, m, v, g, x["decay"], 5, factor=float(gs), **HYPER)
+        if bits == 32:
+            m32, v32 = moments32(m.astype(np.float32), v.astype(np.float32), g, 0.9, 0.999, gs)
+            assert np.array_equal(x["m"].get(), m32) and np.array_equal(x["v"].get(), v32)
+        got_w = x["weight"].get().astype(np.float64)
+        # (one more rounding, of the scaled gradient: in the moment it counts once more, in the square root once)
+        extra = U * 2 * HYPER["lr"] / (1 - 0.9 ** 5) * (np.abs(m) + np.abs(g * gs)) / (np.sqrt(want_v / (1 - 0.999 ** 5)) + 1e-8)
+        assert np.all(np.abs(got_w - want_w) <= weight_bound(w, m, g * gs, want_m, want_v, 5, **HYPER) + extra)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_step_that_overflowed_is_skipped(bits, bad):
+    t = make([700, 4097], "f16", bits, copy=True)
+    t[1]["grad"].t[4096] = bad
+    plan = plan_of(t, "f16", bits)
+    out = torch.zeros(2, device="cuda")
+    before = [[x[k].get() for k in sorted(x) if k != "decay"] for x in t]
+    plan.grad_norm(out, max_norm=1.0)
+    assert not np.isfinite(out[0].item())
+    plan.step(1, clip=out, **HYPER)
+    for x, b in zip(t, before):
+        for k, y in zip([k for k in sorted(x) if k != "decay"], b):
+            assert np.array_equal(x[k].get(), y, equal_nan=True), k
+
+
+def test_a_bad_gradient_stays_in_its_place():
+    """Without a clip, NaN and infinity reach their own element's states and weight; in 8 bits the block's states, which read as NaN
+    from then on, and nothing else."""
+    for bits in (32, 8):
+        t = make([1024], "f32", bits)
+        t[0]["grad"].t[300] = float("nan")
+        t[0]["grad"].t[700] = float("inf")
+        plan = plan_of(t, "f32", bits)
+        w, m, v, g = values(t[0], bits)
+        plan.step(1, **HYPER)
+        got_w, got_m, got_v, _ = values(t[0], bits)
+        good = np.ones(1024, bool)
+        good[[300, 700]] = False
+        want = plain_step(w[good], m[good], v[good], g[good], t[0]["decay"], 1, **HYPER)
+        assert np.isfinite(got_w[good]).all() and np.allclose(got_w[good], want[0], rtol=1e-5, atol=1e-7)
+        if bits == 32:
+            assert np.isnan(got_m[300]) and np.isinf(got_m[700]) and np.isfinite(got_m[good]).all() and np.isfinite(got_v[good]).all()
+        else:
+            assert np.isnan(got_m[256:512]).all() and np.isnan(got_v[512:768]).all()
+            assert np.isfinite(got_m[:256]).all() and np.isfinite(got_v[768:]).all() and np.isfinite(got_m[768:]).all()
+            plan.step(2, **HYPER)
+            later = values(t[0], bits)[0]
+            assert np.isnan(later[256:768]).all() and np.isfinite(later[:256]).all() and np.isfinite(later[768:]).all()
+
+
+@pytest.mark.parametrize("scale", [1e-42, 1e-30, 1e-19, 1e15, 1e18])
+def test_8_bit_states_of_extreme_size(scale):
+    """Blocks whose squares are denormal, zero or near overflow: codes as the definition has them."""
+    r = np.random.default_rng(1)
+    n = 1024
+    t = make([n], "f32", 8)
+    for name in ("m", "v"):
+        t[0][name].t.zero_()
+        t[0][name + "_scale"].t.zero_()
+    g = (r.normal(0, 1, n) * 10.0 ** r.uniform(-6, 0, n)).astype(np.float32) * np.float32(scale)
+    t[0]["grad"].t.copy_(torch.from_numpy(g))
+    plan_of(t, "f32", 8).step(1, seed=11, **HYPER)
+    zero = np.zeros(n, np.float32)
+    m32, v32 = moments32(zero, zero, g, 0.9, 0.999, 1.0)
+    for name, x, top, d in (("m", m32, 14, dither(n, 11)[0]), ("v", v32, 30, dither(n, 11)[1])):
+        codes, s = encode(x, top, d)
+        assert np.array_equal(t[0][name + "_scale"].get(), s) and np.array_equal(t[0][name].get(), codes), name
+
+
+def test_8_bit_averages_follow_their_inputs():
+    """An average whose weight is 0.999 moves by less than a hundredth of a code's step in a step; it gets there all the same."""
+    n = 1 << 14
+    t = make([n], "f32", 8)
+    for name in ("m", "v"):
+        t[0][name].t.zero_()
+        t[0][name + "_scale"].t.zero_()
+    r = np.random.default_rng(2)
+    g = (r.normal(0, 1, n) * 10.0 ** r.uniform(-2, 0, n)).astype(np.float32)
+    t[0]["grad"].t.copy_(torch.from_numpy(g))
+    plan = plan_of(t, "f32", 8)
+    steps = 2000
+    for s in range(1, steps + 1):
+        plan.step(s, lr=0.0, seed=s)
+    _, m, v, _ = values(t[0], 8)
+    want_m, want_v = g.astype(np.float64), g.astype(np.float64) ** 2 * (1 - 0.999 ** steps)
+    big = np.abs(g) > 1e-2
+    # a state's own rounding is uniform over a step of up to an eighth, remembered for 1 / (1 - beta) steps: in the mean over
+    # thousands of elements it is gone
+    assert abs(np.mean(m[big] / want_m[big]) - 1) < 0.01
+    assert abs(np.mean(v[big] / want_v[big]) - 1) < 0.02
+
+
+@pytest.mark.parametrize("grad", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("sizes", [[1], [2], [5, 1, 1000], [16384], [16383, 16385], [40000, 3, 100001]], ids=lambda s: "+".join(map(str, s)))
+def test_norm(grad, sizes):
+    r = np.random.default_rng(sum(sizes))
+    gs = [Guarded(r.normal(0, 3, n).astype(np.float32), TYPES[grad]) for n in sizes]
+    norm = B.GradNorm([g.t for g in gs])
+    want = np.sqrt(sum(np.sum(g.get().astype(np.float64) ** 2) for g in gs))
+    out = torch.zeros(2, device="cuda")
+    for max_norm, scale in ((float("inf"), 1.0), (1e-3, -0.25), (want * 10, 1.0), (want * 2, 4.0)):
+        norm.compute(out, grad_scale=scale, max_norm=max_norm)
+        got = out.cpu().numpy().astype(np.float64)
+        w = want * abs(scale)
+        assert abs(got[0] - w) <= 2 * U * w
+        f = min(1.0, max_norm / w)
+        assert abs(got[1] - f) <= 2 * U * f
+
+
+def test_norm_of_extremes():
+    big = torch.full((100000,), 1e30, device="cuda")          # squares beyond 32 bits
+    out = torch.zeros(2, device="cuda")
+    B.GradNorm([big]).compute(out, max_norm=1.0)
+    want = 1e30 * np.sqrt(100000)
+    assert abs(out[0].item() - want) < 1e-6 * want and abs(out[1].item() * want - 1) < 1e-6
+    tiny = torch.full((100000,), 1e-40, device="cuda")        # squares below them
+    B.GradNorm([tiny]).compute(out, max_norm=1.0)
+    want = float(np.float32(1e-40)) * np.sqrt(100000)
+    assert abs(out[0].item() - want) < 1e-4 * want and out[1].item() == 1.0
+    zero = torch.zeros(300, device="cuda")
+    B.GradNorm([zero]).compute(out, max_norm=1.0)
+    assert out.tolist() == [0.0, 1.0]
+    for bad in (float("nan"), float("inf")):
+        zero[299] = bad
+        B.GradNorm([zero]).compute(out, max_norm=1.0)
+        assert not np.isfinite(out[0].item())
+
+
+def test_norm_refuses():
+    n = B.GradNorm([torch.zeros(8, device="cuda")])
+    out = torch.zeros(2, device="cuda")
+    for kw in (dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(grad_scale=float("inf"))):
+        with pytest.raises(B.CdsgdError) as e:
+            n.compute(out, **kw)
+        assert e.value.status == B.ERR_PARAM
+    with pytest.raises(ValueError):
+        n.compute(torch.zeros(3, device="cuda"))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_on_another_stream_and_in_a_graph(bits):
+    """Passes on a stream of their own, eager and replayed, leave the same bits as on the default stream."""
+    kinds = []
+    for how in ("default", "stream", "graph"):
+        t = make([70000, 513, 2], "bf16", bits, copy=True, seed=5)
+        plan = plan_of(t, "bf16", bits)
+        out = torch.zeros(2, device="cuda")
+
+        def go():
+            plan.grad_norm(out, max_norm=0.1)
+            plan.step(3, seed=4, clip=out, **HYPER)
+
+        if how == "default":
+            for _ in range(4):
+                go()
+        else:
+            s = torch.cuda.Stream()
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                go()
+                if how == "stream":
+                    for _ in range(3):
+                        go()
+            torch.cuda.current_stream().wait_stream(s)
+            if how == "graph":
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph):
+                    go()
+                for _ in range(3):
+                    graph.replay()
+                    torch.cuda.synchronize()
+                    torch.zeros(1000, device="cuda").add_(1).sum().item()
+        torch.cuda.synchronize()
+        kinds.append([x[k].get() for x in t for k in sorted(x) if k != "decay"] + [out.cpu().numpy()])
+    for other in kinds[1:]:
+        for a, b in zip(kinds[0], other):
+            assert np.array_equal(a, b)

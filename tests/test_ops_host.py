@@ -1,0 +1,124 @@
+"""Host-side checks of include/cdsgd_ops.h that need no GPU: the library exports what the header declares, and bad arguments
+become status codes before any HIP call."""
+import ctypes
+import os
+import re
+
+import pytest
+
+from paper_2106_10796_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "cdsgd_ops.h")
+A = 0x7F0000000000          # addresses that are never dereferenced
+F32, BF16, F16 = 0, 1, 2
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2106_10796_amd import build
+    build.ensure_built()
+    return B.lib()
+
+
+def _header():
+    with open(HEADER) as fh:
+        return re.sub(r"/\*.*?\*/", "", fh.read(), flags=re.S)
+
+
+def test_library_exports_every_declared_symbol(L):
+    names = sorted(set(re.findall(r"\b(cdsgd_[a-z0-9_]+)\s*\(", _header())))
+    assert len(names) >= 10
+    for name in names:
+        fn = getattr(L, name)
+        assert fn.argtypes is not None, "%s has no signature in the binding" % name
+
+
+def test_constants(L):
+    assert int(re.search(r"#define CDSGD_STATE_BLOCK (\d+)", _header())[1]) == B.STATE_BLOCK
+    for n, blocks in ((1, 1), (256, 1), (257, 2), (1 << 33, 1 << 25)):
+        assert L.cdsgd_state_blocks(n) == blocks
+
+
+def _adamw(n=1000, bits=32, i=0, **over):
+    at = A + i * 0x1000000
+    t = dict(weight=at, weight16=None, grad=at + 0x100000, m=at + 0x200000, v=at + 0x300000,
+             m_scale=at + 0x400000 if bits == 8 else None, v_scale=at + 0x500000 if bits == 8 else None, n=n, weight_decay=0.1)
+    t.update(over)
+    return B.cdsgd_adamw_tensor(**t)
+
+
+def _create(L, tensors, dtype=F32, bits=32):
+    out = ctypes.c_void_p(1)
+    arr = (B.cdsgd_adamw_tensor * max(len(tensors), 1))(*tensors)
+    st = L.cdsgd_adamw_plan_create(arr, len(tensors), dtype, bits, ctypes.byref(out))
+    assert out.value is None
+    return st
+
+
+@pytest.mark.parametrize("want,dtype,bits,over", [
+    (B.ERR_NULL, F32, 32, dict(weight=None)), (B.ERR_NULL, F32, 32, dict(grad=None)),
+    (B.ERR_NULL, F32, 32, dict(m=None)), (B.ERR_NULL, F32, 32, dict(v=None)),
+    (B.ERR_NULL, F32, 8, dict(m_scale=None)), (B.ERR_NULL, F32, 8, dict(v_scale=None)),
+    (B.ERR_PARAM, F32, 32, dict(m_scale=A + 0x700000)), (B.ERR_SIZE, F32, 32, dict(n=0)), (B.ERR_SIZE, F32, 32, dict(n=1 << 50)),
+    (B.ERR_SIZE, F32, 32, dict(n=1 << 39)),
+    (B.ERR_PARAM, F32, 32, dict(weight_decay=-0.1)), (B.ERR_PARAM, F32, 32, dict(weight_decay=float("nan"))),
+    (B.ERR_PARAM, F32, 32, dict(weight16=A + 0x700000)),           # a copy no narrower than the weights
+    (B.ERR_PARAM, 3, 32, {}), (B.ERR_PARAM, F32, 16, {}),
+    (B.ERR_ALIGN, F32, 32, dict(weight=A + 4)), (B.ERR_ALIGN, BF16, 32, dict(grad=A + 0x100008)),
+    (B.ERR_ALIGN, F32, 8, dict(m=A + 0x200001)), (B.ERR_ALIGN, BF16, 8, dict(weight16=A + 0x700002)),
+    (B.ERR_ALIAS, F32, 32, dict(m=A)), (B.ERR_ALIAS, F32, 32, dict(grad=A + 16)), (B.ERR_ALIAS, F32, 8, dict(m_scale=A + 0x200000)),
+    (B.ERR_ALIAS, F32, 8, dict(m_scale=A + 0x200000 + 999)), (B.ERR_ALIAS, F32, 8, dict(v_scale=A + 0x400003)),
+    (B.ERR_ALIAS, F16, 32, dict(weight16=A + 0x100000 + 1984)),
+])
+def test_adamw_plan_refuses(L, want, dtype, bits, over):
+    assert _create(L, [_adamw(bits=bits, **over)], dtype, bits) == want
+    other = {k: (v + 0x1000000 if isinstance(v, int) and v >= A else v) for k, v in over.items()}
+    if "weight16" not in over:
+        assert _create(L, [_adamw(bits=bits), _adamw(bits=bits, i=1, **other)], dtype, bits) == want
+
+
+def test_adamw_refuses_more(L):
+    assert _create(L, []) == B.ERR_SIZE
+    assert L.cdsgd_adamw_plan_create(None, 1, F32, 32, ctypes.byref(ctypes.c_void_p())) == B.ERR_NULL
+    assert L.cdsgd_adamw_plan_create((B.cdsgd_adamw_tensor * 1)(_adamw()), 1, F32, 32, None) == B.ERR_NULL
+    # a 16-bit copy of some tensors alone
+    assert _create(L, [_adamw(), _adamw(i=1, weight16=A + 0x1700000)], BF16) == B.ERR_PARAM
+    assert L.cdsgd_adamw_step(None, 1, 1e-3, 0.9, 0.999, 1e-8, 1.0, 0, None, None) == B.ERR_NULL
+    assert L.cdsgd_adamw_grad_norm(None, 1.0, 1.0, A, None) == B.ERR_NULL
+    assert L.cdsgd_adamw_bind_readout(None, None, None, 0) == B.ERR_NULL
+    assert L.cdsgd_adamw_read_states(None, None) == B.ERR_NULL
+    assert L.cdsgd_adamw_plan_destroy(None) == B.OK
+
+
+def test_grad_norm_refuses(L):
+    out = ctypes.c_void_p(1)
+    one, n = (ctypes.c_void_p * 1)(A), (ctypes.c_size_t * 1)(100)
+    create = L.cdsgd_grad_norm_create
+    assert create(None, n, 1, F32, ctypes.byref(out)) == B.ERR_NULL
+    assert create(one, None, 1, F32, ctypes.byref(out)) == B.ERR_NULL
+    assert create(one, n, 1, F32, None) == B.ERR_NULL
+    assert create(one, n, 0, F32, ctypes.byref(out)) == B.ERR_SIZE
+    assert create(one, n, 1, 7, ctypes.byref(out)) == B.ERR_PARAM
+    assert create((ctypes.c_void_p * 1)(None), n, 1, F32, ctypes.byref(out)) == B.ERR_NULL
+    assert create((ctypes.c_void_p * 1)(A + 8), n, 1, F32, ctypes.byref(out)) == B.ERR_ALIGN
+    for bad in (0, 1 << 50, 1 << 39):
+        assert create(one, (ctypes.c_size_t * 1)(bad), 1, F32, ctypes.byref(out)) == B.ERR_SIZE
+    assert out.value is None
+    assert L.cdsgd_grad_norm_compute(None, 1.0, 1.0, A, None) == B.ERR_NULL
+    assert L.cdsgd_grad_norm_destroy(None) == B.OK
+
+
+def test_binding_says_what_is_wrong(L):
+    import torch
+    t = dict(weight=torch.zeros(4), grad=torch.zeros(4), m=torch.zeros(4), v=torch.zeros(4))
+    with pytest.raises(TypeError, match="weight must be"):
+        B.AdamWPlan([t])
+    with pytest.raises(TypeError, match="gradients must be"):
+        B.AdamWPlan([t], grad_dtype=torch.float64)
+    with pytest.raises(TypeError, match="gradients must be"):
+        B.GradNorm([torch.zeros(4, dtype=torch.float64)])
+    with pytest.raises(TypeError, match=r"grads\[0\] must be"):
+        B.GradNorm([torch.zeros(4)])
+    with pytest.raises(B.CdsgdError):
+        B.GradNorm([])
