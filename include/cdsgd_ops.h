@@ -109,6 +109,50 @@ int cdsgd_adamw_grad_norm(cdsgd_adamw_plan *plan, double grad_scale, double max_
 int cdsgd_adamw_bind_readout(cdsgd_adamw_plan *plan, void *const *m_out, void *const *v_out, int dtype);
 int cdsgd_adamw_read_states(cdsgd_adamw_plan *plan, void *hip_stream);
 
+/*
+ * Matrices in microscaled 4-bit floating point (the MXFP4 of the OCP Microscaling Formats specification 1.0).
+ * Values are 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign; 32 values in a row share a power of two.  A matrix of `rows` by
+ * `cols` is held in two buffers, with g = ceil(cols / 128):
+ *   codes   uint8[rows][64 g]   cdsgd_mxfp4_code_bytes(rows, cols).  Element c of a row is half c % 2 (0: the low one) of byte
+ *                               c / 2: magnitude 0..7 in the order above, sign as bit 3.  16-byte aligned.
+ *   scales  uint8[g][rows][4]   cdsgd_mxfp4_scale_bytes(rows, cols).  Byte j of (i, r) belongs to elements 128 i + 32 j ... + 31 of
+ *                               row r and stands for 2^(byte - 127); 255 is NaN.  4-byte aligned.
+ * Everything from `cols` to 128 g is 0.  (Whole rows of 128: a product's loads need no test along the axis that it sums
+ * over, and the four scales that a matrix instruction takes for a row are one word.)
+ *
+ * cdsgd_mxfp4_quantize   of a matrix x: `codes` / `scales` receive it in blocks along its rows, codes_t / scales_t its
+ *                        transpose in blocks along the transpose's rows, i.e. down x's columns (a matrix of `cols` by `rows`).
+ *                        Either pair may be NULL, not both.  A block's scale is 2^(floor(log2 of the largest magnitude) - 2),
+ *                        not below 2^-127; values are rounded to the nearest, ties to the even code, and above 6 they are 6.
+ *                        A NaN or an infinity in a block makes its scale NaN.  x may have rows further apart than `cols`
+ *                        elements (ld), and needs no more than its own type's alignment.
+ * cdsgd_mxfp4_dequantize the values that a matrix stands for, rounded once if the type has not enough bits; out has rows
+ *                        ld elements apart.
+ * x and out have element type `dtype` (the values of cdsgd_grad_dtype).
+ */
+size_t cdsgd_mxfp4_code_bytes(size_t rows, size_t cols);
+size_t cdsgd_mxfp4_scale_bytes(size_t rows, size_t cols);
+int cdsgd_mxfp4_quantize(const void *x, int dtype, size_t rows, size_t cols, size_t ld, uint8_t *codes, uint8_t *scales,
+                         uint8_t *codes_t, uint8_t *scales_t, void *hip_stream);
+int cdsgd_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, size_t rows, size_t cols, void *out, int dtype,
+                           size_t ld, void *hip_stream);
+
+/*
+ * out[m, n] = sum over k of A[m, k] B[n, k], A (M by K) and B (N by K) as above, summed in fp32 and rounded once to
+ * out's type.  A linear layer's forward pass is x w^T with x and w in blocks along their rows; with the transposes that
+ * cdsgd_mxfp4_quantize writes, the gradients are dx = dy (w^T)^T, summed over the outputs, and dw = dy^T (x^T)^T, summed over
+ * the tokens.  accumulate != 0 adds the product to what out holds (gradients of several micro-batches).
+ *   out        [M][ld], element type `dtype`, aligned to its type
+ *   workspace  cdsgd_mxfp4_matmul_workspace(M, N, K) bytes, 16-byte aligned, NULL where that is 0: room for the partial
+ *              sums of a product with few outputs, whose long axis is split over many workgroups.  Calls that share one
+ *              must be ordered; its content means nothing between calls.
+ *   M, N, K    positive, at most 2^31 - 1; CDSGD_ERR_SIZE if workspace_bytes is less than what is needed
+ */
+size_t cdsgd_mxfp4_matmul_workspace(size_t M, size_t N, size_t K);
+int cdsgd_mxfp4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes, const uint8_t *b_scales, size_t M,
+                       size_t N, size_t K, void *out, int dtype, size_t ld, int accumulate, void *workspace,
+                       size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

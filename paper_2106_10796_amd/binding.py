@@ -11,6 +11,7 @@ that module is not there, or was built for another library, torch or Python, cty
 import ctypes
 import os
 import sysconfig
+from typing import NamedTuple
 
 import torch
 
@@ -195,7 +196,13 @@ def _declare_ops(L):
             ("cdsgd_adamw_step", i, [vp, ctypes.c_long, d, d, d, d, d, ctypes.c_uint64, vp, vp]),
             ("cdsgd_adamw_grad_norm", i, [vp, d, d, vp, vp]),
             ("cdsgd_adamw_bind_readout", i, [vp, pvp, pvp, i]),
-            ("cdsgd_adamw_read_states", i, [vp, vp])):
+            ("cdsgd_adamw_read_states", i, [vp, vp]),
+            ("cdsgd_mxfp4_code_bytes", sz, [sz, sz]),
+            ("cdsgd_mxfp4_scale_bytes", sz, [sz, sz]),
+            ("cdsgd_mxfp4_quantize", i, [vp, i, sz, sz, sz, vp, vp, vp, vp, vp]),
+            ("cdsgd_mxfp4_dequantize", i, [vp, vp, sz, sz, vp, i, sz, vp]),
+            ("cdsgd_mxfp4_matmul_workspace", sz, [sz, sz, sz]),
+            ("cdsgd_mxfp4_matmul", i, [vp, vp, vp, vp, sz, sz, sz, vp, i, sz, i, vp, sz, vp])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = restype, argtypes
 
@@ -573,7 +580,7 @@ class Trainer:
 
 
 # ---------------------------------------------------------------------------
-# include/cdsgd_ops.h: norms of gradients, AdamW
+# include/cdsgd_ops.h: norms of gradients, AdamW, MXFP4
 # ---------------------------------------------------------------------------
 STATE_BLOCK = 256   # CDSGD_STATE_BLOCK
 
@@ -703,3 +710,92 @@ class AdamWPlan:
             self.destroy()
         except Exception:
             pass
+
+
+class _Mxfp4(NamedTuple):
+    codes: torch.Tensor
+    scales: torch.Tensor
+    rows: int
+    cols: int
+
+
+class Mxfp4(_Mxfp4):
+    """A matrix of `rows` by `cols` in microscaled 4-bit floating point (the layout is in include/cdsgd_ops.h):
+    codes uint8 [rows, 64 g] and scales uint8 [g, rows, 4] with g = ceil(cols / 128), contiguous CUDA tensors, which are
+    kept as they are.  Bytes in integers of another type, as a quantiser written in torch leaves them, are converted here."""
+    __slots__ = ()
+
+    def __new__(cls, codes, scales, rows, cols):
+        held = [t.to(torch.uint8).contiguous() if isinstance(t, torch.Tensor) and t.dtype in (torch.int16, torch.int32, torch.int64) else t
+                for t in (codes, scales)]
+        return super().__new__(cls, *held, int(rows), int(cols))
+
+
+def new_mxfp4(rows: int, cols: int, device="cuda") -> Mxfp4:
+    """Room for a matrix; every byte of it is written by cdsgd_mxfp4_quantize."""
+    g = -(-cols // 128)
+    return Mxfp4(torch.empty(rows, 64 * g, dtype=torch.uint8, device=device),
+                 torch.empty(g, rows, 4, dtype=torch.uint8, device=device), rows, cols)
+
+
+def new_mxfp4_workspace(shapes, device="cuda"):
+    """Workspace for products of any of the shapes (M, N, K): a uint8 tensor, or None where none of them needs one."""
+    need = max((int(lib().cdsgd_mxfp4_matmul_workspace(*map(int, s))) for s in shapes), default=0)
+    return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+
+
+def _mx(q, name, rows=None, cols=None):
+    """The addresses of a matrix: (codes, scales); (None, None) for None."""
+    if q is None:
+        return None, None
+    if not isinstance(q, Mxfp4):
+        raise TypeError("%s must be an Mxfp4" % name)
+    if rows is not None and (q.rows, q.cols) != (rows, cols):
+        raise ValueError("%s is a matrix of %d by %d, expected %d by %d" % (name, q.rows, q.cols, rows, cols))
+    g = -(-q.cols // 128)
+    return (_dev(q.codes, torch.uint8, q.rows * 64 * g, name + ".codes"), _dev(q.scales, torch.uint8, q.rows * 4 * g, name + ".scales"))
+
+
+def _rows(t, name, rows=None, cols=None):
+    """(address, type, rows, cols, elements between two rows) of a matrix whose rows are contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in GRAD_DTYPES):
+        raise TypeError("%s must be a CUDA matrix of float32, bfloat16 or float16" % name)
+    if rows is not None and tuple(t.shape) != (rows, cols):
+        raise ValueError("%s is a matrix of %d by %d, expected %d by %d" % (name, *t.shape, rows, cols))
+    r, c = t.shape
+    if (c > 1 and t.stride(1) != 1) or (r > 1 and t.stride(0) < c):
+        raise TypeError("the rows of %s must be contiguous and not overlap" % name)
+    return t.data_ptr(), GRAD_DTYPES[t.dtype], r, c, t.stride(0) if r > 1 else c
+
+
+def cdsgd_mxfp4_quantize(x, row=None, col=None):
+    """x [rows, cols] into `row` (blocks along its rows) and into `col`, its transpose [cols, rows] (blocks down its columns); either
+    may be None."""
+    p, dtype, r, c, ld = _rows(x, "x")
+    codes, scales = _mx(row, "row", r, c)
+    codes_t, scales_t = _mx(col, "col", c, r)
+    st = lib().cdsgd_mxfp4_quantize(p, dtype, r, c, ld, codes, scales, codes_t, scales_t, _stream())
+    if st != OK:
+        _check(st, "cdsgd_mxfp4_quantize")
+
+
+def cdsgd_mxfp4_dequantize(q, out):
+    """The values that q stands for, into out [rows, cols]."""
+    codes, scales = _mx(q, "q")
+    p, dtype, r, c, ld = _rows(out, "out", q.rows, q.cols)
+    st = lib().cdsgd_mxfp4_dequantize(codes, scales, r, c, p, dtype, ld, _stream())
+    if st != OK:
+        _check(st, "cdsgd_mxfp4_dequantize")
+
+
+def cdsgd_mxfp4_matmul(a, b, out, workspace=None, accumulate=False):
+    """out [M, N] = a [M, K] times the transpose of b [N, K]; accumulate adds it to what out holds.  workspace: from
+    new_mxfp4_workspace, not shared by products that may overlap."""
+    ac, as_ = _mx(a, "a")
+    bc, bs = _mx(b, "b", b.rows, a.cols)
+    p, dtype, M, N, ld = _rows(out, "out", a.rows, b.rows)
+    st = lib().cdsgd_mxfp4_matmul(ac, as_, bc, bs, M, N, a.cols, p, dtype, ld, int(bool(accumulate)),
+                                  _dev(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0,
+                                  _stream())
+    if st != OK:
+        _check(st, "cdsgd_mxfp4_matmul")

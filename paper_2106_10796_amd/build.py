@@ -11,7 +11,7 @@ import sysconfig
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "cdsgd.hip")
-SRC_OPS = [os.path.join(PKG, "csrc", name) for name in ("adamw.hip",)]          # translation units of their own
+SRC_OPS = [os.path.join(PKG, "csrc", name) for name in ("adamw.hip", "mxfp4.hip")]   # translation units of their own
 SRC_HOST = [os.path.join(PKG, "csrc", "cdsgd_cost_model.cpp")]   # host-only parts of the library
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcdsgd.so")

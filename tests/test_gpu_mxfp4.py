@@ -1,0 +1,321 @@
+"""Matrices in MXFP4 on the GPU against plain implementations in 64 bits: quantisation and values exactly, products within what
+the rounding of sums in 32 bits can add up to."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2106_10796_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+EPS = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+SHAPES = [(1, 1), (1, 32), (1, 33), (2, 127), (31, 128), (32, 129), (33, 31), (127, 257), (128, 128), (129, 640), (130, 1023), (257, 70),
+          (300, 512), (5, 4099), (1030, 513)]
+
+
+# ---- plain implementations ------------------------------------------------------------------------------------------------
+
+def quantize(x):
+    """(codes, scales) of a matrix in 64 bits, laid out as the header says."""
+    rows, cols = x.shape
+    g = -(-cols // 128)
+    p = np.zeros((rows, g * 128))
+    p[:, :cols] = x
+    b = p.reshape(rows, g * 4, 32)
+    most = np.abs(b).max(2)
+    bad = ~np.isfinite(most)
+    with np.errstate(all="ignore"):
+        e = np.where(most > 0, np.floor(np.log2(np.where(bad | (most == 0), 1, most))), -1000)
+    s = np.where(bad, 255, np.maximum(e - 2, -127) + 127).astype(np.int64)
+    y = np.abs(np.where(bad[:, :, None], 0, b)) * np.exp2(127.0 - s)[:, :, None]
+    d = np.abs(y[..., None] - GRID)
+    near = d.min(-1, keepdims=True)
+    tie = d == near                                             # one grid point, or two neighbours: the even one of them
+    code = np.where(tie.sum(-1) == 2, np.argmax(tie & (np.arange(8) % 2 == 0), -1), np.argmax(tie, -1))
+    code = (code + 8 * np.signbit(b)).reshape(rows, -1)
+    return (code[:, 0::2] + 16 * code[:, 1::2]).astype(np.uint8), s.reshape(rows, g, 4).transpose(1, 0, 2).astype(np.uint8)
+
+
+def values(codes, scales, cols):
+    rows = codes.shape[0]
+    n = np.stack((codes & 15, codes >> 4), 2).reshape(rows, -1).astype(np.int64)
+    s = np.repeat(scales.transpose(1, 0, 2).reshape(rows, -1).astype(np.int64), 32, 1)
+    v = GRID[n & 7] * np.where(n & 8, -1, 1) * np.exp2(s - 127.0)
+    return np.where(s == 255, np.nan, v)[:, :cols]
+
+
+def of(q):
+    return q.codes.cpu().numpy(), q.scales.cpu().numpy()
+
+
+def on_gpu(codes, scales, rows, cols):
+    return B.Mxfp4(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), rows, cols)
+
+
+def room(rows, cols):
+    """An Mxfp4 between guards, and a check that the guards are whole."""
+    g = -(-cols // 128)
+    all_c = torch.full((rows * 64 * g + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    all_s = torch.full((rows * 4 * g + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    q = B.Mxfp4(all_c[128:128 + rows * 64 * g].view(rows, 64 * g), all_s[128:128 + rows * 4 * g].view(g, rows, 4), rows, cols)
+
+    def whole():
+        return all(bool((t[:128] == 0xA5).all()) and bool((t[128 + n:] == 0xA5).all())
+                   for t, n in ((all_c, rows * 64 * g), (all_s, rows * 4 * g)))
+    return q, whole
+
+
+def matrix(rows, cols, dtype, seed, ld=0, spread=6):
+    """A matrix with blocks of very different size, zeros, ties and a row stride of its own: (tensor, values in 64 bits)."""
+    r = np.random.default_rng(seed)
+    x = r.normal(0, 1, (rows, cols)) * 10.0 ** r.uniform(-spread, 0, (rows, 1)) * 10.0 ** r.integers(-1, 2, (rows, cols))
+    x[r.random((rows, cols)) < 0.1] = 0
+    x[r.random((rows, cols)) < 0.2] = r.choice([0.25, -0.75, 1.25, 2.5, -3.5, 5, 7, 4])
+    t = torch.zeros(rows, max(ld, cols), dtype=TYPES[dtype], device="cuda")
+    t[:, cols:] = float("nan")                                   # what lies between the rows is nobody's
+    t[:, :cols] = torch.from_numpy(x)
+    t = t[:, :cols]
+    return t, t.double().cpu().numpy()
+
+
+def random_mx(rows, cols, seed, low=118, high=130):
+    """Codes of every kind, scales within a few binades of one another."""
+    r = np.random.default_rng(seed)
+    g = -(-cols // 128)
+    n = r.integers(0, 16, (rows, g * 128))
+    n[:, cols:] = 0
+    s = r.integers(low, high, (rows, g * 4))
+    s[:, -(-cols // 32):] = 0
+    return ((n[:, 0::2] + 16 * n[:, 1::2]).astype(np.uint8), np.ascontiguousarray(s.reshape(rows, g, 4).transpose(1, 0, 2)).astype(np.uint8))
+
+
+# ---- quantisation ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("forms", ["row", "col", "both"])
+def test_quantize(rows, cols, dtype, forms):
+    x, want = matrix(rows, cols, dtype, rows * 7 + cols, ld=cols + cols % 5)
+    row, whole = room(rows, cols)
+    col, whole_t = room(cols, rows)
+    B.cdsgd_mxfp4_quantize(x, row if forms != "col" else None, col if forms != "row" else None)
+    if forms != "col":
+        codes, scales = quantize(want)
+        got = of(row)
+        assert np.array_equal(got[1], scales) and np.array_equal(got[0], codes)
+    if forms != "row":
+        codes, scales = quantize(want.T)
+        got = of(col)
+        assert np.array_equal(got[1], scales) and np.array_equal(got[0], codes)
+    assert whole() and whole_t()
+
+
+@pytest.mark.parametrize("offset", [1, 2, 3, 5])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_from_any_address(offset, dtype):
+    """Rows that begin at any element, at odd distances."""
+    base, want = matrix(150, 600, dtype, 3)
+    flat = torch.zeros(150 * 601 + 16, dtype=TYPES[dtype], device="cuda")
+    x = torch.as_strided(flat, (150, 600), (601, 1), offset)
+    x.copy_(base)
+    row, col = B.new_mxfp4(150, 600), B.new_mxfp4(600, 150)
+    B.cdsgd_mxfp4_quantize(x, row, col)
+    for q, w in ((row, want), (col, want.T)):
+        codes, scales = quantize(w)
+        assert np.array_equal(of(q)[0], codes) and np.array_equal(of(q)[1], scales)
+
+
+@pytest.mark.parametrize("exponent", [-149, -140, -127, -126, -125, -124, -100, 100, 120, 127])
+def test_quantize_extremes(exponent):
+    """Denormal and huge 32-bit values: the scale stops at 2^-127, and nothing overflows."""
+    with np.errstate(all="ignore"):
+        x = np.ldexp(np.array([1, 1.5, 1.75, 0.875, -0.375, 0, 1.0625, -1.25] * 8), exponent).astype(np.float32).reshape(2, 32)
+    t = torch.from_numpy(x).cuda()
+    row, col = B.new_mxfp4(2, 32), B.new_mxfp4(32, 2)
+    B.cdsgd_mxfp4_quantize(t, row, col)
+    for q, w in ((row, x), (col, x.T)):
+        codes, scales = quantize(w.astype(np.float64))
+        assert np.array_equal(of(q)[1], scales) and np.array_equal(of(q)[0], codes)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_a_block_that_is_not_finite(bad, dtype):
+    x = torch.ones(64, 256, dtype=TYPES[dtype], device="cuda")
+    x[40, 100] = bad
+    row, col = B.new_mxfp4(64, 256), B.new_mxfp4(256, 64)
+    B.cdsgd_mxfp4_quantize(x, row, col)
+    out, out_t = torch.zeros(64, 256, device="cuda"), torch.zeros(256, 64, device="cuda")
+    B.cdsgd_mxfp4_dequantize(row, out)
+    B.cdsgd_mxfp4_dequantize(col, out_t)
+    want = torch.ones(64, 256)
+    want[40, 96:128] = float("nan")
+    want_t = torch.ones(256, 64)
+    want_t[100, 32:64] = float("nan")
+    assert torch.equal(out.cpu().isnan(), want.isnan()) and torch.equal(out.cpu().nan_to_num(7), want.nan_to_num(7))
+    assert torch.equal(out_t.cpu().isnan(), want_t.isnan()) and torch.equal(out_t.cpu().nan_to_num(7), want_t.nan_to_num(7))
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_values(rows, cols, dtype):
+    codes, scales = random_mx(rows, cols, rows + cols, 110, 140)
+    scales[0, 0, 0] = 255
+    q = on_gpu(codes, scales, rows, cols)
+    ld = cols + 3
+    flat = torch.full((rows * ld + 64,), 77.0, dtype=TYPES[dtype], device="cuda")
+    out = torch.as_strided(flat, (rows, cols), (ld, 1), 1)
+    B.cdsgd_mxfp4_dequantize(q, out)
+    want = torch.from_numpy(values(codes, scales, cols)).to(TYPES[dtype])
+    assert torch.equal(out.cpu().nan_to_num(5), want.nan_to_num(5)) and torch.equal(out.cpu().isnan(), want.isnan())
+    out.fill_(77.0)
+    assert bool((flat == 77).all())                             # nothing between the rows or around them
+
+
+def test_values_at_the_ends_of_the_scale():
+    scales = np.zeros((1, 6, 4), np.uint8)
+    scales[0, :, 0] = [0, 1, 2, 252, 253, 254]
+    codes = np.zeros((6, 64), np.uint8)
+    codes[:, :8] = np.arange(8) * 2 + 16 * (np.arange(8) * 2 + 1)          # every code
+    out = torch.zeros(6, 16, device="cuda")
+    B.cdsgd_mxfp4_dequantize(on_gpu(codes, scales, 6, 16), out)
+    with np.errstate(over="ignore"):
+        want = values(codes, scales, 16).astype(np.float32)
+    assert np.array_equal(out.cpu().numpy(), want)
+
+
+# ---- products -------------------------------------------------------------------------------------------------------------
+
+def check_product(M, N, K, dtype, seed=0, accumulate=False, ld=0):
+    ac, as_ = random_mx(M, K, seed)
+    bc, bs = random_mx(N, K, seed + 1)
+    a, b = on_gpu(ac, as_, M, K), on_gpu(bc, bs, N, K)
+    ld = max(ld, N)
+    flat = torch.full((M * ld + 64,), 77.0, dtype=TYPES[dtype], device="cuda")
+    out = torch.as_strided(flat, (M, N), (ld, 1), 32)
+    start = torch.zeros(M, N, dtype=torch.float64)
+    if accumulate:
+        out.copy_(torch.randn(M, N, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)))
+        start = out.double().cpu()
+    B.cdsgd_mxfp4_matmul(a, b, out, B.new_mxfp4_workspace([(M, N, K)]), accumulate=accumulate)
+    va, vb = torch.from_numpy(values(ac, as_, K)), torch.from_numpy(values(bc, bs, K))
+    want = va @ vb.T
+    # 32 products under one pair of scales are multiples of a quarter below 2^11 and add up exactly; the sums of the blocks are
+    # rounded once each, in any order, and the result once
+    size = va.abs() @ vb.abs().T
+    bound = (K / 32 + 8) * U * size + EPS[dtype] * (want + start).abs() + U * start.abs() + (1e-7 if dtype == "f16" else 1e-30)
+    got = out.double().cpu()
+    err = (got - want - start).abs()
+    assert bool((err <= bound).all()), "worst %g of its bound" % float((err / bound).max())
+    out.fill_(77.0)
+    assert bool((flat == 77).all())
+
+
+SMALL = [(1, 1, 1), (1, 1, 32), (2, 3, 33), (1, 16, 128), (16, 16, 128), (17, 15, 129), (31, 33, 300), (32, 32, 256), (1, 1000, 640),
+         (3, 129, 2049), (16, 255, 1024), (33, 64, 130), (64, 65, 4096), (65, 127, 384), (127, 128, 513), (128, 129, 1000), (129, 256, 257),
+         (255, 257, 900), (256, 256, 2048), (257, 300, 1), (300, 511, 777), (513, 520, 1536), (1, 2000, 25088), (5, 40, 30000), (128, 384, 8192),
+         (200, 1030, 640), (1024, 768, 512), (1025, 1100, 385)]
+
+
+@pytest.mark.parametrize("M,N,K", SMALL)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_product(M, N, K, dtype):
+    check_product(M, N, K, dtype, seed=M + N + K)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 100, 513), (7, 1000, 4096), (64, 130, 300), (130, 257, 2049), (512, 600, 256), (1100, 1030, 700)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_product_added_to_a_strided_result(M, N, K, dtype):
+    check_product(M, N, K, dtype, seed=M, accumulate=True, ld=N + 13)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 64, 1024), (40, 64, 1024), (300, 300, 1024), (1200, 1100, 512)])
+def test_a_nan_stays_in_its_row_and_column(M, N, K):
+    ac, as_ = random_mx(M, K, 1)
+    bc, bs = random_mx(N, K, 2)
+    as_[1, M - 1, 2] = 255
+    bs[K // 128 - 1, N - 2, 3] = 255
+    out = torch.zeros(M, N, device="cuda")
+    B.cdsgd_mxfp4_matmul(on_gpu(ac, as_, M, K), on_gpu(bc, bs, N, K), out, B.new_mxfp4_workspace([(M, N, K)]))
+    want = torch.zeros(M, N, dtype=torch.bool)
+    want[M - 1] = True
+    want[:, N - 2] = True
+    assert torch.equal(out.cpu().isnan(), want)
+
+
+def test_products_of_the_smallest_scales():
+    """A block of scale 0 is 2^-127, not nothing; under the other operand's largest scale it counts."""
+    a, b = np.zeros((2, 64), np.uint8), np.zeros((3, 64), np.uint8)
+    a[:, :16], b[:, :16] = 0x22, 0x22                                # 32 ones
+    sa, sb = np.zeros((1, 2, 4), np.uint8), np.zeros((1, 3, 4), np.uint8)
+    sb[0, :, 0] = [254, 127, 0]
+    out = torch.zeros(2, 3, device="cuda")
+    B.cdsgd_mxfp4_matmul(on_gpu(a, sa, 2, 32), on_gpu(b, sb, 3, 32), out)
+    assert np.array_equal(out.cpu().numpy()[0], np.array([32.0, 32 * 2.0 ** -127, 0.0], np.float32))
+
+
+def test_matmul_refuses():
+    a, b, out = B.new_mxfp4(4, 256), B.new_mxfp4(8, 256), torch.zeros(4, 8, device="cuda")
+    with pytest.raises(ValueError, match="b is a matrix of 8 by 128"):
+        B.cdsgd_mxfp4_matmul(a, B.new_mxfp4(8, 128), out)
+    with pytest.raises(ValueError, match="out is a matrix of 8 by 4"):
+        B.cdsgd_mxfp4_matmul(a, b, out.t().contiguous())
+    with pytest.raises(TypeError, match="rows of out"):
+        B.cdsgd_mxfp4_matmul(a, b, torch.zeros(8, 4, device="cuda").t())
+    with pytest.raises(TypeError, match="rows of out"):
+        B.cdsgd_mxfp4_matmul(a, b, torch.zeros(8, device="cuda").expand(4, 8))
+    with pytest.raises(TypeError, match="float32, bfloat16 or float16"):
+        B.cdsgd_mxfp4_matmul(a, b, out.double())
+    with pytest.raises(ValueError, match="codes has"):
+        B.cdsgd_mxfp4_matmul(B.Mxfp4(a.codes[:3], a.scales, 4, 256), b, out)
+    with pytest.raises(ValueError, match="row is a matrix"):
+        B.cdsgd_mxfp4_quantize(torch.zeros(5, 256, device="cuda"), a)
+    with pytest.raises(B.CdsgdError) as e:
+        B.cdsgd_mxfp4_quantize(torch.zeros(4, 256, device="cuda"))
+    assert e.value.status == B.ERR_NULL
+
+
+# ---- a linear layer -------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens,outs,ins", [(1, 40, 70), (33, 64, 128), (200, 129, 300)])
+def test_gradients_of_a_linear_layer(tokens, outs, ins):
+    """dx and dw by the formulas, and dx against differences of the layer's own output: it is linear in its quantised input."""
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=gen)  # noqa: E731
+    x, w, dy = rnd(tokens, ins), rnd(outs, ins), rnd(tokens, outs)
+    qx, qx_t, qw, qw_t = B.new_mxfp4(tokens, ins), B.new_mxfp4(ins, tokens), B.new_mxfp4(outs, ins), B.new_mxfp4(ins, outs)
+    qdy, qdy_t = B.new_mxfp4(tokens, outs), B.new_mxfp4(outs, tokens)
+    B.cdsgd_mxfp4_quantize(x, qx, qx_t)
+    B.cdsgd_mxfp4_quantize(w, qw, qw_t)
+    B.cdsgd_mxfp4_quantize(dy, qdy, qdy_t)
+    ws = B.new_mxfp4_workspace([(tokens, outs, ins), (tokens, ins, outs), (outs, ins, tokens)])
+    y, dx, dw = (torch.zeros(*s, device="cuda") for s in ((tokens, outs), (tokens, ins), (outs, ins)))
+    B.cdsgd_mxfp4_matmul(qx, qw, y, ws)
+    B.cdsgd_mxfp4_matmul(qdy, qw_t, dx, ws)
+    B.cdsgd_mxfp4_matmul(qdy_t, qx_t, dw, ws)
+    v = {n: values(*of(q), q.cols) for n, q in (("x", qx), ("x_t", qx_t), ("w", qw), ("w_t", qw_t), ("dy", qdy), ("dy_t", qdy_t))}
+    for got, p, q in ((y, "x", "w"), (dx, "dy", "w_t"), (dw, "dy_t", "x_t")):
+        want, size = v[p] @ v[q].T, np.abs(v[p]) @ np.abs(v[q]).T
+        assert np.all(np.abs(got.cpu().numpy() - want) <= (v[p].shape[1] / 32 + 8) * U * size + U * np.abs(want))
+    # differences: the loss sum(dy y) at inputs that differ by one quantised step in one place; y is linear, so the difference is the
+    # gradient with the weight's row form, whose values the column form's differ from by the two quantisations alone
+    at = (tokens // 2, ins // 3)
+    codes = qx.codes.clone()
+    byte, half = at[1] // 2, at[1] % 2
+    old = int(codes[at[0], byte])
+    new = (old & 0xF0 | (old & 0xF ^ 0x7)) if half == 0 else (old & 0x0F | (old & 0xF0 ^ 0x70))
+    codes[at[0], byte] = new
+    q2 = B.Mxfp4(codes, qx.scales, tokens, ins)
+    y2 = torch.zeros_like(y)
+    B.cdsgd_mxfp4_matmul(q2, qw, y2, ws)
+    step = values(*of(q2), ins)[at] - v["x"][at]
+    assert step != 0
+    slope = float((v["dy"] * (y2.double() - y.double()).cpu().numpy()).sum()) / step
+    want = float(v["dy"][at[0]] @ v["w"][:, at[1]])
+    noise = float(np.abs(v["dy"][at[0]]).sum()) * U * (ins / 32 + 8) * float((np.abs(v["x"]) @ np.abs(v["w"]).T).max()) / abs(step)
+    assert abs(slope - want) <= noise
+    # the weight in blocks down its columns is within a quarter of a binade's step of the one in blocks along its rows
+    assert abs(float(dx[at].item()) - want) <= float(np.abs(v["dy"][at[0]]) @ (np.abs(v["w"][:, at[1]] - v["w_t"][at[1]]))) + 1e-3

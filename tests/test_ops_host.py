@@ -122,3 +122,88 @@ def test_binding_says_what_is_wrong(L):
         B.GradNorm([torch.zeros(4)])
     with pytest.raises(B.CdsgdError):
         B.GradNorm([])
+
+
+def test_mxfp4_sizes(L):
+    for r, c, g in ((1, 1, 1), (3, 128, 1), (3, 129, 2), (100000, 25088, 196)):
+        assert L.cdsgd_mxfp4_code_bytes(r, c) == r * g * 64 and L.cdsgd_mxfp4_scale_bytes(r, c) == r * g * 4
+
+
+Q = [A + i * 0x10000000 for i in range(8)]     # buffers far apart
+
+
+def test_mxfp4_quantize_refuses(L):
+    f = L.cdsgd_mxfp4_quantize
+    ok = [Q[0], F32, 100, 200, 200, Q[1], Q[2], Q[3], Q[4], None]
+
+    def st(**over):
+        names = ("x", "dtype", "rows", "cols", "ld", "codes", "scales", "codes_t", "scales_t", "stream")
+        return f(*[over.get(n, v) for n, v in zip(names, ok)])
+    for over in (dict(x=None), dict(codes=None), dict(scales=None), dict(codes_t=None), dict(scales_t=None),
+                 dict(codes=None, scales=None, codes_t=None, scales_t=None)):
+        assert st(**over) == B.ERR_NULL, over
+    assert st(dtype=3) == B.ERR_PARAM
+    for over in (dict(rows=0), dict(cols=0), dict(rows=1 << 31), dict(cols=1 << 31), dict(ld=199), dict(ld=1 << 50)):
+        assert st(**over) == B.ERR_SIZE, over
+    for over in (dict(x=Q[0] + 2), dict(dtype=BF16, x=Q[0] + 1), dict(codes=Q[1] + 8), dict(scales=Q[2] + 2), dict(codes_t=Q[3] + 4),
+                 dict(scales_t=Q[4] + 1)):
+        assert st(**over) == B.ERR_ALIGN, over
+    for over in (dict(codes=Q[0]), dict(codes_t=Q[1]), dict(scales=Q[1] + 100 * 128 - 4), dict(scales_t=Q[3]),
+                 dict(codes=Q[0] + 4 * (99 * 200 + 200) // 16 * 16 - 16)):
+        assert st(**over) == B.ERR_ALIAS, over
+
+
+def test_mxfp4_dequantize_refuses(L):
+    f = L.cdsgd_mxfp4_dequantize
+    assert f(None, Q[1], 10, 20, Q[2], F32, 20, None) == B.ERR_NULL
+    assert f(Q[0], None, 10, 20, Q[2], F32, 20, None) == B.ERR_NULL
+    assert f(Q[0], Q[1], 10, 20, None, F32, 20, None) == B.ERR_NULL
+    assert f(Q[0], Q[1], 10, 20, Q[2], 5, 20, None) == B.ERR_PARAM
+    assert f(Q[0], Q[1], 0, 20, Q[2], F32, 20, None) == B.ERR_SIZE
+    assert f(Q[0], Q[1], 10, 20, Q[2], F32, 19, None) == B.ERR_SIZE
+    assert f(Q[0] + 4, Q[1], 10, 20, Q[2], F32, 20, None) == B.ERR_ALIGN
+    assert f(Q[0], Q[1] + 2, 10, 20, Q[2], F32, 20, None) == B.ERR_ALIGN
+    assert f(Q[0], Q[1], 10, 20, Q[2] + 2, F32, 20, None) == B.ERR_ALIGN
+    assert f(Q[0], Q[1], 10, 20, Q[0] + 16, F32, 20, None) == B.ERR_ALIAS
+    assert f(Q[0], Q[1], 10, 20, Q[1] + 36, F32, 20, None) == B.ERR_ALIAS
+
+
+def test_mxfp4_matmul_refuses(L):
+    names = ("ac", "as_", "bc", "bs", "M", "N", "K", "out", "dtype", "ld", "add", "ws", "wb", "stream")
+    ok = [Q[0], Q[1], Q[2], Q[3], 300, 400, 500, Q[4], F32, 400, 0, Q[5], 1 << 27, None]
+
+    def st(**over):
+        return L.cdsgd_mxfp4_matmul(*[over.get(n, v) for n, v in zip(names, ok)])
+    for n in ("ac", "as_", "bc", "bs", "out"):
+        assert st(**{n: None}) == B.ERR_NULL
+    assert st(dtype=9) == B.ERR_PARAM
+    for over in (dict(M=0), dict(N=0), dict(K=0), dict(M=1 << 31), dict(N=1 << 31, ld=1 << 31), dict(K=1 << 31), dict(ld=399)):
+        assert st(**over) == B.ERR_SIZE, over
+    for over in (dict(ac=Q[0] + 8), dict(bc=Q[2] + 1), dict(as_=Q[1] + 2), dict(bs=Q[3] + 1), dict(out=Q[4] + 2), dict(ws=Q[5] + 8)):
+        assert st(**over) == B.ERR_ALIGN, over
+    for over in (dict(out=Q[0]), dict(out=Q[1] + 4), dict(out=Q[2] - 4), dict(out=Q[3])):
+        assert st(**over) == B.ERR_ALIAS, over
+    # a product that needs a workspace
+    shapes = [(m, n, k) for m in (1, 16, 64, 300) for n in (128, 400, 4096) for k in (4096, 25088)]
+    for M, N, K in [s for s in shapes if L.cdsgd_mxfp4_matmul_workspace(*s)]:
+        need = L.cdsgd_mxfp4_matmul_workspace(M, N, K)
+        assert need % 16 == 0
+        assert st(M=M, N=N, K=K, ld=N, ws=None, wb=0) == B.ERR_NULL
+        assert st(M=M, N=N, K=K, ld=N, wb=need - 1) == B.ERR_SIZE
+        assert st(M=M, N=N, K=K, ld=N, ws=Q[4], wb=need) == B.ERR_ALIAS
+        assert st(M=M, N=N, K=K, ld=N, ws=Q[2], wb=need) == B.ERR_ALIAS
+
+
+def test_mxfp4_binding_says_what_is_wrong(L):
+    import torch
+    q = B.new_mxfp4(3, 130, device="cpu")
+    assert q.codes.shape == (3, 128) and q.scales.shape == (2, 3, 4)
+    with pytest.raises(TypeError, match="x must be a CUDA matrix"):
+        B.cdsgd_mxfp4_quantize(torch.zeros(3, 130), q)
+    with pytest.raises(TypeError, match="q must be an Mxfp4"):
+        B.cdsgd_mxfp4_dequantize(q.codes, torch.zeros(3, 130))
+    with pytest.raises(TypeError, match=r"a.codes must be"):
+        B.cdsgd_mxfp4_matmul(q, q, torch.zeros(3, 3))
+    assert B.new_mxfp4_workspace([]) is None
+    wide = B.Mxfp4(q.codes.long(), q.scales, 3, 130)
+    assert wide.codes.dtype == torch.uint8 and torch.equal(wide.codes, q.codes) and wide.scales is q.scales
