@@ -146,7 +146,8 @@ int cdsgd_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, size_t r
  *   workspace  cdsgd_mxfp4_matmul_workspace(M, N, K) bytes, 16-byte aligned, NULL where that is 0: room for the partial
  *              sums of a product with few outputs, whose long axis is split over many workgroups.  Calls that share one
  *              must be ordered; its content means nothing between calls.
- *   M, N, K    positive, at most 2^31 - 1; CDSGD_ERR_SIZE if workspace_bytes is less than what is needed
+ *   M, N       positive, at most 2^29;  K positive, at most 2^24
+ *   errors     CDSGD_ERR_SIZE also if workspace_bytes is less than what is needed
  */
 size_t cdsgd_mxfp4_matmul_workspace(size_t M, size_t N, size_t K);
 int cdsgd_mxfp4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes, const uint8_t *b_scales, size_t M,

@@ -1,4 +1,4 @@
-// Matrices in microscaled 4-bit floating point: quantisation along rows and columns, values, products.
+// Matrices in microscaled 4-bit floating point: quantisation along rows and columns, values, the matrix instruction.
 #pragma once
 
 namespace {
@@ -261,48 +261,6 @@ template <int DT>
 __device__ __forceinline__ void put(Elem<DT> *p, float v, bool add)
 {
     *p = (Elem<DT>)(add ? (float)*p + v : v);
-}
-
-// A wave per 32 by 32 outputs, operands straight from memory.
-template <int DT>
-__global__ __launch_bounds__(64) void k_mxfp4_simple(const uint8_t *__restrict__ a, const uint8_t *__restrict__ as,
-                                                     const uint8_t *__restrict__ b, const uint8_t *__restrict__ bs, unsigned M,
-                                                     unsigned N, unsigned groups, Elem<DT> *__restrict__ out, size_t ld, int add)
-{
-    const unsigned across = (N + 31u) / 32u, m0 = blockIdx.x / across * 32u, n0 = blockIdx.x % across * 32u;
-    const unsigned l = threadIdx.x % 16u, j = threadIdx.x / 16u;
-    const size_t stride = (size_t)groups * 64u;
-    unsigned ra[2], rb[2];
-#pragma unroll
-    for (unsigned i = 0; i < 2; ++i) {
-        ra[i] = m0 + 16u * i + l < M ? m0 + 16u * i + l : M - 1u;
-        rb[i] = n0 + 16u * i + l < N ? n0 + 16u * i + l : N - 1u;
-    }
-    f4 c[2][2] = {};
-    for (unsigned g = 0; g < groups; ++g) {
-        i4v va[2], vb[2];
-        int sa[2], sb[2];
-#pragma unroll
-        for (unsigned i = 0; i < 2; ++i) {
-            va[i] = *reinterpret_cast<const i4v *>(a + ra[i] * stride + g * 64u + j * 16u);
-            vb[i] = *reinterpret_cast<const i4v *>(b + rb[i] * stride + g * 64u + j * 16u);
-            sa[i] = as[((size_t)g * M + ra[i]) * 4u + j];
-            sb[i] = bs[((size_t)g * N + rb[i]) * 4u + j];
-        }
-#pragma unroll
-        for (unsigned i = 0; i < 2; ++i)
-#pragma unroll
-            for (unsigned k = 0; k < 2; ++k) c[i][k] = mfma16<0, 0>(va[i], vb[k], c[i][k], sa[i], sb[k]);
-    }
-#pragma unroll
-    for (unsigned i = 0; i < 2; ++i)
-#pragma unroll
-        for (unsigned k = 0; k < 2; ++k)
-#pragma unroll
-            for (unsigned q = 0; q < 4; ++q) {
-                const unsigned m = m0 + 16u * i + 4u * j + q, n = n0 + 16u * k + l;
-                if (m < M && n < N) put<DT>(out + (size_t)m * ld + n, c[i][k][q], add);
-            }
 }
 
 }  // namespace

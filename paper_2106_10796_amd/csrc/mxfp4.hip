@@ -1,5 +1,5 @@
 // Matrices in microscaled 4-bit floating point (include/cdsgd_ops.h): the C ABI's host side.  The kernels are in
-// kernels_mxfp4.hpp.
+// kernels_mxfp4.hpp (quantisation, values) and kernels_mxfp4_product.hpp.
 
 #include <hip/hip_runtime.h>
 
@@ -13,6 +13,7 @@
 #include "device_common.hpp"
 
 #include "kernels_mxfp4.hpp"
+#include "kernels_mxfp4_product.hpp"
 
 namespace {
 
@@ -20,6 +21,13 @@ inline bool good_dtype(int t) { return t == CDSGD_GRAD_F32 || t == CDSGD_GRAD_BF
 inline size_t bytes_of(int dtype) { return dtype == CDSGD_GRAD_F32 ? 4u : 2u; }
 inline size_t groups_of(size_t cols) { return (cols + kGroup - 1) / kGroup; }
 inline bool good_extent(size_t n) { return n > 0 && n <= 0x7FFFFFFFu; }
+
+// Sizes of a product that the kernels hold in 32 bits: offsets inside a tile of 256 rows, and scale words of two groups.
+inline bool good_product(size_t M, size_t N, size_t K)
+{
+    constexpr size_t kMostRows = (size_t)1 << 29, kMostSum = (size_t)1 << 24;
+    return M > 0 && M <= kMostRows && N > 0 && N <= kMostRows && K > 0 && K <= kMostSum;
+}
 
 // Bytes from the first element of a matrix to the last, both included.
 inline size_t extent_bytes(size_t rows, size_t cols, size_t ld, size_t elem) { return ((rows - 1) * ld + cols) * elem; }
@@ -41,6 +49,57 @@ inline int check_matrix(size_t rows, size_t cols)
 }
 
 constexpr unsigned long long kMostGroups = 0xFFFFFFFFull / 256;  // workgroups of 256 lanes in a launch
+
+// How a product is computed.  Few rows of A, and a matrix B that is read once: rings of a wave's own (ring: fragments of 16 rows of
+// A to a group, and its waves).  Otherwise tiles, whose sum is split over groups where it is long and the tiles are few.
+struct Product {
+    int ring_rows, ring_waves;  // 0: tiles
+    int tile;
+    unsigned splits;
+};
+
+inline unsigned long long count_of(size_t n, size_t each) { return (n + each - 1) / each; }
+
+// us, bf16 results, three sets of operands in turn; rWxF: rings of W waves, F fragments; tB: tiles of B by B; /S: split S ways
+//   16 x 8192 x 8192    r8x1 9.0, r4x1 10.6, t64 11.2            5 x 8192 x 300     r8x1 2.7, r4x1 2.5;  1 x 25088 x 512 6.1, 4.0
+//   32 x 8192 x 8192    r8x2 12.0, r4x2 10.7, t64 11.3           32 x 4096 x 4096   r8x2 3.4, r4x2 3.6
+//   128 x 1000 x 25088  r8x2 11.7, r4x4 15.0, t64 28.5           96 x 4096 x 4096   r8x2 9.8, r4x2 7.1, t64 6.9
+//   64 x 4096 x 4096    r8x2 7.0, r4x4 4.8, t64 6.5              64 x 8192 x 8192   r4x4 14.5, t64 11.8
+//   512 x 4096 x 4096   t64 10.6, t128 14.1, t256 24.3           256 x 8192 x 8192  t64 17.6, t128 27.0;  300 x 8192 x 300 5.4, 4.4
+//   512 x 8192 x 8192   t64 34.4, t128 31.5, t256 44.8           1024 x 4096 x 4096 t64 18.2, t128 16.8, t256 24.9
+//   2048 x 8192 x 8192  t128 89.4, t256 74.2                     2048 x 4096 x 25088 t128 124.7, t256 139.4
+//   256 x 4096 x 25088  t64 33.3, t128 67.1, t128/2 41.8, /4 30.7   512 x 4096 x 25088 t64 55.5, t128 68.0, /2 47.4, /4 46.8
+//   256 x 4096 x 4096   t64 7.7, t128/2 16.3: the parts' way through memory and the second launch are worth 64 stages
+inline Product product_of(size_t M, size_t N, size_t K)
+{
+    const unsigned long long n16 = count_of(N, 16);
+    if (M <= 16) return {1, n16 <= 512 ? 8 : 4, 0, 1};
+    if (M <= 128 && n16 * count_of(M, 32) <= 256) return {2, 8, 0, 1};
+    if (M <= 32) return {2, 4, 0, 1};
+    if (M <= 64 && n16 <= 256) return {4, 4, 0, 1};
+    const unsigned long long t64 = count_of(M, 64) * count_of(N, 64), t128 = count_of(M, 128) * count_of(N, 128),
+                             t256 = count_of(M, 256) * count_of(N, 256), stages = count_of(K, 256);
+    if (stages >= 64 && t128 >= 32 && t128 <= 128) return {0, 0, 128, 4};
+    if (t64 <= 512) return {0, 0, 64, 1};
+    if (t256 < 192 || stages < 8) return {0, 0, 128, 1};
+    return {0, 0, 256, 1};
+}
+
+// Calls f(kernel, groups, lanes) with the kernel that `how` names, for results of type DT.
+template <int DT, typename F>
+void with_product_kernel(const Product &how, size_t M, size_t N, F f)
+{
+    const auto ring = [&](auto kernel) { f(kernel, count_of(M, 16u * how.ring_rows) * count_of(N, 16), 64u * how.ring_waves); };
+    const unsigned long long tiles = how.tile ? count_of(M, how.tile) * count_of(N, how.tile) * how.splits : 0;
+    if (how.ring_rows == 1 && how.ring_waves == 8) ring(k_ring<DT, 1, 1, 2, 8>);
+    else if (how.ring_rows == 1) ring(k_ring<DT, 1, 1, 2, 4>);
+    else if (how.ring_rows == 2 && how.ring_waves == 8) ring(k_ring<DT, 2, 1, 2, 8>);
+    else if (how.ring_rows == 2) ring(k_ring<DT, 2, 1, 2, 4>);
+    else if (how.ring_rows == 4) ring(k_ring<DT, 4, 1, 2, 4>);
+    else if (how.tile == 64) f(k_tiles<DT, 64, 64, 2, 2, 4>, tiles, 256u);
+    else if (how.tile == 128) f(k_tiles<DT, 128, 128, 2, 2, 2>, tiles, 256u);
+    else f(k_tiles<DT, 256, 256, 2, 4, 2>, tiles, 512u);
+}
 
 }  // namespace
 
@@ -106,7 +165,12 @@ int cdsgd_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, size_t r
     return launch_status();
 }
 
-size_t cdsgd_mxfp4_matmul_workspace(size_t, size_t, size_t) { return 0; }
+size_t cdsgd_mxfp4_matmul_workspace(size_t M, size_t N, size_t K)
+{
+    if (!good_product(M, N, K)) return 0;
+    const unsigned splits = product_of(M, N, K).splits;
+    return splits > 1 ? (splits * M * N * sizeof(float) + 15u) / 16u * 16u : 0;
+}
 
 int cdsgd_mxfp4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes, const uint8_t *b_scales, size_t M,
                        size_t N, size_t K, void *out, int dtype, size_t ld, int accumulate, void *workspace, size_t workspace_bytes,
@@ -114,7 +178,7 @@ int cdsgd_mxfp4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const ui
 {
     if (!a_codes || !a_scales || !b_codes || !b_scales || !out) return CDSGD_ERR_NULL;
     if (!good_dtype(dtype)) return CDSGD_ERR_PARAM;
-    if (!good_extent(M) || !good_extent(N) || !good_extent(K) || ld < N || ld > (size_t)1 << 40) return CDSGD_ERR_SIZE;
+    if (!good_product(M, N, K) || ld < N || ld > (size_t)1 << 40) return CDSGD_ERR_SIZE;
     const size_t want = cdsgd_mxfp4_matmul_workspace(M, N, K);
     if (want && !workspace) return CDSGD_ERR_NULL;
     if (workspace_bytes < want) return CDSGD_ERR_SIZE;
@@ -128,13 +192,34 @@ int cdsgd_mxfp4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const ui
     for (int i = 0; i < 4; ++i)
         if (overlap2(out, ob, in[i], bytes[i]) || (want && overlap2(workspace, want, in[i], bytes[i]))) return CDSGD_ERR_ALIAS;
     if (want && overlap2(out, ob, workspace, want)) return CDSGD_ERR_ALIAS;
-    const unsigned long long tiles = (unsigned long long)((M + 31) / 32) * ((N + 31) / 32);
-    if (tiles > 0xFFFFFFFFull / 64) return CDSGD_ERR_SIZE;
-    with_dtype(dtype, [&](auto dt) {
-        constexpr int DT = decltype(dt)::value;
-        hipLaunchKernelGGL((k_mxfp4_simple<DT>), dim3((unsigned)tiles), dim3(64), 0, (hipStream_t)hip_stream, a_codes, a_scales, b_codes,
-                           b_scales, (unsigned)M, (unsigned)N, (unsigned)groups_of(K), static_cast<Elem<DT> *>(out), ld, accumulate);
-    });
+    const Product how = product_of(M, N, K);
+    int status = CDSGD_OK;
+    hipStream_t s = (hipStream_t)hip_stream;
+    const unsigned m = (unsigned)M, n = (unsigned)N, groups = (unsigned)groups_of(K);
+    const auto launch = [&](auto kernel, unsigned long long count, unsigned lanes, auto *to, size_t row, int add) {
+        if (count > 0xFFFFFFFFull / lanes) status = CDSGD_ERR_SIZE;
+        else hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(lanes), 0, s, a_codes, a_scales, b_codes, b_scales, m, n, groups, to, row, add, how.splits);
+    };
+    if (how.splits > 1) {
+        float *parts = static_cast<float *>(workspace);
+        const unsigned long long quads = count_of(N, 4) * M;
+        if (quads > kMostGroups * 256) return CDSGD_ERR_SIZE;
+        with_product_kernel<kGradF32>(how, M, N, [&](auto kernel, unsigned long long count, unsigned lanes) { launch(kernel, count, lanes, parts, N, 0); });
+        with_dtype(dtype, [&](auto dt) {
+            constexpr int DT = decltype(dt)::value;
+            if (status == CDSGD_OK)
+                hipLaunchKernelGGL((k_join<DT>), dim3((unsigned)count_of(quads, 256)), dim3(256), 0, s, parts, m, n, how.splits,
+                                   static_cast<Elem<DT> *>(out), ld, accumulate);
+        });
+    } else {
+        with_dtype(dtype, [&](auto dt) {
+            constexpr int DT = decltype(dt)::value;
+            with_product_kernel<DT>(how, M, N, [&](auto kernel, unsigned long long count, unsigned lanes) {
+                launch(kernel, count, lanes, static_cast<Elem<DT> *>(out), ld, accumulate);
+            });
+        });
+    }
+    if (status != CDSGD_OK) return status;
     return launch_status();
 }
 

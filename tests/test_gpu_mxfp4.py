@@ -217,7 +217,7 @@ def check_product(M, N, K, dtype, seed=0, accumulate=False, ld=0):
 SMALL = [(1, 1, 1), (1, 1, 32), (2, 3, 33), (1, 16, 128), (16, 16, 128), (17, 15, 129), (31, 33, 300), (32, 32, 256), (1, 1000, 640),
          (3, 129, 2049), (16, 255, 1024), (33, 64, 130), (64, 65, 4096), (65, 127, 384), (127, 128, 513), (128, 129, 1000), (129, 256, 257),
          (255, 257, 900), (256, 256, 2048), (257, 300, 1), (300, 511, 777), (513, 520, 1536), (1, 2000, 25088), (5, 40, 30000), (128, 384, 8192),
-         (200, 1030, 640), (1024, 768, 512), (1025, 1100, 385)]
+         (200, 1030, 640), (1024, 768, 512), (1025, 1100, 385), (600, 800, 16500), (129, 4001, 16384)]
 
 
 @pytest.mark.parametrize("M,N,K", SMALL)
@@ -226,7 +226,7 @@ def test_product(M, N, K, dtype):
     check_product(M, N, K, dtype, seed=M + N + K)
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 100, 513), (7, 1000, 4096), (64, 130, 300), (130, 257, 2049), (512, 600, 256), (1100, 1030, 700)])
+@pytest.mark.parametrize("M,N,K", [(1, 100, 513), (7, 1000, 4096), (64, 130, 300), (130, 257, 2049), (512, 600, 256), (1100, 1030, 700), (520, 1000, 16700)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_product_added_to_a_strided_result(M, N, K, dtype):
     check_product(M, N, K, dtype, seed=M, accumulate=True, ld=N + 13)

@@ -177,15 +177,17 @@ def test_mxfp4_matmul_refuses(L):
     for n in ("ac", "as_", "bc", "bs", "out"):
         assert st(**{n: None}) == B.ERR_NULL
     assert st(dtype=9) == B.ERR_PARAM
-    for over in (dict(M=0), dict(N=0), dict(K=0), dict(M=1 << 31), dict(N=1 << 31, ld=1 << 31), dict(K=1 << 31), dict(ld=399)):
+    for over in (dict(M=0), dict(N=0), dict(K=0), dict(M=(1 << 29) + 1), dict(N=(1 << 29) + 1, ld=1 << 30), dict(K=(1 << 24) + 1), dict(ld=399)):
         assert st(**over) == B.ERR_SIZE, over
     for over in (dict(ac=Q[0] + 8), dict(bc=Q[2] + 1), dict(as_=Q[1] + 2), dict(bs=Q[3] + 1), dict(out=Q[4] + 2), dict(ws=Q[5] + 8)):
         assert st(**over) == B.ERR_ALIGN, over
     for over in (dict(out=Q[0]), dict(out=Q[1] + 4), dict(out=Q[2] - 4), dict(out=Q[3])):
         assert st(**over) == B.ERR_ALIAS, over
     # a product that needs a workspace
-    shapes = [(m, n, k) for m in (1, 16, 64, 300) for n in (128, 400, 4096) for k in (4096, 25088)]
-    for M, N, K in [s for s in shapes if L.cdsgd_mxfp4_matmul_workspace(*s)]:
+    shapes = [(m, n, k) for m in (1, 16, 64, 300) for n in (128, 400, 4096) for k in (4096, 25088)] + [(600, 800, 16500)]
+    shapes = [s for s in shapes if L.cdsgd_mxfp4_matmul_workspace(*s)]
+    assert shapes
+    for M, N, K in shapes:
         need = L.cdsgd_mxfp4_matmul_workspace(M, N, K)
         assert need % 16 == 0
         assert st(M=M, N=N, K=K, ld=N, ws=None, wb=0) == B.ERR_NULL
