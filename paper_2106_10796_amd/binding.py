@@ -77,7 +77,8 @@ _calls = _Declines()
 # in the order in which _calls.bind takes them
 _CALLED = ("cdsgd_quantize_pack", "cdsgd_decode_sum", "cdsgd_decode_sum_sparse", "cdsgd_update", "cdsgd_sparse_encode",
            "cdsgd_sparse_words", "cdsgd_sparse_segments", "cdsgd_step_fused", "cdsgd_step_fused_range",
-           "cdsgd_step_fused_static")
+           "cdsgd_step_fused_static", "cdsgd_grad_norm_compute", "cdsgd_adamw_step", "cdsgd_adamw_grad_norm",
+           "cdsgd_adamw_read_states", "cdsgd_mxfp4_quantize", "cdsgd_mxfp4_dequantize", "cdsgd_mxfp4_matmul")
 
 
 def _native():
@@ -600,7 +601,7 @@ class GradNorm:
     """The norm of a list of gradients (cdsgd_grad_norm_*): contiguous CUDA tensors of one type.  Keeps references to them."""
 
     def __init__(self, grads):
-        self._handle = None
+        self._handle = self._at = None
         dtype = grads[0].dtype if len(grads) else torch.float32
         if dtype not in GRAD_DTYPES:
             raise TypeError("gradients must be float32, bfloat16 or float16")
@@ -610,19 +611,21 @@ class GradNorm:
         handle = ctypes.c_void_p()
         st = lib().cdsgd_grad_norm_create(arr, sizes, len(grads), GRAD_DTYPES[dtype], ctypes.byref(handle))
         _check(st, "cdsgd_grad_norm_create")
-        self._handle, self._keep = handle, list(grads)
+        self._handle, self._at, self._keep = handle, handle.value, list(grads)
 
     def compute(self, out, grad_scale=1.0, max_norm=float("inf")):
         """out (float32, 2 elements) receives the norm and the factor that brings it down to max_norm."""
-        st = lib().cdsgd_grad_norm_compute(self._handle, float(grad_scale), float(max_norm), _dev(out, torch.float32, 2, "out"),
-                                           _stream())
+        st = _calls.grad_norm_compute(self._at, out, grad_scale, max_norm, _stream)
+        if st < 0:
+            st = lib().cdsgd_grad_norm_compute(self._handle, float(grad_scale), float(max_norm), _dev(out, torch.float32, 2, "out"),
+                                               _stream())
         if st != OK:
             _check(st, "cdsgd_grad_norm_compute")
 
     def destroy(self):
         if self._handle is not None and self._handle.value:
             lib().cdsgd_grad_norm_destroy(self._handle)
-        self._handle = self._keep = None
+        self._handle = self._at = self._keep = None
 
     def __del__(self):
         try:
@@ -667,15 +670,19 @@ class AdamWPlan:
 
     def step(self, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, seed=0, clip=None):
         """Step number `step` (from 1 on).  clip: the out of grad_norm, or None.  seed: another one for every step with 8-bit states."""
-        st = lib().cdsgd_adamw_step(self._handle, int(step), float(lr), float(beta1), float(beta2), float(eps), float(grad_scale),
-                                    int(seed) & 0xFFFFFFFFFFFFFFFF, _dev(clip, torch.float32, 2, "clip"), _stream())
+        st = _calls.adamw_step(self._at, step, lr, beta1, beta2, eps, grad_scale, seed, clip, _stream)
+        if st < 0:
+            st = lib().cdsgd_adamw_step(self._handle, int(step), float(lr), float(beta1), float(beta2), float(eps), float(grad_scale),
+                                        int(seed) & 0xFFFFFFFFFFFFFFFF, _dev(clip, torch.float32, 2, "clip"), _stream())
         if st != OK:
             _check(st, "cdsgd_adamw_step")
 
     def grad_norm(self, out, grad_scale=1.0, max_norm=float("inf")):
         """The norm of the plan's gradients and the factor for clipping, into out (float32, 2 elements)."""
-        st = lib().cdsgd_adamw_grad_norm(self._handle, float(grad_scale), float(max_norm), _dev(out, torch.float32, 2, "out"),
-                                         _stream())
+        st = _calls.adamw_grad_norm(self._at, out, grad_scale, max_norm, _stream)
+        if st < 0:
+            st = lib().cdsgd_adamw_grad_norm(self._handle, float(grad_scale), float(max_norm), _dev(out, torch.float32, 2, "out"),
+                                             _stream())
         if st != OK:
             _check(st, "cdsgd_adamw_grad_norm")
 
@@ -696,7 +703,9 @@ class AdamWPlan:
 
     def read_states(self):
         """The values that 8-bit states stand for, into the tensors of bind_readout."""
-        st = lib().cdsgd_adamw_read_states(self._handle, _stream())
+        st = _calls.adamw_read_states(self._at, _stream)
+        if st < 0:
+            st = lib().cdsgd_adamw_read_states(self._handle, _stream())
         if st != OK:
             _check(st, "cdsgd_adamw_read_states")
 
@@ -771,19 +780,23 @@ def _rows(t, name, rows=None, cols=None):
 def cdsgd_mxfp4_quantize(x, row=None, col=None):
     """x [rows, cols] into `row` (blocks along its rows) and into `col`, its transpose [cols, rows] (blocks down its columns); either
     may be None."""
-    p, dtype, r, c, ld = _rows(x, "x")
-    codes, scales = _mx(row, "row", r, c)
-    codes_t, scales_t = _mx(col, "col", c, r)
-    st = lib().cdsgd_mxfp4_quantize(p, dtype, r, c, ld, codes, scales, codes_t, scales_t, _stream())
+    st = _native().mxfp4_quantize(x, row, col, _stream)
+    if st < 0:
+        p, dtype, r, c, ld = _rows(x, "x")
+        codes, scales = _mx(row, "row", r, c)
+        codes_t, scales_t = _mx(col, "col", c, r)
+        st = lib().cdsgd_mxfp4_quantize(p, dtype, r, c, ld, codes, scales, codes_t, scales_t, _stream())
     if st != OK:
         _check(st, "cdsgd_mxfp4_quantize")
 
 
 def cdsgd_mxfp4_dequantize(q, out):
     """The values that q stands for, into out [rows, cols]."""
-    codes, scales = _mx(q, "q")
-    p, dtype, r, c, ld = _rows(out, "out", q.rows, q.cols)
-    st = lib().cdsgd_mxfp4_dequantize(codes, scales, r, c, p, dtype, ld, _stream())
+    st = _native().mxfp4_dequantize(q, out, _stream)
+    if st < 0:
+        codes, scales = _mx(q, "q")
+        p, dtype, r, c, ld = _rows(out, "out", q.rows, q.cols)
+        st = lib().cdsgd_mxfp4_dequantize(codes, scales, r, c, p, dtype, ld, _stream())
     if st != OK:
         _check(st, "cdsgd_mxfp4_dequantize")
 
@@ -791,11 +804,13 @@ def cdsgd_mxfp4_dequantize(q, out):
 def cdsgd_mxfp4_matmul(a, b, out, workspace=None, accumulate=False):
     """out [M, N] = a [M, K] times the transpose of b [N, K]; accumulate adds it to what out holds.  workspace: from
     new_mxfp4_workspace, not shared by products that may overlap."""
-    ac, as_ = _mx(a, "a")
-    bc, bs = _mx(b, "b", b.rows, a.cols)
-    p, dtype, M, N, ld = _rows(out, "out", a.rows, b.rows)
-    st = lib().cdsgd_mxfp4_matmul(ac, as_, bc, bs, M, N, a.cols, p, dtype, ld, int(bool(accumulate)),
-                                  _dev(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0,
-                                  _stream())
+    st = _native().mxfp4_matmul(a, b, out, workspace, accumulate, _stream)
+    if st < 0:
+        ac, as_ = _mx(a, "a")
+        bc, bs = _mx(b, "b", b.rows, a.cols)
+        p, dtype, M, N, ld = _rows(out, "out", a.rows, b.rows)
+        st = lib().cdsgd_mxfp4_matmul(ac, as_, bc, bs, M, N, a.cols, p, dtype, ld, int(bool(accumulate)),
+                                      _dev(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0,
+                                      _stream())
     if st != OK:
         _check(st, "cdsgd_mxfp4_matmul")

@@ -12,8 +12,10 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
+#include <cstring>
 
 #include "cdsgd.h"
+#include "cdsgd_ops.h"
 
 namespace {
 
@@ -28,6 +30,13 @@ struct Library {
     decltype(&cdsgd_step_fused) step_fused;
     decltype(&cdsgd_step_fused_range) step_fused_range;
     decltype(&cdsgd_step_fused_static) step_fused_static;
+    decltype(&cdsgd_grad_norm_compute) grad_norm_compute;
+    decltype(&cdsgd_adamw_step) adamw_step;
+    decltype(&cdsgd_adamw_grad_norm) adamw_grad_norm;
+    decltype(&cdsgd_adamw_read_states) adamw_read_states;
+    decltype(&cdsgd_mxfp4_quantize) mxfp4_quantize;
+    decltype(&cdsgd_mxfp4_dequantize) mxfp4_dequantize;
+    decltype(&cdsgd_mxfp4_matmul) mxfp4_matmul;
 } lib;
 
 struct NotPlain {};  // leave it to the binding
@@ -51,11 +60,13 @@ float *floats(PyObject *o, size_t n, size_t *numel = nullptr) { return static_ca
 float *floats_or_null(PyObject *o, size_t n) { return o == Py_None ? nullptr : floats(o, n); }
 uint32_t *words(PyObject *o, size_t n) { return static_cast<uint32_t *>(buffer(o, at::kInt, n)); }
 
-float number(PyObject *o)
+double real(PyObject *o)
 {
-    if (PyFloat_CheckExact(o)) return (float)PyFloat_AS_DOUBLE(o);
+    if (PyFloat_CheckExact(o)) return PyFloat_AS_DOUBLE(o);
     throw NotPlain();
 }
+
+float number(PyObject *o) { return (float)real(o); }
 
 long whole(PyObject *o)
 {
@@ -232,6 +243,140 @@ PyObject *step_static(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// A handle's address (not 0: a handle that has been destroyed).
+template <typename T>
+T *handle(PyObject *o)
+{
+    T *p = address<T>(o);
+    if (!p) throw NotPlain();
+    return p;
+}
+
+template <typename Handle, typename Call>
+PyObject *norm_of(PyObject *const *a, Py_ssize_t n, Call f)
+{
+    return guarded(n, 5, [&] {
+        Handle *h = handle<Handle>(a[0]);
+        float *out = floats(a[1], 2);
+        const double scale = real(a[2]), max_norm = real(a[3]);
+        void *s = stream_of(a[4]);
+        return unlocked([&] { return (lib.*f)(h, scale, max_norm, out, s); });
+    });
+}
+
+PyObject *grad_norm_compute(PyObject *, PyObject *const *a, Py_ssize_t n) { return norm_of<cdsgd_grad_norm>(a, n, &Library::grad_norm_compute); }
+PyObject *adamw_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n) { return norm_of<cdsgd_adamw_plan>(a, n, &Library::adamw_grad_norm); }
+
+PyObject *adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&] {
+        cdsgd_adamw_plan *plan = handle<cdsgd_adamw_plan>(a[0]);
+        const long i = whole(a[1]);
+        const double lr = real(a[2]), beta1 = real(a[3]), beta2 = real(a[4]), eps = real(a[5]), scale = real(a[6]);
+        if (!PyLong_CheckExact(a[7])) throw NotPlain();
+        const uint64_t seed = PyLong_AsUnsignedLongLongMask(a[7]);
+        const float *clip = floats_or_null(a[8], 2);
+        void *s = stream_of(a[9]);
+        return unlocked([&] { return lib.adamw_step(plan, i, lr, beta1, beta2, eps, scale, seed, clip, s); });
+    });
+}
+
+PyObject *adamw_read_states(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 2, [&] {
+        cdsgd_adamw_plan *plan = handle<cdsgd_adamw_plan>(a[0]);
+        void *s = stream_of(a[1]);
+        return unlocked([&] { return lib.adamw_read_states(plan, s); });
+    });
+}
+
+// A matrix in MXFP4, as the binding's class of that name holds it.
+struct Mx {
+    uint8_t *codes = nullptr, *scales = nullptr;
+    size_t rows = 0, cols = 0;
+};
+
+Mx mx(PyObject *o)
+{
+    if (!PyTuple_Check(o) || std::strcmp(Py_TYPE(o)->tp_name, "Mxfp4") != 0 || PyTuple_GET_SIZE(o) != 4) throw NotPlain();
+    const long rows = whole(PyTuple_GET_ITEM(o, 2)), cols = whole(PyTuple_GET_ITEM(o, 3));
+    if (rows < 1 || cols < 1 || rows > INT_MAX || cols > INT_MAX) throw NotPlain();
+    const size_t groups = ((size_t)cols + 127) / 128;
+    Mx q;
+    q.rows = (size_t)rows;
+    q.cols = (size_t)cols;
+    q.codes = static_cast<uint8_t *>(buffer(PyTuple_GET_ITEM(o, 0), at::kByte, q.rows * 64 * groups));
+    q.scales = static_cast<uint8_t *>(buffer(PyTuple_GET_ITEM(o, 1), at::kByte, q.rows * 4 * groups));
+    return q;
+}
+
+// A matrix of ordinary numbers whose rows are contiguous and do not overlap.
+struct Matrix {
+    void *p;
+    int dtype;
+    size_t rows, cols, ld;
+};
+
+Matrix matrix(PyObject *o)
+{
+    if (!THPVariable_CheckExact(o)) throw NotPlain();
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.dim() != 2) throw NotPlain();
+    Matrix m;
+    switch (t.scalar_type()) {
+    case at::kFloat: m.dtype = CDSGD_GRAD_F32; break;
+    case at::kBFloat16: m.dtype = CDSGD_GRAD_BF16; break;
+    case at::kHalf: m.dtype = CDSGD_GRAD_F16; break;
+    default: throw NotPlain();
+    }
+    const int64_t rows = t.size(0), cols = t.size(1), row = t.stride(0);
+    if (rows < 1 || cols < 1 || (cols > 1 && t.stride(1) != 1) || (rows > 1 && row < cols)) throw NotPlain();
+    m.p = t.data_ptr();
+    m.rows = (size_t)rows;
+    m.cols = (size_t)cols;
+    m.ld = (size_t)(rows > 1 ? row : cols);
+    return m;
+}
+
+PyObject *mxfp4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 4, [&] {
+        const Matrix x = matrix(a[0]);
+        const Mx row = a[1] == Py_None ? Mx() : mx(a[1]), col = a[2] == Py_None ? Mx() : mx(a[2]);
+        if ((row.codes && (row.rows != x.rows || row.cols != x.cols)) || (col.codes && (col.rows != x.cols || col.cols != x.rows))) throw NotPlain();
+        void *s = stream_of(a[3]);
+        return unlocked([&] { return lib.mxfp4_quantize(x.p, x.dtype, x.rows, x.cols, x.ld, row.codes, row.scales, col.codes, col.scales, s); });
+    });
+}
+
+PyObject *mxfp4_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 3, [&] {
+        const Mx q = mx(a[0]);
+        const Matrix out = matrix(a[1]);
+        if (out.rows != q.rows || out.cols != q.cols) throw NotPlain();
+        void *s = stream_of(a[2]);
+        return unlocked([&] { return lib.mxfp4_dequantize(q.codes, q.scales, q.rows, q.cols, out.p, out.dtype, out.ld, s); });
+    });
+}
+
+PyObject *mxfp4_matmul(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 6, [&] {
+        const Mx x = mx(a[0]), y = mx(a[1]);
+        const Matrix out = matrix(a[2]);
+        if (x.cols != y.cols || out.rows != x.rows || out.cols != y.rows) throw NotPlain();
+        size_t room = 0;
+        void *workspace = a[3] == Py_None ? nullptr : buffer(a[3], at::kByte, kAny, &room);
+        if (a[4] != Py_False && a[4] != Py_True) throw NotPlain();
+        const int add = a[4] == Py_True;
+        void *s = stream_of(a[5]);
+        return unlocked([&] {
+            return lib.mxfp4_matmul(x.codes, x.scales, y.codes, y.scales, x.rows, y.rows, x.cols, out.p, out.dtype, out.ld, add, workspace, room, s);
+        });
+    });
+}
+
 // bind(addresses of the library's functions, in the order of `Library`)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -261,7 +406,11 @@ PyMethodDef method(const char *name, F f)
 PyMethodDef methods[] = {method("bind", bind), method("quantize_pack", quantize_pack), method("decode_sum", decode_sum),
                          method("decode_sum_sparse", decode_sum_sparse), method("update", update),
                          method("sparse_encode", sparse_encode), method("step", step), method("step_range", step_range),
-                         method("step_static", step_static), {nullptr, nullptr, 0, nullptr}};
+                         method("step_static", step_static),
+                         method("grad_norm_compute", grad_norm_compute), method("adamw_step", adamw_step),
+                         method("adamw_grad_norm", adamw_grad_norm), method("adamw_read_states", adamw_read_states),
+                         method("mxfp4_quantize", mxfp4_quantize), method("mxfp4_dequantize", mxfp4_dequantize),
+                         method("mxfp4_matmul", mxfp4_matmul), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

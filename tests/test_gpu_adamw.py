@@ -437,3 +437,35 @@ def test_on_another_stream_and_in_a_graph(bits):
     for other in kinds[1:]:
         for a, b in zip(kinds[0], other):
             assert np.array_equal(a, b)
+
+
+class _Declines:
+    def __getattr__(self, name):
+        return lambda *a: -1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_both_ways_of_marshalling_do_the_same(monkeypatch, bits):
+    got = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(B, "_calls", _Declines())
+        t = make([700, 4097], "bf16", bits, copy=True, seed=8)
+        plan, out, alone = plan_of(t, "bf16", bits), torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda")
+        plan.grad_norm(out, 0.5, 0.01)
+        norm = B.GradNorm([x["grad"].t for x in t])
+        norm.compute(alone, 0.5, 0.01)
+        plan.step(3, 1e-2, 0.8, 0.99, 1e-7, 0.5, 1 << 63, out)
+        outs = []
+        if bits == 8:
+            outs = [[torch.zeros(700, device="cuda"), torch.zeros(4097, device="cuda")] for _ in range(2)]
+            plan.bind_readout(*outs)
+            plan.read_states()
+        got.append([x[k].get() for x in t for k in sorted(x) if k != "decay"] + [o.cpu().numpy() for o in (out, alone, *sum(outs, []))])
+        plan.destroy()
+        norm.destroy()
+        for call in (lambda: plan.step(3, 1e-2), lambda: plan.grad_norm(out), plan.read_states, lambda: norm.compute(out)):
+            with pytest.raises(B.CdsgdError) as e:
+                call()
+            assert e.value.status == B.ERR_NULL
+    assert all(np.array_equal(a, b) for a, b in zip(*got))

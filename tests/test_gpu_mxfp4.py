@@ -319,3 +319,27 @@ def test_gradients_of_a_linear_layer(tokens, outs, ins):
     assert abs(slope - want) <= noise
     # the weight in blocks down its columns is within a quarter of a binade's step of the one in blocks along its rows
     assert abs(float(dx[at].item()) - want) <= float(np.abs(v["dy"][at[0]]) @ (np.abs(v["w"][:, at[1]] - v["w_t"][at[1]]))) + 1e-3
+
+
+class _Declines:
+    def __getattr__(self, name):
+        return lambda *a: -1
+
+
+def test_both_ways_of_marshalling_do_the_same(monkeypatch):
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, w = torch.randn(70, 300, device="cuda", generator=gen), torch.randn(90, 300, device="cuda", generator=gen)
+    got = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(B, "_calls", _Declines())
+        qx, qw, qt = B.new_mxfp4(70, 300), B.new_mxfp4(90, 300), B.new_mxfp4(300, 90)
+        for t in (*qx[:2], *qw[:2], *qt[:2]):
+            t.fill_(7)
+        B.cdsgd_mxfp4_quantize(x, qx)
+        B.cdsgd_mxfp4_quantize(w, qw, qt)
+        y, back = torch.ones(70, 90, device="cuda", dtype=torch.bfloat16), torch.zeros(300, 90, device="cuda")
+        B.cdsgd_mxfp4_matmul(qx, qw, y, None, accumulate=True)
+        B.cdsgd_mxfp4_dequantize(qt, back)
+        got.append((*qx[:2], *qw[:2], *qt[:2], y, back))
+    assert all(torch.equal(a, b) for a, b in zip(*got))

@@ -209,3 +209,26 @@ def test_mxfp4_binding_says_what_is_wrong(L):
     assert B.new_mxfp4_workspace([]) is None
     wide = B.Mxfp4(q.codes.long(), q.scales, 3, 130)
     assert wide.codes.dtype == torch.uint8 and torch.equal(wide.codes, q.codes) and wide.scales is q.scales
+
+
+def test_native_calls_decline_what_is_not_plainly_good(L):
+    import torch
+    native = B._native()
+    if isinstance(native, B._Declines):
+        pytest.skip("the native calls are not there")
+
+    def no_stream():
+        raise AssertionError("asked for a stream though an argument is not good")
+
+    f, q = torch.zeros(4, 256), B.new_mxfp4(4, 256, device="cpu")
+    two = torch.zeros(2)
+    for got in (native.mxfp4_quantize(f, q, None, no_stream), native.mxfp4_quantize(None, q, None, no_stream), native.mxfp4_quantize(f, q, None),
+                native.mxfp4_dequantize(q, f, no_stream), native.mxfp4_dequantize(tuple(q), f, no_stream),
+                native.mxfp4_matmul(q, q, f, None, False, no_stream), native.mxfp4_matmul(q, q, f, None, 0, no_stream),
+                native.adamw_step(None, 1, 0.1, 0.9, 0.999, 1e-8, 1.0, 0, None, no_stream),
+                native.adamw_step(0, 1, 0.1, 0.9, 0.999, 1e-8, 1.0, 0, None, no_stream),
+                native.adamw_step(16, 1, 1, 0.9, 0.999, 1e-8, 1.0, 0, None, no_stream),
+                native.adamw_step(16, 1, 0.1, 0.9, 0.999, 1e-8, 1.0, 0, two, no_stream),
+                native.adamw_grad_norm(None, two, 1.0, 1.0, no_stream), native.adamw_grad_norm(16, two, 1.0, 1.0, no_stream),
+                native.grad_norm_compute(None, two, 1.0, 1.0, no_stream), native.adamw_read_states(None, no_stream)):
+        assert got == -1
