@@ -26,10 +26,30 @@ inline size_t bytes_of(int dtype) { return dtype == CDSGD_GRAD_F32 ? 4u : 2u; }
 // A launch of one wave per piece stays below 2^32 threads, and a table below 1 GiB.
 constexpr unsigned long long kMaxStepChunks = 1ull << 22, kMaxNormChunks = 1ull << 24;
 
+inline unsigned norm_elems(int dtype) { return kNormBytes / (unsigned)bytes_of(dtype); }
+
 inline unsigned long long pieces(size_t n, unsigned each) { return (n + each - 1ull) / each; }
 
-// Groups of k_grad_norm: as many as are resident at once with their loads in flight (eight on each of 256 compute units).
-constexpr unsigned kNormGroups = 2048;
+// Groups of k_grad_norm.  A group's turn at the counter takes 12 ns, so there are as few as keep the memory busy (us, fp32, 64 / 128
+// / 256 / 512 / 1024 groups: 4 M elements 7.7 / 6.3 / 7.0 / 9.5 / 9.5, 8 M 13.2 / 9.1 / 9.2 / 11.9 / 17.2, 26 M 35.6 / 21.3 / 17.8 /
+// 20.2 / 23.7, 138 M 183 / 109 / 80 / 83 / 89).
+inline unsigned norm_groups(unsigned chunks) { return chunks <= 128 ? chunks : (chunks <= 512 ? 128 : 256); }
+
+// How the caches are used, and LDS that a wave asks for to bound the waves resident (160 KiB / bytes), by the length of the list.
+//   up to kShortList     loads keep what they find, stores are written through and stay in the memory-side cache
+//   up to kLongList      loads keep, stores are written through and do not stay
+//   above                loads do not keep either (states in 32 bits; in 8 bits as before)
+// us, bf16 gradients with a copy, three sets of buffers in turn / ten, which no cache holds:
+//   32 bits   non-temporal   2 M 10.1 / 10.6   4 M 19.2 / 19.6   8 M 36.0 / 36.4   26 M 109   138 M 594
+//             first form     2 M  7.2 / 11.4   4 M 13.6 / 21.4   8 M 39.3 / 39.9   26 M 120   138 M 640
+//             second         2 M 10.0 / 10.4   4 M 18.6 / 18.8   8 M 35.0 / 35.1   26 M 105   138 M 615
+//             third          2 M     -         4 M 18.1          8 M 36.1          26 M 110   138 M 586
+//   8 bits    non-temporal   2 M  7.6 /  8.1   4 M 13.6 / 14.4   8 M 24.2 / 24.5   26 M 69    138 M 364
+//             first form     2 M  6.3 /  7.0   4 M 10.4 / 16.1   8 M 18.0 / 27.0   26 M 74    138 M 376
+//             second         2 M  7.7 /  8.6   4 M 13.9 / 14.3   8 M 23.2 / 23.3   26 M 63    138 M 360
+// Waves resident, second form: 32 bits 26 M, all 112, 20 waves 108, 16 107, 13 105, 10 107;  8 bits 26 M, all 65.0, 22 63.4, 20 64.7,
+// 16 66.5;  138 M 393, 375, 360, 365.
+constexpr unsigned long long kShortList = 2500000, kMidList = 16ull << 20, kLongList = 64ull << 20;
 
 struct Block {  // device memory of a handle
     void *p = nullptr;
@@ -70,6 +90,7 @@ struct cdsgd_adamw_plan {
     std::vector<size_t> sizes;
     Block block;
     cdsgd_grad_norm norm;
+    unsigned long long elements = 0;
     int grad_dtype = 0, state_bits = kState32, readout_dtype = -1;
     bool copies = false;
 
@@ -85,20 +106,20 @@ int norm_create(cdsgd_grad_norm &h, const void *const *grads, const size_t *size
         if (!grads[i]) return CDSGD_ERR_NULL;
         if (sizes[i] == 0 || sizes[i] > (size_t)1 << 40) return CDSGD_ERR_SIZE;
         if (!aligned(grads[i], 16)) return CDSGD_ERR_ALIGN;
-        total += pieces(sizes[i], kNormChunk);
+        total += pieces(sizes[i], norm_elems(grad_dtype));
         if (total > kMaxNormChunks) return CDSGD_ERR_SIZE;
     }
     h.grad_dtype = grad_dtype;
     h.num_chunks = (unsigned)total;
-    h.groups = h.num_chunks < kNormGroups ? h.num_chunks : kNormGroups;
+    h.groups = norm_groups(h.num_chunks);
     // counter, partial sums, chunks
     const size_t off_p = 256, off_c = off_p + ((sizeof(double) * h.groups + 255) & ~(size_t)255);
     std::vector<unsigned char> image(off_c + sizeof(NormChunk) * (size_t)total, 0);
     NormChunk *c = reinterpret_cast<NormChunk *>(image.data() + off_c);
     for (int i = 0; i < num_tensors; ++i)
-        for (size_t at = 0; at < sizes[i]; at += kNormChunk, ++c) {
+        for (size_t at = 0; at < sizes[i]; at += norm_elems(grad_dtype), ++c) {
             c->grad = static_cast<const char *>(grads[i]) + at * bytes_of(grad_dtype);
-            c->elems = (unsigned)(sizes[i] - at < kNormChunk ? sizes[i] - at : kNormChunk);
+            c->elems = (unsigned)(sizes[i] - at < norm_elems(grad_dtype) ? sizes[i] - at : norm_elems(grad_dtype));
         }
     const int rc = h.block.fill(image.data(), image.size());
     if (rc != CDSGD_OK) return rc;
@@ -213,6 +234,7 @@ try {
         const cdsgd_adamw_tensor &t = tensors[i];
         grads.push_back(t.grad);
         plan->sizes.push_back(t.n);
+        plan->elements += t.n;
         for (size_t at = 0; at < t.n; at += kStepChunk) {
             StepChunk c{};
             c.weight = t.weight + at;
@@ -268,18 +290,25 @@ int cdsgd_adamw_step(cdsgd_adamw_plan *plan, long step, double lr, double beta1,
     hipStream_t s = (hipStream_t)hip_stream;
     const unsigned per = kStepChunk / (plan->state_bits == kState32 ? kStepLanes * 4u : kStep8Elems);
     const dim3 grid((unsigned)plan->host_chunks.size() * per), block(kStepLanes);
-#define CDSGD_LAUNCH_ADAMW(KERNEL, GT, COPY) \
-    hipLaunchKernelGGL((KERNEL<GT, COPY, kStream>), grid, block, 0, s, plan->chunks(), per, clip, f)
-#define CDSGD_LAUNCH_ADAMW_T(KERNEL)                                                                            \
-    do {                                                                                                        \
-        if (plan->grad_dtype == CDSGD_GRAD_BF16 && plan->copies) CDSGD_LAUNCH_ADAMW(KERNEL, kGradBF16, true);   \
-        else if (plan->grad_dtype == CDSGD_GRAD_BF16) CDSGD_LAUNCH_ADAMW(KERNEL, kGradBF16, false);             \
-        else if (plan->grad_dtype == CDSGD_GRAD_F16 && plan->copies) CDSGD_LAUNCH_ADAMW(KERNEL, kGradF16, true);\
-        else if (plan->grad_dtype == CDSGD_GRAD_F16) CDSGD_LAUNCH_ADAMW(KERNEL, kGradF16, false);               \
-        else CDSGD_LAUNCH_ADAMW(KERNEL, kGradF32, false);                                                       \
+    const unsigned long long n = plan->elements;
+#define CDSGD_LAUNCH_ADAMW(KERNEL, GT, COPY, LOAD, STORE, LDS) \
+    hipLaunchKernelGGL((KERNEL<GT, COPY, LOAD, STORE>), grid, block, LDS, s, plan->chunks(), per, clip, f)
+#define CDSGD_LAUNCH_ADAMW_T(KERNEL, LOAD, STORE, LDS)                                                                              \
+    do {                                                                                                                            \
+        if (plan->grad_dtype == CDSGD_GRAD_BF16 && plan->copies) CDSGD_LAUNCH_ADAMW(KERNEL, kGradBF16, true, LOAD, STORE, LDS);     \
+        else if (plan->grad_dtype == CDSGD_GRAD_BF16) CDSGD_LAUNCH_ADAMW(KERNEL, kGradBF16, false, LOAD, STORE, LDS);               \
+        else if (plan->grad_dtype == CDSGD_GRAD_F16 && plan->copies) CDSGD_LAUNCH_ADAMW(KERNEL, kGradF16, true, LOAD, STORE, LDS);  \
+        else if (plan->grad_dtype == CDSGD_GRAD_F16) CDSGD_LAUNCH_ADAMW(KERNEL, kGradF16, false, LOAD, STORE, LDS);                 \
+        else CDSGD_LAUNCH_ADAMW(KERNEL, kGradF32, false, LOAD, STORE, LDS);                                                         \
     } while (0)
-    if (plan->state_bits == kState32) CDSGD_LAUNCH_ADAMW_T(k_adamw32);
-    else CDSGD_LAUNCH_ADAMW_T(k_adamw8);
+    if (plan->state_bits == kState32) {
+        if (n <= kShortList) CDSGD_LAUNCH_ADAMW_T(k_adamw32, 0, kThrough, 0);
+        else if (n <= kLongList) CDSGD_LAUNCH_ADAMW_T(k_adamw32, 0, kThroughStream, n <= kMidList ? 10240 : 12288);
+        else CDSGD_LAUNCH_ADAMW_T(k_adamw32, kStream, kThroughStream, 12288);
+    } else {
+        if (n <= kShortList) CDSGD_LAUNCH_ADAMW_T(k_adamw8, 0, kThrough, 0);
+        else CDSGD_LAUNCH_ADAMW_T(k_adamw8, 0, kThroughStream, n <= kLongList ? 7168 : 8192);
+    }
 #undef CDSGD_LAUNCH_ADAMW_T
 #undef CDSGD_LAUNCH_ADAMW
     return launch_status();
