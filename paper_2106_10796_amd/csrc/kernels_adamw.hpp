@@ -394,7 +394,7 @@ __global__ __launch_bounds__(64) void k_adamw8(const StepChunk *__restrict__ chu
 }
 
 // What 8-bit states stand for: OT is kGradF32 or kGradBF16.
-template <int OT, bool RAGGED>
+template <int OT, bool RAGGED, int LOAD, int STORE>
 __device__ __forceinline__ void read_states_piece(const StepChunk &c, unsigned piece)
 {
     constexpr int E = 4, B = kStep8Blocks;
@@ -406,8 +406,8 @@ __device__ __forceinline__ void read_states_piece(const StepChunk &c, unsigned p
         const unsigned first = piece + k * CDSGD_STATE_BLOCK + threadIdx.x * 4u;
         b[0][k] = (unsigned char)__builtin_amdgcn_raw_buffer_load_b8(sms.rsrc, (int)(block + k), 0, 0);
         b[1][k] = (unsigned char)__builtin_amdgcn_raw_buffer_load_b8(svs.rsrc, (int)(block + k), 0, 0);
-        w[0][k] = Span<E, kStream, kStream>(c.m, c.elems, 1, first).template load8<RAGGED>();
-        w[1][k] = Span<E, kStream, kStream>(c.v, c.elems, 1, first).template load8<RAGGED>();
+        w[0][k] = Span<E, LOAD, STORE>(c.m, c.elems, 1, first).template load8<RAGGED>();
+        w[1][k] = Span<E, LOAD, STORE>(c.v, c.elems, 1, first).template load8<RAGGED>();
     }
 #pragma unroll
     for (int k = 0; k < B; ++k) {
@@ -419,23 +419,23 @@ __device__ __forceinline__ void read_states_piece(const StepChunk &c, unsigned p
             else decode4<false>(w[1][k], b[1][k], x);
             void *const out = z == 0 ? c.m_out : c.v_out;
             if constexpr (OT == kGradF32) {
-                Span<E, kStream, kStream>(out, c.elems, 4, first).store32(x);
+                Span<E, LOAD, STORE>(out, c.elems, 4, first).store32(x);
             } else {
                 const unsigned h[2] = {narrow2<OT>(x[0], x[1]), narrow2<OT>(x[2], x[3])};
-                Span<E, kStream, kStream>(out, c.elems, 2, first).template store16<RAGGED>(h);
+                Span<E, LOAD, STORE>(out, c.elems, 2, first).template store16<RAGGED>(h);
             }
         }
     }
 }
 
-template <int OT>
+template <int OT, int LOAD, int STORE>
 __global__ __launch_bounds__(64) void k_read_states(const StepChunk *__restrict__ chunks, unsigned per_chunk)
 {
     const StepChunk c = chunks[blockIdx.x / per_chunk];
     const unsigned piece = blockIdx.x % per_chunk * kStep8Elems;
     if (piece >= c.elems) return;
-    if (piece + kStep8Elems <= c.elems) read_states_piece<OT, false>(c, piece);
-    else read_states_piece<OT, true>(c, piece);
+    if (piece + kStep8Elems <= c.elems) read_states_piece<OT, false, LOAD, STORE>(c, piece);
+    else read_states_piece<OT, true, LOAD, STORE>(c, piece);
 }
 
 // ---------------------------------------------------------------------------

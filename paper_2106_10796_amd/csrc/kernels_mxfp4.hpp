@@ -4,6 +4,8 @@
 namespace {
 
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned u4_by2 __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any address of a 16-bit (32-bit) element
+typedef unsigned u4_by4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr unsigned kGroup = 128;  // elements of a row that one scale word covers
 
@@ -34,26 +36,70 @@ __device__ __forceinline__ unsigned scale_of(unsigned most)
 // What the conversion instructions take: the exponent as a float's.  Byte 0 gives the pattern 0, which they read as 2^-127.
 __device__ __forceinline__ float scale_operand(unsigned scale) { return __builtin_bit_cast(float, scale << 23); }
 
-// Eight codes of a block in a word.
-__device__ __forceinline__ unsigned encode8(const float (&x)[8], float scale)
+__device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
+
+// Elements as words: an fp32 one each, or two of 16 bits, which are compared and converted in pairs as they are: a third of the
+// instructions that widening them takes (4096 x 4095 in bf16 in both forms: 14.4 us widened, 12.9 so; large ones the same).
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
+// The larger magnitudes (of each half) of two words; `a` has no sign bits.
+template <int DT>
+__device__ __forceinline__ unsigned most_of(unsigned a, unsigned b)
 {
+    if constexpr (DT == kGradF32) return larger(a, b & 0x7FFFFFFFu);
+    else return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b & 0x7FFF7FFFu)));
+}
+
+// A magnitude (of 16 bits: in the low half) as fp32 bits.
+template <int DT>
+__device__ __forceinline__ unsigned fp32_bits(unsigned a)
+{
+    if constexpr (DT == kGradF32) return a;
+    else return __builtin_bit_cast(unsigned, widen16<DT>(a & 0xFFFFu));
+}
+
+// Two codes into byte `at` of w: of two fp32 words, or of the pair in word a.
+template <int DT, int at>
+__device__ __forceinline__ unsigned encode2(unsigned w, unsigned a, unsigned b, float scale)
+{
+    if constexpr (DT == kGradF32) {
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __builtin_bit_cast(float, a), __builtin_bit_cast(float, b), scale, at);
+    } else if constexpr (DT == kGradBF16) {
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(b2, a), scale, at);
+    } else {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(h2, a), scale, at);
+    }
+}
+
+// Eight elements in a row.
+template <int DT>
+constexpr int kWords = DT == kGradF32 ? 8 : 4;
+template <int DT>
+struct Words {
+    unsigned w[kWords<DT>];
+};
+
+template <int DT>
+__device__ __forceinline__ unsigned encode8(const unsigned (&x)[kWords<DT>], float scale)
+{
+    constexpr int k = kWords<DT> / 4;
     unsigned w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+    w = encode2<DT, 0>(w, x[0], x[k - 1], scale);
+    w = encode2<DT, 1>(w, x[k], x[2 * k - 1], scale);
+    w = encode2<DT, 2>(w, x[2 * k], x[3 * k - 1], scale);
+    w = encode2<DT, 3>(w, x[3 * k], x[4 * k - 1], scale);
     return w;
 }
 
-__device__ __forceinline__ unsigned magnitude(float x) { return __builtin_bit_cast(unsigned, x) & 0x7FFFFFFFu; }
-__device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
-
-__device__ __forceinline__ unsigned most_of(const float (&x)[8])
+template <int DT>
+__device__ __forceinline__ unsigned most_of_eight(const unsigned (&x)[kWords<DT>])
 {
     unsigned m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = larger(m, magnitude(x[i]));
-    return m;
+    for (int i = 0; i < kWords<DT>; ++i) m = most_of<DT>(m, x[i]);
+    return fp32_bits<DT>(DT == kGradF32 ? m : larger(m & 0xFFFFu, m >> 16));
 }
 
 // ... over the four lanes that hold a block.
@@ -63,33 +109,59 @@ __device__ __forceinline__ unsigned most_of_quad(unsigned m)
     return larger(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true));
 }
 
+// 16 bytes of a row, the first of which are elements `d` and on of those that were loaded: what is past them is 0.
 template <int DT>
-__device__ __forceinline__ void widen8(const Eight<DT> &e, float (&x)[8])
+__device__ __forceinline__ u4 shifted(u4 w, unsigned d)
 {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (float)e.v[i];
+    const unsigned words = DT == kGradF32 ? d : d / 2u;
+    u4 t = (words & 1u) ? u4{w.y, w.z, w.w, 0u} : w;
+    t = (words & 2u) ? u4{t.z, t.w, 0u, 0u} : t;
+    if (words > 3u) t = u4{0u, 0u, 0u, 0u};
+    if constexpr (DT != kGradF32) {
+        if (d & 1u) t = u4{t.x >> 16 | t.y << 16, t.y >> 16 | t.z << 16, t.z >> 16 | t.w << 16, t.w >> 16};
+    }
+    return t;
 }
 
-// Eight elements of row `r` from column `c` on; what lies outside the matrix is 0.  The loads of an edge are as independent of
-// one another as those of the interior: addresses are moved inside, and the values dropped.
+// Eight elements of row `r` from column `c` on; what lies outside the matrix is 0.  At an edge the load is moved inside the row and
+// its elements back to their places, so that it is one load there, too.
 template <int DT, bool EDGE>
 __device__ __forceinline__ Eight<DT> load8(const Elem<DT> *x, size_t ld, unsigned rows, unsigned cols, unsigned r, unsigned c)
 {
     if constexpr (!EDGE) {
         return reinterpret_cast<const EightAt<DT> *>(x + (size_t)r * ld + c)->e;
     } else {
-        Eight<DT> e;
+        constexpr unsigned kEach = 16 / sizeof(Elem<DT>), kLoads = 8 / kEach;
         const Elem<DT> *row = x + (size_t)(r < rows ? r : rows - 1u) * ld;
+        Eight<DT> e;
+        if (cols >= kEach) {
+            struct {
+                u4 q[kLoads];
+            } got;
 #pragma unroll
-        for (unsigned i = 0; i < 8; ++i) e.v[i] = row[c + i < cols ? c + i : cols - 1u];
+            for (unsigned k = 0; k < kLoads; ++k) {
+                struct __attribute__((packed, aligned(sizeof(Elem<DT>)))) At {
+                    u4 v;
+                };
+                const unsigned from = c + k * kEach, at = from + kEach <= cols ? from : cols - kEach;
+                got.q[k] = shifted<DT>(reinterpret_cast<const At *>(row + at)->v, from - at);
+                if (r >= rows) got.q[k] = u4{0u, 0u, 0u, 0u};
+            }
+            e = __builtin_bit_cast(Eight<DT>, got);
+        } else {
 #pragma unroll
-        for (unsigned i = 0; i < 8; ++i)
-            if (!(r < rows && c + i < cols)) e.v[i] = (Elem<DT>)0.0f;
+            for (unsigned i = 0; i < 8; ++i) e.v[i] = row[c + i < cols ? c + i : cols - 1u];
+#pragma unroll
+            for (unsigned i = 0; i < 8; ++i)
+                if (!(r < rows && c + i < cols)) e.v[i] = (Elem<DT>)0.0f;
+        }
         return e;
     }
 }
 
-// Blocks along the rows alone.  A wave takes 512 columns of ROWS rows, eight elements a lane, four lanes a block.
+// Blocks along the rows alone.  A wave takes 512 columns of ROWS rows, eight elements to a lane, four lanes to a block.  Bound by
+// HBM: 5.5 TB/s over 2048 x 25088 in bf16, 5.6 over 4096 x 25088 in fp32 (4 rows; with loads that do not keep 22 and 92 us instead of
+// 23 and 84, codes stored past the caches 21 and 81, but a product reads them next).
 constexpr unsigned kRowCols = 512;
 template <int DT, int ROWS, bool EDGE>
 __device__ __forceinline__ void quantize_rows(const Elem<DT> *x, size_t ld, unsigned rows, unsigned cols, unsigned r0, unsigned c,
@@ -101,10 +173,9 @@ __device__ __forceinline__ void quantize_rows(const Elem<DT> *x, size_t ld, unsi
     for (int i = 0; i < ROWS; ++i) e[i] = load8<DT, EDGE>(x, ld, rows, cols, r0 + i, c);
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        float v[8];
-        widen8<DT>(e[i], v);
-        const unsigned s = scale_of(most_of_quad(most_of(v)));
-        const unsigned w = encode8(v, scale_operand(s));
+        const Words<DT> v = __builtin_bit_cast(Words<DT>, e[i]);
+        const unsigned s = scale_of(most_of_quad(most_of_eight<DT>(v.w)));
+        const unsigned w = encode8<DT>(v.w, scale_operand(s));
         const unsigned r = r0 + i;
         if (EDGE && (r >= rows || c >= groups * kGroup)) continue;
         reinterpret_cast<unsigned *>(codes + (size_t)r * (groups * 64u))[c / 8u] = w;
@@ -126,33 +197,44 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const Elem<DT> *__restric
 
 // Blocks down the columns, and along the rows in the same pass if ROW.  A group takes a tile of 128 by 128: 64 bytes of every
 // row of either result, and the scale words of 128 of them in a row.  The tile goes through LDS in the matrix's own type; a band
-// of 32 rows is turned by a quarter of a row against the one above, so that the lanes that read one column in four bands
-// meet different banks.
+// of 32 rows is turned by 64 bytes against the one above, so that the lanes that read one column in four bands meet different banks.
+// Bound by HBM and by its stores of half lines: both forms of 4096 x 25088 in fp32 5.2 TB/s (99 us; 106 with neighbouring tiles on
+// different XCDs), of 2048 x 25088 in bf16 4.5 (35 us; 37.5).
 constexpr unsigned kTile = 128;
 template <int DT>
 __device__ __forceinline__ unsigned lds_at(unsigned r, unsigned c)  // in elements
 {
-    constexpr unsigned turn = kTile / 4;
+    constexpr unsigned turn = 64 / sizeof(Elem<DT>);
     return r * kTile + ((c + r / 32u * turn) & (kTile - 1u));
 }
+
+inline unsigned long long tile_groups(size_t rows, size_t cols)
+{
+    const unsigned long long supers = (unsigned long long)((rows + 2 * kTile - 1) / (2 * kTile)) * ((cols + 2 * kTile - 1) / (2 * kTile));
+    return (supers + 7u) / 8u * 32u;
+}
+
+// A lane's part of a column pass is 4 bytes of a row: one fp32 column, or two of 16 bits.
+template <int DT>
+constexpr unsigned kTileLanes = 512 / (4 / sizeof(Elem<DT>));
 
 template <int DT, bool ROW, bool EDGE>
 __device__ __forceinline__ void load_tile(const Elem<DT> *x, size_t ld, unsigned rows, unsigned cols, unsigned r0, unsigned c0,
                                           uint8_t *codes, uint8_t *scales, Elem<DT> *tile)
 {
+    constexpr unsigned kRows = kTileLanes<DT> / 16u;
     const unsigned groups = (cols + kGroup - 1) / kGroup, c = threadIdx.x % 16u * 8u;
-    Eight<DT> e[8];
+    Eight<DT> e[kTile / kRows];
 #pragma unroll
-    for (unsigned i = 0; i < 8; ++i) e[i] = load8<DT, EDGE>(x, ld, rows, cols, r0 + i * 16u + threadIdx.x / 16u, c0 + c);
+    for (unsigned i = 0; i < kTile / kRows; ++i) e[i] = load8<DT, EDGE>(x, ld, rows, cols, r0 + i * kRows + threadIdx.x / 16u, c0 + c);
 #pragma unroll
-    for (unsigned i = 0; i < 8; ++i) {
-        const unsigned r = i * 16u + threadIdx.x / 16u;
+    for (unsigned i = 0; i < kTile / kRows; ++i) {
+        const unsigned r = i * kRows + threadIdx.x / 16u;
         *reinterpret_cast<Eight<DT> *>(__builtin_assume_aligned(tile + lds_at<DT>(r, c), 16)) = e[i];
         if constexpr (ROW) {
-            float v[8];
-            widen8<DT>(e[i], v);
-            const unsigned s = scale_of(most_of_quad(most_of(v)));
-            const unsigned w = encode8(v, scale_operand(s));
+            const Words<DT> v = __builtin_bit_cast(Words<DT>, e[i]);
+            const unsigned s = scale_of(most_of_quad(most_of_eight<DT>(v.w)));
+            const unsigned w = encode8<DT>(v.w, scale_operand(s));
             if (EDGE && r0 + r >= rows) continue;
             reinterpret_cast<unsigned *>(codes + (size_t)(r0 + r) * (groups * 64u))[(c0 + c) / 8u] = w;
             if (threadIdx.x % 4u == 0u) scales[((size_t)(c0 / kGroup) * rows + r0 + r) * 4u + c / 32u] = (uint8_t)s;
@@ -161,40 +243,42 @@ __device__ __forceinline__ void load_tile(const Elem<DT> *x, size_t ld, unsigned
 }
 
 template <int DT, bool ROW>
-__global__ __launch_bounds__(256) void k_quantize_tiles(const Elem<DT> *__restrict__ x, size_t ld, unsigned rows, unsigned cols,
-                                                        uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
-                                                        uint8_t *__restrict__ codes_t, uint8_t *__restrict__ scales_t)
+__global__ __launch_bounds__(kTileLanes<DT>) void k_quantize_tiles(const Elem<DT> *__restrict__ x, size_t ld, unsigned rows,
+                                                                   unsigned cols, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
+                                                                   uint8_t *__restrict__ codes_t, uint8_t *__restrict__ scales_t)
 {
     __shared__ __align__(16) Elem<DT> tile[kTile * kTile];
-    const unsigned across = (cols + kTile - 1) / kTile;
-    const unsigned r0 = blockIdx.x / across * kTile, c0 = blockIdx.x % across * kTile;
+    // Four tiles, two by two, run on one XCD (group b on XCD b % 8) one after the other, so that the halves of a line of codes that
+    // neighbouring tiles write meet in one L2.
+    const unsigned supers_across = (cols + 2 * kTile - 1) / (2 * kTile), i = blockIdx.x / 8u, super = i / 4u * 8u + blockIdx.x % 8u;
+    const unsigned r0 = (super / supers_across * 2u + i / 2u % 2u) * kTile, c0 = (super % supers_across * 2u + i % 2u) * kTile;
+    if (r0 >= rows || c0 >= cols) return;
     if (r0 + kTile <= rows && c0 + kTile <= cols) load_tile<DT, ROW, false>(x, ld, rows, cols, r0, c0, codes, scales, tile);
     else load_tile<DT, ROW, true>(x, ld, rows, cols, r0, c0, codes, scales, tile);
     __syncthreads();
-    // two neighbouring columns of one band to a lane; four lanes in a row hold the bands of a column
-    const unsigned band = threadIdx.x % 4u, c = threadIdx.x / 4u * 2u;
-    struct __attribute__((aligned(2 * sizeof(Elem<DT>)))) Two {
-        Elem<DT> a, b;
-    } e[32];
+    // four lanes in a row hold the bands of a column (of two neighbouring ones)
+    constexpr unsigned kCols = 4 / sizeof(Elem<DT>);
+    const unsigned band = threadIdx.x % 4u, c = threadIdx.x / 4u * kCols;
+    unsigned e[32];
 #pragma unroll
-    for (unsigned i = 0; i < 32; ++i) e[i] = *reinterpret_cast<const Two *>(tile + lds_at<DT>(band * 32u + i, c));
-    unsigned most[2] = {0, 0};
-#pragma unroll
-    for (unsigned i = 0; i < 32; ++i) {
-        most[0] = larger(most[0], magnitude((float)e[i].a));
-        most[1] = larger(most[1], magnitude((float)e[i].b));
-    }
+    for (unsigned i = 0; i < 32; ++i) e[i] = *reinterpret_cast<const unsigned *>(__builtin_assume_aligned(tile + lds_at<DT>(band * 32u + i, c), 4));
     const unsigned groups_t = (rows + kGroup - 1) / kGroup;
+    unsigned most = 0;
 #pragma unroll
-    for (unsigned k = 0; k < 2; ++k) {
-        const unsigned s = scale_of(most[k]), col = c0 + c + k;
+    for (unsigned i = 0; i < 32; ++i) most = most_of<DT>(most, e[i]);
+#pragma unroll
+    for (unsigned k = 0; k < kCols; ++k) {
+        const unsigned s = scale_of(fp32_bits<DT>(k ? most >> 16 : most)), col = c0 + c + k;
         u4 w;
 #pragma unroll
         for (unsigned q = 0; q < 4; ++q) {
-            float v[8];
+            unsigned v[kWords<DT>];
 #pragma unroll
-            for (unsigned i = 0; i < 8; ++i) v[i] = (float)(k ? e[8 * q + i].b : e[8 * q + i].a);
-            w[q] = encode8(v, scale_operand(s));
+            for (unsigned z = 0; z < kWords<DT>; ++z) {
+                if constexpr (DT == kGradF32) v[z] = e[8 * q + z];
+                else v[z] = __builtin_amdgcn_perm(e[8 * q + 2 * z + 1], e[8 * q + 2 * z], k ? 0x07060302u : 0x05040100u);  // this column's half of two rows
+            }
+            w[q] = encode8<DT>(v, scale_operand(s));
         }
         if (col < cols) {
             *reinterpret_cast<u4 *>(codes_t + (size_t)col * (groups_t * 64u) + r0 / 2u + band * 16u) = w;
@@ -206,19 +290,25 @@ __global__ __launch_bounds__(256) void k_quantize_tiles(const Elem<DT> *__restri
 // ---------------------------------------------------------------------------
 // values
 // ---------------------------------------------------------------------------
+// 16 bytes of a row to a lane, so that a wave's store is to whole lines in a row, past the caches (fp32, 4096 x 25088: 7.0 TB/s, 88 us
+// at the default policy, 66 so; eight elements to a lane 160).
+template <int DT>
+constexpr unsigned kValueCols = 64 * 16 / sizeof(Elem<DT>);
 template <int DT, int ROWS>
 __global__ __launch_bounds__(256) void k_dequantize(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                     unsigned rows, unsigned cols, Elem<DT> *__restrict__ out, size_t ld)
 {
-    const unsigned col_blocks = (cols + kRowCols - 1) / kRowCols, groups = (cols + kGroup - 1) / kGroup;
+    constexpr unsigned E = 16 / sizeof(Elem<DT>);
+    const unsigned col_blocks = (cols + kValueCols<DT> - 1) / kValueCols<DT>, groups = (cols + kGroup - 1) / kGroup;
     const unsigned r0 = (blockIdx.x / col_blocks * 4u + threadIdx.x / 64u) * ROWS;
-    const unsigned c = blockIdx.x % col_blocks * kRowCols + threadIdx.x % 64u * 8u;
+    const unsigned c = blockIdx.x % col_blocks * kValueCols<DT> + threadIdx.x % 64u * E;
     if (r0 >= rows || c >= cols) return;
     unsigned w[ROWS], s[ROWS];
 #pragma unroll
     for (unsigned i = 0; i < ROWS; ++i) {
         const unsigned r = r0 + i < rows ? r0 + i : rows - 1u;
-        w[i] = reinterpret_cast<const unsigned *>(codes + (size_t)r * (groups * 64u))[c / 8u];
+        const uint8_t *row = codes + (size_t)r * (groups * 64u);
+        w[i] = E == 8 ? reinterpret_cast<const unsigned *>(row)[c / 8u] : reinterpret_cast<const uint16_t *>(row)[c / 4u];
         s[i] = scales[((size_t)(c / kGroup) * rows + r) * 4u + c / 32u % 4u];
     }
 #pragma unroll
@@ -226,18 +316,27 @@ __global__ __launch_bounds__(256) void k_dequantize(const uint8_t *__restrict__ 
         if (r0 + i >= rows) break;
         typedef float f2 __attribute__((ext_vector_type(2)));
         const float scale = scale_operand(s[i]);
-        const f2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 1),
-                         __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 3)};
-        EightAt<DT> e;
+        f2 v[4];
+        v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 0);
+        v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 1);
+        if constexpr (E == 8) {
+            v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 2);
+            v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 3);
+        }
+        struct {
+            Elem<DT> v[E];
+        } e;
 #pragma unroll
-        for (unsigned k = 0; k < 8; ++k) e.e.v[k] = s[i] == 255u ? (Elem<DT>)__builtin_nanf("") : (Elem<DT>)v[k / 2][k % 2];
+        for (unsigned k = 0; k < E; ++k) e.v[k] = s[i] == 255u ? (Elem<DT>)__builtin_nanf("") : (Elem<DT>)v[k / 2][k % 2];
         Elem<DT> *to = out + (size_t)(r0 + i) * ld + c;
-        if (c + 8u <= cols) {
-            *reinterpret_cast<EightAt<DT> *>(to) = e;
+        if (c + E <= cols) {
+            typedef typename std::conditional<sizeof(Elem<DT>) == 4, u4_by4, u4_by2>::type u4_at;
+            const u4 bits = __builtin_bit_cast(u4, e);
+            __builtin_nontemporal_store(bits, reinterpret_cast<u4_at *>(to));
         } else {
 #pragma unroll
-            for (unsigned k = 0; k < 8; ++k)
-                if (c + k < cols) to[k] = e.e.v[k];
+            for (unsigned k = 0; k < E; ++k)
+                if (c + k < cols) to[k] = e.v[k];
         }
     }
 }

@@ -13,8 +13,6 @@ namespace {
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef int i4s __attribute__((ext_vector_type(4)));
-typedef unsigned u4_by2 __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any address of a 16-bit (32-bit) element
-typedef unsigned u4_by4 __attribute__((ext_vector_type(4), aligned(4)));
 
 // v_mfma_scale_f32_32x32x64: lane l holds elements 32 (l / 32) ... + 31 of row l % 32 of either operand and their scale, and of
 // the result rows i % 4 + 8 (i / 4) + 4 (l / 32), i = 0 ... 15, of column l % 32.

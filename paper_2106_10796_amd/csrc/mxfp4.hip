@@ -48,6 +48,8 @@ inline int check_matrix(size_t rows, size_t cols)
     return CDSGD_OK;
 }
 
+inline unsigned long long count_of(size_t n, size_t each) { return (n + each - 1) / each; }
+
 constexpr unsigned long long kMostGroups = 0xFFFFFFFFull / 256;  // workgroups of 256 lanes in a launch
 
 // How a product is computed.  Few rows of A, and a matrix B that is read once: rings of a wave's own (ring: fragments of 16 rows of
@@ -57,8 +59,6 @@ struct Product {
     int tile;
     unsigned splits;
 };
-
-inline unsigned long long count_of(size_t n, size_t each) { return (n + each - 1) / each; }
 
 // us, bf16 results, three sets of operands in turn; rWxF: rings of W waves, F fragments; tB: tiles of B by B; /S: split S ways
 //   16 x 8192 x 8192    r8x1 9.0, r4x1 10.6, t64 11.2            5 x 8192 x 300     r8x1 2.7, r4x1 2.5;  1 x 25088 x 512 6.1, 4.0
@@ -127,15 +127,18 @@ int cdsgd_mxfp4_quantize(const void *x, int dtype, size_t rows, size_t cols, siz
             if (overlap2(buffer[a], bytes[a], buffer[b], bytes[b])) return CDSGD_ERR_ALIAS;
     hipStream_t s = (hipStream_t)hip_stream;
     const unsigned r = (unsigned)rows, c = (unsigned)cols;
-    constexpr unsigned kRows = 4;
-    const unsigned long long groups = codes_t ? (unsigned long long)((rows + kTile - 1) / kTile) * ((cols + kTile - 1) / kTile)
-                                              : (unsigned long long)((rows + 4 * kRows - 1) / (4 * kRows)) * ((cols + kRowCols - 1) / kRowCols);
-    if (groups > kMostGroups) return CDSGD_ERR_SIZE;
+    // rows to a wave: 4 on large matrices, 1 where that leaves compute units idle (us, 1003 x 2049 in fp16: 2.8 with 4, 2.4 with 1;
+    // 8192 x 4096 in bf16 12.8 and 14.1)
+    const unsigned long long across = count_of(cols, kRowCols);
+    const bool many = across * count_of(rows, 16) >= 256;
+    const unsigned long long groups = codes_t ? tile_groups(rows, cols) : across * count_of(rows, many ? 16 : 4);
+    if (groups > kMostGroups / 2) return CDSGD_ERR_SIZE;
     with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         const Elem<DT> *from = static_cast<const Elem<DT> *>(x);
-        const dim3 grid((unsigned)groups), block(256);
-        if (!codes_t) hipLaunchKernelGGL((k_quantize_rows<DT, kRows>), grid, block, 0, s, from, ld, r, c, codes, scales);
+        const dim3 grid((unsigned)groups), block(codes_t ? kTileLanes<DT> : 256u);
+        if (!codes_t && many) hipLaunchKernelGGL((k_quantize_rows<DT, 4>), grid, block, 0, s, from, ld, r, c, codes, scales);
+        else if (!codes_t) hipLaunchKernelGGL((k_quantize_rows<DT, 1>), grid, block, 0, s, from, ld, r, c, codes, scales);
         else if (codes) hipLaunchKernelGGL((k_quantize_tiles<DT, true>), grid, block, 0, s, from, ld, r, c, codes, scales, codes_t, scales_t);
         else hipLaunchKernelGGL((k_quantize_tiles<DT, false>), grid, block, 0, s, from, ld, r, c, codes, scales, codes_t, scales_t);
     });
@@ -154,13 +157,18 @@ int cdsgd_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, size_t r
     const size_t ob = extent_bytes(rows, cols, ld, bytes_of(dtype));
     if (overlap2(out, ob, codes, cdsgd_mxfp4_code_bytes(rows, cols)) || overlap2(out, ob, scales, cdsgd_mxfp4_scale_bytes(rows, cols)))
         return CDSGD_ERR_ALIAS;
-    constexpr unsigned kRows = 4;
-    const unsigned long long groups = (unsigned long long)((rows + 4 * kRows - 1) / (4 * kRows)) * ((cols + kRowCols - 1) / kRowCols);
+    const unsigned long long across = count_of(cols, dtype == CDSGD_GRAD_F32 ? kValueCols<kGradF32> : kValueCols<kGradBF16>);
+    const bool many = across * count_of(rows, 16) >= 256;
+    const unsigned long long groups = across * count_of(rows, many ? 16 : 4);
     if (groups > kMostGroups) return CDSGD_ERR_SIZE;
     with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        hipLaunchKernelGGL((k_dequantize<DT, kRows>), dim3((unsigned)groups), dim3(256), 0, (hipStream_t)hip_stream, codes, scales,
-                           (unsigned)rows, (unsigned)cols, static_cast<Elem<DT> *>(out), ld);
+        const auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)hip_stream, codes, scales, (unsigned)rows,
+                               (unsigned)cols, static_cast<Elem<DT> *>(out), ld);
+        };
+        if (many) launch(k_dequantize<DT, 4>);
+        else launch(k_dequantize<DT, 1>);
     });
     return launch_status();
 }

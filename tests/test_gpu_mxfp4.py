@@ -13,7 +13,8 @@ TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 EPS = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
 GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
 SHAPES = [(1, 1), (1, 32), (1, 33), (2, 127), (31, 128), (32, 129), (33, 31), (127, 257), (128, 128), (129, 640), (130, 1023), (257, 70),
-          (300, 512), (5, 4099), (1030, 513)]
+          (300, 512), (5, 4099), (1030, 513),
+          (3, 2), (140, 5), (200, 7), (9, 8), (4, 11), (2100, 1030)]
 
 
 # ---- plain implementations ------------------------------------------------------------------------------------------------
@@ -139,6 +140,24 @@ def test_quantize_extremes(exponent):
     for q, w in ((row, x), (col, x.T)):
         codes, scales = quantize(w.astype(np.float64))
         assert np.array_equal(of(q)[1], scales) and np.array_equal(of(q)[0], codes)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_quantize_every_value_of_16_bits(dtype):
+    """Every finite pattern, the denormal ones among them, in blocks of its own size and next to much larger ones."""
+    bits = np.arange(1 << 16, dtype=np.uint16)
+    t = torch.from_numpy(bits.view(np.int16)).view(TYPES[dtype])
+    t = t[torch.isfinite(t.float())]
+    own = t[:t.numel() // 64 * 64].view(-1, 64).contiguous().cuda()
+    mixed = t[torch.randperm(t.numel(), generator=torch.Generator().manual_seed(1))][:t.numel() // 64 * 64].view(-1, 64).contiguous().cuda()
+    for x in (own, mixed):
+        rows, cols = x.shape
+        row, col = B.new_mxfp4(rows, cols), B.new_mxfp4(cols, rows)
+        B.cdsgd_mxfp4_quantize(x, row, col)
+        want = x.double().cpu().numpy()
+        for q, w in ((row, want), (col, want.T)):
+            codes, scales = quantize(w)
+            assert np.array_equal(of(q)[1], scales) and np.array_equal(of(q)[0], codes)
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
