@@ -78,6 +78,34 @@ __device__ __forceinline__ void put4(Elem<DT> *out, size_t ld, unsigned N, unsig
     }
 }
 
+// What four neighbours of out hold; 0 where they are not within [M, N].
+template <int DT>
+__device__ __forceinline__ f4 get4(const Elem<DT> *out, size_t ld, unsigned M, unsigned N, unsigned m, unsigned n)
+{
+    typedef Elem<DT> e4 __attribute__((ext_vector_type(4)));
+    struct __attribute__((packed, aligned(sizeof(Elem<DT>)))) At {
+        e4 v;
+    };
+    const Elem<DT> *p = out + (size_t)m * ld + n;
+    f4 v = {};
+    if (m < M && n + 4u <= N) {
+        const e4 old = reinterpret_cast<const At *>(p)->v;
+        v = f4{(float)old.x, (float)old.y, (float)old.z, (float)old.w};
+    } else if (m < M) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < N) v[e] = (float)p[e];
+    }
+    return v;
+}
+
+// What the lanes of a wave wrote to LDS is there for its other lanes.  (LDS serves a wave in order: this is for the compiler.)
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // ---------------------------------------------------------------------------
 // few rows
 // ---------------------------------------------------------------------------
@@ -428,50 +456,54 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tiles(const uint8_t *__restric
     wait_for_loads<0>();
     __syncthreads();
 
-    if (add) {
+    // In the result's type through LDS, 32 rows of a wave at a time, so that rows are stored in pieces of 16 bytes to a lane: past
+    // the caches, which hold the operands (4096 x 25088 x 2048 in fp32: 204 us at the default policy, 185 so).  What is added to is
+    // read as the products lie, so that the sum is rounded once, from fp32; the loads of 32 rows are all under way before the first
+    // is used (8192 x 4096 x 4096 added to bf16: 90 us; one load and one store after the other, 106).
+    typedef Elem<DT> e4 __attribute__((ext_vector_type(4)));
+    constexpr unsigned E = 16 / sizeof(Elem<DT>), kPerRow = TN / E, kAtOnce = 64 / kPerRow;
+    CDSGD_LDS unsigned char *mine = lds + wave * (32u * kPitch);
 #pragma unroll
-        for (unsigned i = 0; i < FN; ++i)
+    for (unsigned j = 0; j < FM; ++j) {
+        if (add) {
+            f4 old[FN][4];
 #pragma unroll
-            for (unsigned j = 0; j < FM; ++j)
+            for (unsigned i = 0; i < FN; ++i)
 #pragma unroll
-                for (unsigned q = 0; q < 4; ++q) {
-                    const unsigned m = m0 + wm + j * 32u + l32, n = n0 + wn + i * 32u + q * 8u + hi * 4u;
-                    if (m < M && n < N)
-                        put4<DT>(out, ld, N, m, n, f4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}, true);
-                }
-    } else {
-        // In the result's type through LDS, 32 rows of a wave at a time, so that rows are stored in pieces of 16 bytes to a lane: past
-        // the caches, which hold the operands (4096 x 25088 x 2048 in fp32: 204 us at the default policy, 185 so).
-        typedef Elem<DT> e4 __attribute__((ext_vector_type(4)));
-        constexpr unsigned E = 16 / sizeof(Elem<DT>), kPerRow = TN / E, kAtOnce = 64 / kPerRow;
-        CDSGD_LDS unsigned char *mine = lds + wave * (32u * kPitch);
-#pragma unroll
-        for (unsigned j = 0; j < FM; ++j) {
+                for (unsigned q = 0; q < 4; ++q) old[i][q] = get4<DT>(out, ld, M, N, m0 + wm + j * 32u + l32, n0 + wn + i * 32u + q * 8u + hi * 4u);
 #pragma unroll
             for (unsigned i = 0; i < FN; ++i)
 #pragma unroll
                 for (unsigned q = 0; q < 4; ++q)
-                    *(CDSGD_LDS e4 *)(mine + l32 * kPitch + (i * 32u + q * 8u + hi * 4u) * sizeof(Elem<DT>)) =
-                        e4{(Elem<DT>)acc[i][j][4 * q], (Elem<DT>)acc[i][j][4 * q + 1], (Elem<DT>)acc[i][j][4 * q + 2], (Elem<DT>)acc[i][j][4 * q + 3]};
 #pragma unroll
-            for (unsigned r = 0; r < 32; r += kAtOnce) {
-                const unsigned row = r + lane / kPerRow, col = lane % kPerRow * E;
-                const u4 v = *(const CDSGD_LDS u4 *)(mine + row * kPitch + col * sizeof(Elem<DT>));
-                const unsigned m = m0 + wm + j * 32u + row, n = n0 + wn + col;
-                Elem<DT> *p = out + (size_t)m * ld + n;
-                if (m < M && n + E <= N) {
-                    __builtin_nontemporal_store(v, reinterpret_cast<typename std::conditional<sizeof(Elem<DT>) == 4, u4_by4, u4_by2>::type *>(p));
-                } else if (m < M) {
-                    struct Vec {
-                        Elem<DT> v[E];
-                    };
-                    const Vec e = __builtin_bit_cast(Vec, v);
+                    for (unsigned e = 0; e < 4; ++e) acc[i][j][4 * q + e] += old[i][q][e];
+        }
 #pragma unroll
-                    for (unsigned k = 0; k < E; ++k)
-                        if (n + k < N) p[k] = e.v[k];
-                }
+        for (unsigned i = 0; i < FN; ++i)
+#pragma unroll
+            for (unsigned q = 0; q < 4; ++q)
+                *(CDSGD_LDS e4 *)(mine + l32 * kPitch + (i * 32u + q * 8u + hi * 4u) * sizeof(Elem<DT>)) =
+                    e4{(Elem<DT>)acc[i][j][4 * q], (Elem<DT>)acc[i][j][4 * q + 1], (Elem<DT>)acc[i][j][4 * q + 2], (Elem<DT>)acc[i][j][4 * q + 3]};
+        wave_sync();
+#pragma unroll
+        for (unsigned r = 0; r < 32; r += kAtOnce) {
+            const unsigned row = r + lane / kPerRow, col = lane % kPerRow * E;
+            const u4 v = *(const CDSGD_LDS u4 *)(mine + row * kPitch + col * sizeof(Elem<DT>));
+            const unsigned m = m0 + wm + j * 32u + row, n = n0 + wn + col;
+            Elem<DT> *p = out + (size_t)m * ld + n;
+            if (m < M && n + E <= N) {
+                __builtin_nontemporal_store(v, reinterpret_cast<typename std::conditional<sizeof(Elem<DT>) == 4, u4_by4, u4_by2>::type *>(p));
+            } else if (m < M) {
+                struct Vec {
+                    Elem<DT> v[E];
+                };
+                const Vec e = __builtin_bit_cast(Vec, v);
+#pragma unroll
+                for (unsigned k = 0; k < E; ++k)
+                    if (n + k < N) p[k] = e.v[k];
             }
         }
+        wave_sync();
     }
 }
 
