@@ -117,8 +117,7 @@ constexpr unsigned kRingSlot = (FN + FM) * 2048u + ((FN + 1) / 2 + (FM + 1) / 2)
 template <int DT, int FM, int FN, int D, int W>
 __global__ __launch_bounds__(64 * W) void k_ring(const uint8_t *__restrict__ a, const uint8_t *__restrict__ as,
                                                  const uint8_t *__restrict__ b, const uint8_t *__restrict__ bs, unsigned M, unsigned N,
-                                                 unsigned groups, Elem<DT> *__restrict__ out, size_t ld, int add,
-                                                 unsigned /* the sum is not split */)
+                                                 unsigned groups, Elem<DT> *__restrict__ out, size_t ld, int add)
 {
     constexpr unsigned kSlot = kRingSlot<FM, FN>, kSA = (FM + 1) / 2, kSB = (FN + 1) / 2, kLoads = 2 * FN + 2 * FM + kSB + kSA;
     constexpr unsigned kAtA = FN * 2048u, kAtSB = (FN + FM) * 2048u, kAtSA = kAtSB + kSB * 256u;
@@ -233,8 +232,9 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ partial,
 // ---------------------------------------------------------------------------
 // tiles
 // ---------------------------------------------------------------------------
-// `splits` groups may share a sum: out is then [splits][M][N], in fp32, for k_join.  A group of WM by WN waves takes BM rows of A and BN of B, a stage of one line of every row (four steps of 64 elements) at a time,
-// D stages in LDS.
+// A launch computes a part of the result: `tiles_m` by `tiles_n` tiles from row m_from and column n_from on.  `splits` groups may
+// share a sum: out is then [splits][M][N], in fp32, for k_join.  A group of WM by WN waves takes BM rows of A and BN of B, a stage of
+// one line of every row (four steps of 64 elements) at a time, D stages in LDS.
 //
 // The operands of a step are read from LDS while the products of the one before it run, and what is loaded for a later stage
 // is asked for a few instructions at a time between the products: asked for at once, behind the barrier, the loads hold up every
@@ -244,9 +244,9 @@ constexpr unsigned kTileStage = (BM + BN) * 136u;
 
 template <int DT, int BM, int BN, int WM, int WN, int D>
 __global__ __launch_bounds__(64 * WM * WN) void k_tiles(const uint8_t *__restrict__ a, const uint8_t *__restrict__ as,
-                                                             const uint8_t *__restrict__ b, const uint8_t *__restrict__ bs, unsigned M,
-                                                             unsigned N, unsigned all_groups, Elem<DT> *__restrict__ out, size_t ld, int add,
-                                                        unsigned splits)
+                                                        const uint8_t *__restrict__ b, const uint8_t *__restrict__ bs, unsigned M,
+                                                        unsigned N, unsigned all_groups, Elem<DT> *__restrict__ out, size_t ld, int add,
+                                                        unsigned splits, unsigned m_from, unsigned n_from, unsigned tiles_m, unsigned tiles_n)
 {
     constexpr unsigned W = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
     constexpr unsigned kA = BM * 128, kSA = (BM + BN) * 128, kSB = kSA + BM * 8, kStage = kTileStage<BM, BN>;
@@ -257,12 +257,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tiles(const uint8_t *__restric
 
     // The tiles that run on one XCD at a time lie next to one another: group b runs on XCD b % 8, which takes a run of
     // tiles, in bands of 8 rows of tiles.
-    const unsigned tiles_m = (M + BM - 1u) / BM, tiles_n = (N + BN - 1u) / BN, total = tiles_m * tiles_n;
+    const unsigned total = tiles_m * tiles_n;
     const unsigned split = blockIdx.x / total, nth = blockIdx.x % total;
     const unsigned xcd = nth % 8u, id = xcd * (total / 8u) + (xcd < total % 8u ? xcd : total % 8u) + nth / 8u;
     constexpr unsigned kBand = 8;
     const unsigned band = id / (kBand * tiles_n), in = id % (kBand * tiles_n), left = tiles_m - band * kBand, high = left < kBand ? left : kBand;
-    const unsigned m0 = (band * kBand + in % high) * BM, n0 = in / high * BN;
+    const unsigned m0 = m_from + (band * kBand + in % high) * BM, n0 = n_from + in / high * BN;
 
     // this group's part of the sum: lines `line` ... of every row
     const unsigned stride = all_groups * 64u, lines = (all_groups + 1u) / 2u, each = (lines + splits - 1u) / splits, line = split * each;

@@ -53,12 +53,39 @@ inline unsigned long long count_of(size_t n, size_t each) { return (n + each - 1
 constexpr unsigned long long kMostGroups = 0xFFFFFFFFull / 256;  // workgroups of 256 lanes in a launch
 
 // How a product is computed.  Few rows of A, and a matrix B that is read once: rings of a wave's own (ring: fragments of 16 rows of
-// A to a group, and its waves).  Otherwise tiles, whose sum is split over groups where it is long and the tiles are few.
+// A to a group, and its waves).  Otherwise tiles, whose sum is split over groups where it is long and the tiles are few, and whose last
+// rows or columns may be left to a second launch with smaller ones.
 struct Product {
     int ring_rows, ring_waves;  // 0: tiles
     int tile;
     unsigned splits;
+    int rest_tile = 0;  // 0: all in one launch; else the rows from rest_m on or the columns from rest_n on are the second one's
+    size_t rest_m = 0, rest_n = 0;
 };
+
+// Tiles run in rounds, `round` of them at a time.  Where the last round would be nearly empty, its part of the result is taken off
+// along one of the two extents: no more tiles of half or a quarter of the size than run at a time (us, bf16 results, in one launch and
+// in two: 4352 x 4096 x 4096 56.4 and 44.1, 5120 x 4096 x 4096 56.7 and 52.7, 8190 x 4098 x 4096 103 and 90, 2304 x 4096 x 4096 31.7 and
+// 29.4; not below eight stages: 4352 x 4096 x 1024 19.6 and 21.2).
+inline Product without_a_last_round(Product p, size_t M, size_t N, unsigned long long round)
+{
+    const size_t tile = p.tile;
+    const unsigned long long tiles_m = count_of(M, tile), tiles_n = count_of(N, tile), full = tiles_m * tiles_n / round * round;
+    if (full == 0 || full == tiles_m * tiles_n) return p;
+    for (const size_t small : {(size_t)64, (size_t)128}) {
+        if (small >= tile) break;
+        const size_t rest_n = full / tiles_m * tile, rest_m = full / tiles_n * tile;
+        if (rest_n && rest_n < N && count_of(M, small) * count_of(N - rest_n, small) <= 512) {
+            p.rest_tile = (int)small, p.rest_n = rest_n;
+            return p;
+        }
+        if (rest_m && rest_m < M && count_of(M - rest_m, small) * count_of(N, small) <= 512) {
+            p.rest_tile = (int)small, p.rest_m = rest_m;
+            return p;
+        }
+    }
+    return p;
+}
 
 // us, bf16 results, three sets of operands in turn; rWxF: rings of W waves, F fragments; tB: tiles of B by B; /S: split S ways
 //   16 x 8192 x 8192    r8x1 9.0, r4x1 10.6, t64 11.2            5 x 8192 x 300     r8x1 2.7, r4x1 2.5;  1 x 25088 x 512 6.1, 4.0
@@ -81,24 +108,29 @@ inline Product product_of(size_t M, size_t N, size_t K)
                              t256 = count_of(M, 256) * count_of(N, 256), stages = count_of(K, 256);
     if (stages >= 64 && t128 >= 32 && t128 <= 128) return {0, 0, 128, 4};
     if (t64 <= 512) return {0, 0, 64, 1};
-    if (t256 < 192 || stages < 8) return {0, 0, 128, 1};
-    return {0, 0, 256, 1};
+    if (stages < 8) return {0, 0, 128, 1};
+    return t256 < 192 ? without_a_last_round({0, 0, 128, 1}, M, N, 512) : without_a_last_round({0, 0, 256, 1}, M, N, 256);
 }
 
-// Calls f(kernel, groups, lanes) with the kernel that `how` names, for results of type DT.
+// Calls f(kernel, groups, lanes) with the ring that `how` names, for results of type DT.
 template <int DT, typename F>
-void with_product_kernel(const Product &how, size_t M, size_t N, F f)
+void with_ring(const Product &how, size_t M, size_t N, F f)
 {
     const auto ring = [&](auto kernel) { f(kernel, count_of(M, 16u * how.ring_rows) * count_of(N, 16), 64u * how.ring_waves); };
-    const unsigned long long tiles = how.tile ? count_of(M, how.tile) * count_of(N, how.tile) * how.splits : 0;
     if (how.ring_rows == 1 && how.ring_waves == 8) ring(k_ring<DT, 1, 1, 2, 8>);
     else if (how.ring_rows == 1) ring(k_ring<DT, 1, 1, 2, 4>);
     else if (how.ring_rows == 2 && how.ring_waves == 8) ring(k_ring<DT, 2, 1, 2, 8>);
     else if (how.ring_rows == 2) ring(k_ring<DT, 2, 1, 2, 4>);
-    else if (how.ring_rows == 4) ring(k_ring<DT, 4, 1, 2, 4>);
-    else if (how.tile == 64) f(k_tiles<DT, 64, 64, 2, 2, 4>, tiles, 256u);
-    else if (how.tile == 128) f(k_tiles<DT, 128, 128, 2, 2, 2>, tiles, 256u);
-    else f(k_tiles<DT, 256, 256, 2, 4, 2>, tiles, 512u);
+    else ring(k_ring<DT, 4, 1, 2, 4>);
+}
+
+// The same with the kernel for tiles of `tile` by `tile`.
+template <int DT, typename F>
+void with_tiles(int tile, F f)
+{
+    if (tile == 64) f(k_tiles<DT, 64, 64, 2, 2, 4>, 256u);
+    else if (tile == 128) f(k_tiles<DT, 128, 128, 2, 2, 2>, 256u);
+    else f(k_tiles<DT, 256, 256, 2, 4, 2>, 512u);
 }
 
 }  // namespace
@@ -204,29 +236,40 @@ int cdsgd_mxfp4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const ui
     int status = CDSGD_OK;
     hipStream_t s = (hipStream_t)hip_stream;
     const unsigned m = (unsigned)M, n = (unsigned)N, groups = (unsigned)groups_of(K);
-    const auto launch = [&](auto kernel, unsigned long long count, unsigned lanes, auto *to, size_t row, int add) {
+    const auto fits = [&](unsigned long long count, unsigned lanes) {
         if (count > 0xFFFFFFFFull / lanes) status = CDSGD_ERR_SIZE;
-        else hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(lanes), 0, s, a_codes, a_scales, b_codes, b_scales, m, n, groups, to, row, add, how.splits);
+        return status == CDSGD_OK;
     };
-    if (how.splits > 1) {
-        float *parts = static_cast<float *>(workspace);
-        const unsigned long long quads = count_of(N, 4) * M;
-        if (quads > kMostGroups * 256) return CDSGD_ERR_SIZE;
-        with_product_kernel<kGradF32>(how, M, N, [&](auto kernel, unsigned long long count, unsigned lanes) { launch(kernel, count, lanes, parts, N, 0); });
-        with_dtype(dtype, [&](auto dt) {
-            constexpr int DT = decltype(dt)::value;
-            if (status == CDSGD_OK)
-                hipLaunchKernelGGL((k_join<DT>), dim3((unsigned)count_of(quads, 256)), dim3(256), 0, s, parts, m, n, how.splits,
-                                   static_cast<Elem<DT> *>(out), ld, accumulate);
+    // rows [m0, m1) and columns [n0, n1) of the result, in tiles
+    const auto tiles = [&](auto dt, int tile, size_t m0, size_t n0, size_t m1, size_t n1, auto *to, size_t row, int add) {
+        with_tiles<decltype(dt)::value>(tile, [&](auto kernel, unsigned lanes) {
+            const unsigned long long tiles_m = count_of(m1 - m0, tile), tiles_n = count_of(n1 - n0, tile), count = tiles_m * tiles_n * how.splits;
+            if (fits(count, lanes))
+                hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(lanes), 0, s, a_codes, a_scales, b_codes, b_scales, m, n, groups, to,
+                                   row, add, how.splits, (unsigned)m0, (unsigned)n0, (unsigned)tiles_m, (unsigned)tiles_n);
         });
-    } else {
-        with_dtype(dtype, [&](auto dt) {
-            constexpr int DT = decltype(dt)::value;
-            with_product_kernel<DT>(how, M, N, [&](auto kernel, unsigned long long count, unsigned lanes) {
-                launch(kernel, count, lanes, static_cast<Elem<DT> *>(out), ld, accumulate);
+    };
+    with_dtype(dtype, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        Elem<DT> *const to = static_cast<Elem<DT> *>(out);
+        if (how.ring_rows) {
+            with_ring<DT>(how, M, N, [&](auto kernel, unsigned long long count, unsigned lanes) {
+                if (fits(count, lanes))
+                    hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(lanes), 0, s, a_codes, a_scales, b_codes, b_scales, m, n, groups,
+                                       to, ld, accumulate);
             });
-        });
-    }
+        } else if (how.splits > 1) {
+            float *const parts = static_cast<float *>(workspace);
+            const unsigned long long join = count_of(count_of(N, 4) * M, 256);
+            if (!fits(join, 256)) return;
+            tiles(std::integral_constant<int, kGradF32>(), how.tile, 0, 0, M, N, parts, N, 0);
+            if (status == CDSGD_OK)
+                hipLaunchKernelGGL((k_join<DT>), dim3((unsigned)join), dim3(256), 0, s, parts, m, n, how.splits, to, ld, accumulate);
+        } else {
+            tiles(dt, how.tile, 0, 0, how.rest_m ? how.rest_m : M, how.rest_n ? how.rest_n : N, to, ld, accumulate);
+            if (how.rest_tile && status == CDSGD_OK) tiles(dt, how.rest_tile, how.rest_m, how.rest_n, M, N, to, ld, accumulate);
+        }
+    });
     if (status != CDSGD_OK) return status;
     return launch_status();
 }

@@ -251,6 +251,13 @@ def test_product_added_to_a_strided_result(M, N, K, dtype):
     check_product(M, N, K, dtype, seed=M, accumulate=True, ld=N + 13)
 
 
+@pytest.mark.parametrize("M,N,K", [(2100, 4100, 2050), (36000, 130, 2050), (66000, 100, 2050), (5100, 4130, 1800)])
+@pytest.mark.parametrize("dtype,accumulate,more", [("f32", False, 0), ("bf16", True, 5)])
+def test_product_in_two_launches(M, N, K, dtype, accumulate, more):
+    """A few tiles more than run at a time: the last columns or the last rows are smaller tiles of a second launch."""
+    check_product(M, N, K, dtype, seed=M, accumulate=accumulate, ld=N + more)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 64, 1024), (40, 64, 1024), (300, 300, 1024), (1200, 1100, 512)])
 def test_a_nan_stays_in_its_row_and_column(M, N, K):
     ac, as_ = random_mx(M, K, 1)
