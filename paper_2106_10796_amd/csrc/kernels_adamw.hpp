@@ -167,8 +167,9 @@ __device__ __forceinline__ void adamw1(float g, float &m, float &v, float &w, co
 {
     m = m * f.beta1 + g * f.one_minus_beta1;
     v = v * f.beta2 + (g * g) * f.one_minus_beta2;
-    // (one unit in the last place each, of an update that is lr times the size of a weight)
-    const float denom = __builtin_amdgcn_sqrtf(v) * f.inv_sqrt_bias2 + f.eps;
+    // (one unit in the last place each, of an update that is lr times the size of a weight; the instruction takes a denormal for 0)
+    const bool small = v < 0x1p-96f;
+    const float denom = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? 0x1p-32f : 1.0f) * f.inv_sqrt_bias2 + f.eps;
     w = w * keep - (m * __builtin_amdgcn_rcpf(denom)) * f.lr_over_bias1;
 }
 

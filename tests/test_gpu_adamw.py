@@ -329,6 +329,20 @@ def test_8_bit_states_of_extreme_size(scale):
         assert np.array_equal(t[0][name + "_scale"].get(), s) and np.array_equal(t[0][name].get(), codes), name
 
 
+def test_second_moments_below_the_smallest_normal_number():
+    """The square root of an fp32 denormal is a normal number, and counts where eps is smaller still.  Six roundings of a unit in the
+    last place at most (square root, factor, sum, reciprocal, two products) beside that of v itself, which is taken as rounded."""
+    v = np.array([1.5e-45, 1e-42, 1e-40, 3e-39, 1e-38, 1.2e-38, 3e-38, 1e-30], np.float32)
+    n, m = v.size, np.full(v.size, 1e-24, np.float32)
+    t = [torch.from_numpy(x).cuda() for x in (np.zeros(n, np.float32), np.zeros(n, np.float32), m, v)]
+    B.AdamWPlan([dict(zip(("weight", "grad", "m", "v"), t))]).step(1000, 1e-3, 0.5, 0.5, 1e-37)
+    v2, m2 = v * np.float32(0.5), m * np.float32(0.5)
+    assert np.array_equal(t[3].cpu().numpy(), v2)
+    want = -1e-3 * m2.astype(np.float64) / (np.sqrt(v2.astype(np.float64)) + 1e-37)
+    got = t[0].cpu().numpy()
+    assert np.all(np.abs(got - want) <= 8 * 2 * U * np.abs(want))
+
+
 def test_8_bit_averages_follow_their_inputs():
     """An average whose weight is 0.999 moves by less than a hundredth of a code's step in a step; it gets there all the same."""
     n = 1 << 14
