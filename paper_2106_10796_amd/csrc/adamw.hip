@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <memory>
@@ -24,7 +25,7 @@ inline bool good_dtype(int t) { return t == CDSGD_GRAD_F32 || t == CDSGD_GRAD_BF
 inline size_t bytes_of(int dtype) { return dtype == CDSGD_GRAD_F32 ? 4u : 2u; }
 
 // A launch of one wave per piece stays below 2^32 threads, and a table below 1 GiB.
-constexpr unsigned long long kMaxStepChunks = 1ull << 22, kMaxNormChunks = 1ull << 24;
+constexpr unsigned long long kMaxStepChunks = (1ull << 22) - 1, kMaxNormChunks = 1ull << 24;
 
 inline unsigned norm_elems(int dtype) { return kNormBytes / (unsigned)bytes_of(dtype); }
 
@@ -69,6 +70,32 @@ struct Block {  // device memory of a handle
             return CDSGD_ERR_DEVICE;
         }
         return CDSGD_OK;
+    }
+};
+
+// The buffers of a list, for its check: nothing that is written shares a byte with another buffer.
+struct Buffers {
+    struct Range {
+        uintptr_t from, to;
+        bool written;
+    };
+    std::vector<Range> all;
+
+    void add(const void *p, size_t bytes, bool written)
+    {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p) all.push_back({at, at + bytes, written});
+    }
+    bool alias()
+    {
+        std::sort(all.begin(), all.end(), [](const Range &a, const Range &b) { return a.from < b.from; });
+        uintptr_t end = 0, end_written = 0;  // of what lies before
+        for (const Range &r : all) {
+            if (r.from < (r.written ? end : end_written)) return true;
+            end = std::max(end, r.to);
+            if (r.written) end_written = std::max(end_written, r.to);
+        }
+        return false;
     }
 };
 
@@ -153,6 +180,7 @@ int check_adamw_list(const cdsgd_adamw_tensor *tensors, int num_tensors, int gra
     if (num_tensors < 1) return CDSGD_ERR_SIZE;
     if (!good_dtype(grad_dtype) || (state_bits != kState32 && state_bits != kState8)) return CDSGD_ERR_PARAM;
     unsigned long long total = 0;
+    Buffers buffers;
     *copies = tensors[0].weight16 != nullptr;
     for (int i = 0; i < num_tensors; ++i) {
         const cdsgd_adamw_tensor &t = tensors[i];
@@ -168,12 +196,13 @@ int check_adamw_list(const cdsgd_adamw_tensor *tensors, int num_tensors, int gra
         if (!aligned(t.weight, 16) || !aligned(t.weight16, 16) || !aligned(t.grad, 16) || !aligned(t.m, 16) || !aligned(t.v, 16))
             return CDSGD_ERR_ALIGN;
         const size_t state = state_bits / 8 * t.n, blocks = cdsgd_state_blocks(t.n);
-        const void *const buffer[] = {t.weight, t.weight16, t.m, t.v, t.m_scale, t.v_scale, t.grad};
-        const size_t bytes[] = {t.n * 4, t.n * 2, state, state, blocks, blocks, t.n * bytes_of(grad_dtype)};
-        for (int a = 0; a < 7; ++a)
-            for (int b = a + 1; b < 7; ++b)
-                if (overlap2(buffer[a], bytes[a], buffer[b], bytes[b])) return CDSGD_ERR_ALIAS;
+        for (void *p : {t.m, t.v}) buffers.add(p, state_bits / 8 * t.n, true);
+        for (void *p : {t.m_scale, t.v_scale}) buffers.add(p, cdsgd_state_blocks(t.n), true);
+        buffers.add(t.weight, t.n * 4, true);
+        buffers.add(t.weight16, t.n * 2, true);
+        buffers.add(t.grad, t.n * bytes_of(grad_dtype), false);
     }
+    if (buffers.alias()) return CDSGD_ERR_ALIAS;
     return CDSGD_OK;
 }
 
@@ -320,24 +349,26 @@ int cdsgd_adamw_grad_norm(cdsgd_adamw_plan *plan, double grad_scale, double max_
 }
 
 int cdsgd_adamw_bind_readout(cdsgd_adamw_plan *plan, void *const *m_out, void *const *v_out, int dtype)
-{
+try {
     if (!plan || !m_out || !v_out) return CDSGD_ERR_NULL;
     if (plan->state_bits != kState8 || (dtype != CDSGD_GRAD_F32 && dtype != CDSGD_GRAD_BF16)) return CDSGD_ERR_PARAM;
     const size_t ob = bytes_of(dtype);
+    Buffers buffers;
     size_t c = 0;
     for (size_t i = 0; i < plan->sizes.size(); ++i) {
-        const size_t n = plan->sizes[i], blocks = cdsgd_state_blocks(n);
+        const size_t n = plan->sizes[i];
         if (!m_out[i] || !v_out[i]) return CDSGD_ERR_NULL;
         if (!aligned(m_out[i], 16) || !aligned(v_out[i], 16)) return CDSGD_ERR_ALIGN;
+        for (void *p : {m_out[i], v_out[i]}) buffers.add(p, n * ob, true);
         const StepChunk &t = plan->host_chunks[c];
-        const void *const held[] = {t.weight, t.weight16, t.m, t.v, t.m_scale, t.v_scale, t.grad};
-        const size_t bytes[] = {n * 4, n * 2, n, n, blocks, blocks, n * bytes_of(plan->grad_dtype)};
-        bool bad = overlap2(m_out[i], n * ob, v_out[i], n * ob);
-        for (int b = 0; b < 7; ++b)
-            bad = bad || overlap2(m_out[i], n * ob, held[b], bytes[b]) || overlap2(v_out[i], n * ob, held[b], bytes[b]);
-        if (bad) return CDSGD_ERR_ALIAS;
+        for (const void *p : {t.m, t.v}) buffers.add(p, n, false);
+        for (const void *p : {t.m_scale, t.v_scale}) buffers.add(p, cdsgd_state_blocks(n), false);
+        buffers.add(t.weight, n * 4, false);
+        buffers.add(t.weight16, n * 2, false);
+        buffers.add(t.grad, n * bytes_of(plan->grad_dtype), false);
         c += pieces(n, kStepChunk);
     }
+    if (buffers.alias()) return CDSGD_ERR_ALIAS;
     c = 0;
     for (size_t i = 0; i < plan->sizes.size(); ++i)
         for (size_t at = 0; at < plan->sizes[i]; at += kStepChunk, ++c) {
@@ -352,6 +383,8 @@ int cdsgd_adamw_bind_readout(cdsgd_adamw_plan *plan, void *const *m_out, void *c
     }
     plan->readout_dtype = dtype;
     return CDSGD_OK;
+} catch (...) {
+    return CDSGD_ERR_DEVICE;
 }
 
 int cdsgd_adamw_read_states(cdsgd_adamw_plan *plan, void *hip_stream)

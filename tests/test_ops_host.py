@@ -78,6 +78,12 @@ def test_adamw_plan_refuses(L, want, dtype, bits, over):
         assert _create(L, [_adamw(bits=bits), _adamw(bits=bits, i=1, **other)], dtype, bits) == want
 
 
+@pytest.mark.parametrize("over", [dict(weight=A), dict(m=A + 0x300000), dict(v=A + 0x300000 + 3984), dict(grad=A), dict(m=A + 0x100000)])
+def test_adamw_plan_refuses_what_two_tensors_share(L, over):
+    assert _create(L, [_adamw(), _adamw(i=1, **over)]) == B.ERR_ALIAS
+    assert _create(L, [_adamw(i=1, **over), _adamw(i=2), _adamw()]) == B.ERR_ALIAS
+
+
 def test_adamw_refuses_more(L):
     assert _create(L, []) == B.ERR_SIZE
     assert L.cdsgd_adamw_plan_create(None, 1, F32, 32, ctypes.byref(ctypes.c_void_p())) == B.ERR_NULL
