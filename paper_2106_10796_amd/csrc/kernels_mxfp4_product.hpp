@@ -41,9 +41,9 @@ __device__ __forceinline__ void load_to_lds(i4s buffer, CDSGD_LDS unsigned char 
     const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long long)to);
     static_assert(BYTES == 16 || BYTES == 4, "sizes in use");
     if constexpr (BYTES == 16)
-        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory", "m0");
     else
-        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory", "m0");
 }
 
 template <int N>
