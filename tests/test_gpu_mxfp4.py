@@ -245,6 +245,13 @@ def test_product(M, N, K, dtype):
     check_product(M, N, K, dtype, seed=M + N + K)
 
 
+@pytest.mark.parametrize("M,N,K", [(200, 500, 2048), (4001, 16, 300), (256, 1000, 512), (200, 1020, 700), (65, 4090, 12300), (500, 1020, 12545)])
+@pytest.mark.parametrize("dtype,accumulate", [("f32", False), ("bf16", True), ("f16", False)])
+def test_product_of_a_few_tiles(M, N, K, dtype, accumulate):
+    """More rows than a ring takes at a time, and long sums in two parts."""
+    check_product(M, N, K, dtype, seed=M + K, accumulate=accumulate, ld=N + 3)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 100, 513), (7, 1000, 4096), (64, 130, 300), (130, 257, 2049), (512, 600, 256), (1100, 1030, 700), (520, 1000, 16700)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_product_added_to_a_strided_result(M, N, K, dtype):
