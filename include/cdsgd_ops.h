@@ -73,8 +73,8 @@ int cdsgd_grad_norm_destroy(cdsgd_grad_norm *norm);
  *   m, v          i/o fp32[n] (state_bits 32) or uint8[n] (state_bits 8)
  *   m_scale, v_scale  i/o uint8[cdsgd_state_blocks(n)] (state_bits 8); NULL where state_bits is 32
  *   weight_decay  this tensor's (finite, >= 0)
- * weight, weight16, grad, m and v are 16-byte aligned; what a step writes overlaps no other buffer of the whole list.  The plan copies a table to the device and borrows the
- * buffers; passes of one plan must be ordered.
+ * weight, weight16, grad, m and v are 16-byte aligned; what a step writes overlaps no other buffer of the whole
+ * list.  The plan copies a table to the device and borrows the buffers; passes of one plan must be ordered.
  *   step          number of this step, from 1 on;  lr, betas, eps, grad_scale: finite, lr >= 0, 0 <= beta < 1,
  *                 eps >= 1e-37 (CDSGD_ERR_PARAM)
  *   clip          in  fp32[2] as cdsgd_grad_norm_compute writes it, or NULL

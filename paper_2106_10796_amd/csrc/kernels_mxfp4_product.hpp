@@ -1,6 +1,6 @@
 // Products of two matrices in MXFP4: out = A B^T, both in blocks along the axis that is summed over.
 //
-// Both kernels load codes and scale words from memory straight into LDS, a line of 128 bytes (256 elements) of a row at a time.
+// The kernels load codes and scale words from memory straight into LDS, a line of 128 bytes (256 elements) of a row at a time.
 // Eight lanes in a row ask for one line, which is what the path from L2 is fast at: the operand layout of the matrix
 // instructions puts neighbouring lanes in different rows, and loads in that order cost a compute unit 37 cycles each instead
 // of 16 (64 x 1000 x 4096: 8.1 us with operands straight from memory, 3.4 so).  The line's eight chunks of 16 bytes lie in LDS
@@ -110,7 +110,8 @@ __device__ __forceinline__ void wave_sync()
 // few rows
 // ---------------------------------------------------------------------------
 // A group takes 16 FM rows of A and 16 FN of B; its W waves share the sum, line by line, and each has a ring of D slots in LDS of
-// its own, so that no wave waits for another before the end.
+// its own, so that no wave waits for another before the end.  Bound by reading B: 1 x 4096 x 25088 9.9 us, 5.5 TB/s of the whole call,
+// 64 x 25088 x 4096 11.9 us, 4.9 TB/s; on small matrices by the launch (64 x 1000 x 4096: 3.4 us).
 template <int FM, int FN>
 constexpr unsigned kRingSlot = (FN + FM) * 2048u + ((FN + 1) / 2 + (FM + 1) / 2) * 256u;
 
@@ -219,13 +220,8 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ partial,
     const unsigned long long q = (unsigned long long)blockIdx.x * 256u + threadIdx.x;
     if (q >= (unsigned long long)across * M) return;
     const unsigned m = (unsigned)(q / across), n = (unsigned)(q % across) * 4u;
-    f4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (unsigned k = 0; k < splits; ++k) {
-        const float *p = partial + ((size_t)k * M + m) * N + n;
-#pragma unroll
-        for (unsigned e = 0; e < 4; ++e)
-            if (n + e < N) s[e] += p[e];
-    }
+    f4 s = get4<kGradF32>(partial, N, M, N, m, n);
+    for (unsigned k = 1; k < splits; ++k) s += get4<kGradF32>(partial + (size_t)k * M * N, N, M, N, m, n);
     put4<DT>(out, ld, N, m, n, s, add != 0);
 }
 
@@ -239,6 +235,10 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ partial,
 // The operands of a step are read from LDS while the products of the one before it run, and what is loaded for a later stage
 // is asked for a few instructions at a time between the products: asked for at once, behind the barrier, the loads hold up every
 // wave's products for as long as the line to L2 is busy (8192^3: 334 us, 303 so).
+//
+// 8192 x 4096 x 4096 in bf16 takes 72 us, 3.8 PFLOP/s; bound by the card's power, not by any path: 58 us where all codes are the same.
+// Of those 72, 17 are the first loads and the stores of two rounds of tiles, which nothing hides: taking the next tile's loads ahead of
+// the stores, in groups that go from tile to tile, gave nothing (74).  256 by 256 with 4 waves 82, 128 by 128 82.
 template <int BM, int BN>
 constexpr unsigned kTileStage = (BM + BN) * 136u;
 
