@@ -97,10 +97,10 @@ inline Product without_a_last_round(Product p, size_t M, size_t N, unsigned long
 //   512 x 4096 x 4096   t64 10.6, t128 14.1, t256 24.3           256 x 8192 x 8192  t64 17.6, t128 27.0;  300 x 8192 x 300 5.4, 4.4
 //   512 x 8192 x 8192   t64 34.4, t128 31.5, t256 44.8           1024 x 4096 x 4096 t64 18.2, t128 16.8, t256 24.9
 //   2048 x 8192 x 8192  t128 89.4, t256 74.2                     2048 x 4096 x 25088 t128 124.7, t256 139.4
-//   256 x 4096 x 25088  t64 33.3, t128 67.1, t128/2 41.8, /4 30.7   512 x 4096 x 25088 t64 55.5, t128 68.0, /2 47.4, /4 46.8
-//   65 x 2048 x 25088   r4x4 15.6, t64 29.4, /2 19.7, /4 15.1    128 x 4096 x 25088 t64 30.9, /2 21.9, /4 21.2, t128/4 27.5
-//   128 x 4096 x 12544  t64 16.7, /2 14.4, /4 16.6               65 x 8192 x 8192   t64 12.1, /2 15.4
-//   256 x 4096 x 4096   t64 7.7, t128/2 16.3: the parts' way through memory and the second launch are worth 48 to 64 stages
+//   1024 x 1024 x 25088 t64 34.2, /2 28.9, t128/4 32.3           512 x 4096 x 25088 t64 44.5, t128 68.2, /2 45.1, /4 41.9
+//   64 x 4096 x 25088   r4x4 16.5, t64 30.1, /2 19.4, /4 15.5    128 x 4096 x 25088 t64 30.9, /2 21.9, /4 21.2, t128/4 27.5
+//   65 x 4096 x 8192    t64 11.8, /2 10.6, /4 11.2               256 x 4096 x 8192  t64 12.5, /2 15.5, t128/4 16.6
+//   1024 x 4096 x 25088 t128 90.4, /2 77.0, /4 92.1              1024 x 4096 x 12544 t128 43.3, /2 46.1
 inline Product product_of(size_t M, size_t N, size_t K)
 {
     const unsigned long long n16 = count_of(N, 16);
@@ -110,8 +110,8 @@ inline Product product_of(size_t M, size_t N, size_t K)
     if (n16 * count_of(M, 64) <= 256) return {4, 4, 0, 1};
     const unsigned long long t64 = count_of(M, 64) * count_of(N, 64), t128 = count_of(M, 128) * count_of(N, 128),
                              t256 = count_of(M, 256) * count_of(N, 256), stages = count_of(K, 256);
-    if (stages >= 48 && t64 <= 128) return {0, 0, 64, 2};
-    if (stages >= 64 && t128 >= 32 && t128 <= 128) return {0, 0, 128, 4};
+    if (stages >= 32 && (t64 <= 128 || (t64 <= 256 && stages >= 64))) return {0, 0, 64, 2};
+    if (stages >= 64 && t128 <= 256) return {0, 0, 128, t128 <= 128 ? 4u : 2u};
     if (t64 <= 512) return {0, 0, 64, 1};
     if (stages < 8) return {0, 0, 128, 1};
     return t256 < 192 ? without_a_last_round({0, 0, 128, 1}, M, N, 512) : without_a_last_round({0, 0, 256, 1}, M, N, 256);

@@ -245,7 +245,8 @@ def test_product(M, N, K, dtype):
     check_product(M, N, K, dtype, seed=M + N + K)
 
 
-@pytest.mark.parametrize("M,N,K", [(200, 500, 2048), (4001, 16, 300), (256, 1000, 512), (200, 1020, 700), (65, 4090, 12300), (500, 1020, 12545)])
+@pytest.mark.parametrize("M,N,K", [(200, 500, 2048), (4001, 16, 300), (256, 1000, 512), (200, 1020, 700), (65, 4090, 8200), (500, 1020, 16400),
+                                   (1000, 1100, 16400), (1000, 2050, 16390)])
 @pytest.mark.parametrize("dtype,accumulate", [("f32", False), ("bf16", True), ("f16", False)])
 def test_product_of_a_few_tiles(M, N, K, dtype, accumulate):
     """More rows than a ring takes at a time, and long sums in two parts."""
