@@ -97,6 +97,7 @@ inline Product without_a_last_round(Product p, size_t M, size_t N, unsigned long
 //   512 x 4096 x 4096   t64 10.6, t128 14.1, t256 24.3           256 x 8192 x 8192  t64 17.6, t128 27.0;  300 x 8192 x 300 5.4, 4.4
 //   512 x 8192 x 8192   t64 34.4, t128 31.5, t256 44.8           1024 x 4096 x 4096 t64 18.2, t128 16.8, t256 24.9
 //   2048 x 8192 x 8192  t128 89.4, t256 74.2                     2048 x 4096 x 25088 t128 124.7, t256 139.4
+//   16384 x 8192 x 1024 t128 125, t256 105                       8192 x 4096 x 512  t128 24.5, t256 23.4 (fp32 30.0, 32.8)
 //   1024 x 1024 x 25088 t64 34.2, /2 28.9, t128/4 32.3           512 x 4096 x 25088 t64 44.5, t128 68.2, /2 45.1, /4 41.9
 //   64 x 4096 x 25088   r4x4 16.5, t64 30.1, /2 19.4, /4 15.5    128 x 4096 x 25088 t64 30.9, /2 21.9, /4 21.2, t128/4 27.5
 //   65 x 4096 x 8192    t64 11.8, /2 10.6, /4 11.2               256 x 4096 x 8192  t64 12.5, /2 15.5, t128/4 16.6
@@ -113,8 +114,8 @@ inline Product product_of(size_t M, size_t N, size_t K)
     if (stages >= 32 && (t64 <= 128 || (t64 <= 256 && stages >= 64))) return {0, 0, 64, 2};
     if (stages >= 64 && t128 <= 256) return {0, 0, 128, t128 <= 128 ? 4u : 2u};
     if (t64 <= 512) return {0, 0, 64, 1};
-    if (stages < 8) return {0, 0, 128, 1};
-    return t256 < 192 ? without_a_last_round({0, 0, 128, 1}, M, N, 512) : without_a_last_round({0, 0, 256, 1}, M, N, 256);
+    const Product p = {0, 0, stages < 4 || t256 < 192 ? 128 : 256, 1};
+    return stages < 8 ? p : without_a_last_round(p, M, N, p.tile == 128 ? 512 : 256);
 }
 
 // Calls f(kernel, groups, lanes) with the ring that `how` names, for results of type DT.
