@@ -259,6 +259,64 @@ def test_product_added_to_a_strided_result(M, N, K, dtype):
     check_product(M, N, K, dtype, seed=M, accumulate=True, ld=N + 13)
 
 
+@pytest.mark.parametrize("M,N,K", [(3, 70, 300), (40, 70, 300), (300, 500, 300), (520, 1030, 300), (65, 4090, 8200), (4400, 4099, 300)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_product_into_any_address(M, N, K, dtype, accumulate):
+    """A result that begins at every remainder of 16 bytes is the same, and what lies beside it stays."""
+    ac, as_ = random_mx(M, K, 1)
+    bc, bs = random_mx(N, K, 2)
+    a, b, ws = on_gpu(ac, as_, M, K), on_gpu(bc, bs, N, K), B.new_mxfp4_workspace([(M, N, K)])
+    want = torch.ones(M, N, dtype=TYPES[dtype], device="cuda")
+    B.cdsgd_mxfp4_matmul(a, b, want, ws, accumulate=accumulate)
+    for offset in range(1, 16 // want.element_size()):
+        flat = torch.ones(M * N + 32, dtype=want.dtype, device="cuda")
+        out = flat[offset:offset + M * N].view(M, N)
+        B.cdsgd_mxfp4_matmul(a, b, out, ws, accumulate=accumulate)
+        assert torch.equal(out, want)
+        assert bool((flat[:offset] == 1).all()) and bool((flat[offset + M * N:] == 1).all())
+
+
+def test_on_another_stream_and_in_a_graph():
+    """Quantisation, products of every kind and values, captured once and replayed with other inputs."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    shapes = [(5, 300, 700), (100, 4096, 8200), (600, 1100, 900), (2100, 4100, 2050)]   # a ring, a sum in parts, tiles, two launches
+    xs = [torch.randn(m, k, device="cuda", generator=gen).bfloat16() for m, n, k in shapes]
+    ws = [torch.randn(n, k, device="cuda", generator=gen) for m, n, k in shapes]
+    room = B.new_mxfp4_workspace(shapes)
+    qx, qw = [B.new_mxfp4(m, k) for m, n, k in shapes], [B.new_mxfp4(n, k) for m, n, k in shapes]
+    qt = [B.new_mxfp4(k, m) for m, n, k in shapes]
+    ys = [torch.zeros(m, n, device="cuda") for m, n, k in shapes]
+    back = [torch.zeros(k, m, device="cuda", dtype=torch.float16) for m, n, k in shapes]
+
+    def work():
+        for x, w, a, b, t, y, v in zip(xs, ws, qx, qw, qt, ys, back):
+            B.cdsgd_mxfp4_quantize(x, a, t)
+            B.cdsgd_mxfp4_quantize(w, b)
+            B.cdsgd_mxfp4_matmul(a, b, y, room)
+            B.cdsgd_mxfp4_matmul(a, b, y, room, accumulate=True)
+            B.cdsgd_mxfp4_dequantize(t, v)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        work()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        work()
+    for _ in range(4):
+        for x in xs:
+            x.copy_(torch.randn(x.shape, device="cuda", generator=gen))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*ys, *back)]
+        for t in (*ys, *back):
+            t.fill_(3)
+        work()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (*ys, *back)))
+
+
 @pytest.mark.parametrize("M,N,K", [(2100, 4100, 2050), (36000, 130, 2050), (66000, 100, 2050), (5100, 4130, 1800)])
 @pytest.mark.parametrize("dtype,accumulate,more", [("f32", False, 0), ("bf16", True, 5)])
 def test_product_in_two_launches(M, N, K, dtype, accumulate, more):
