@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ partial,
 // there is more than one round, the groups of the first begin one after the other, over about the time that a round's stores take
 // at the rate of HBM (kSpread, in sleeps of 256 cycles), which the others' products then fill.  us, without and with:
 //   8192 x 4096 x 2048 fp32 65.2, 50.2, bf16 50.6, 44.9;  x 4096 fp32 95.0, 83.2, bf16 78.6, 75.8;  16384 x 8192 x 1024 bf16 115, 105;
-//   128 by 128: 8192 x 4096 x 1024 bf16 37.6, 34.1;  spread over a half and over twice as long: 8192 x 4096 x 2048 fp32 58, 56, bf16 47, 45
+//   128 by 128 8192 x 4096 x 1024 bf16 37.6, 34.1;  spread over a half and over twice as long: 8192 x 4096 x 2048 fp32 58, 56, bf16 47, 45
 //
 // 8192 x 4096 x 4096 in bf16, call after call, takes 70 us, 3.9 PFLOP/s; bound by the card's power, not by any path: 58 us (and 57
 // without the spread) where all codes are the same.  256 by 256 with 4 waves 82, 128 by 128 82; the next tile's loads ahead of the
@@ -357,8 +357,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tiles(const uint8_t *__restric
     for (unsigned t = 0; t < D - 1; ++t)
 #pragma unroll
         for (unsigned i = 0; i < kItems; ++i) ask(t, t, i);
-    if constexpr (BM > 64) {
-        constexpr unsigned kAtOnce = BM == 256 ? 256 : 512, kSpread = BM == 128 ? 32 : 24 * sizeof(Elem<DT>);
+    if constexpr (BM == BN && BM > 64) {
+        constexpr unsigned kAtOnce = BM == 256 ? 256 : 512, kSpread = BM == 256 ? 24 * sizeof(Elem<DT>) : 32;
         if (gridDim.x > kAtOnce && blockIdx.x < kAtOnce)
             for (unsigned i = blockIdx.x / 8u * kSpread / (kAtOnce / 8u); i > 0; --i) __builtin_amdgcn_s_sleep(4);
     }

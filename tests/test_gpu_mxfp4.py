@@ -317,7 +317,8 @@ def test_on_another_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(got, (*ys, *back)))
 
 
-@pytest.mark.parametrize("M,N,K", [(2100, 4100, 2050), (36000, 130, 2050), (66000, 100, 2050), (5100, 4130, 1800)])
+@pytest.mark.parametrize("M,N,K", [(2100, 4100, 2050), (36000, 130, 2050), (66000, 100, 2050), (5100, 4130, 1800),
+                                   (4352, 4099, 1800), (76800, 260, 1800), (2100, 1030, 700)])
 @pytest.mark.parametrize("dtype,accumulate,more", [("f32", False, 0), ("bf16", True, 5)])
 def test_product_in_two_launches(M, N, K, dtype, accumulate, more):
     """A few tiles more than run at a time: the last columns or the last rows are smaller tiles of a second launch."""
