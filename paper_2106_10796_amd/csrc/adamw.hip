@@ -195,7 +195,6 @@ int check_adamw_list(const cdsgd_adamw_tensor *tensors, int num_tensors, int gra
         if ((t.weight16 != nullptr) != *copies || (t.weight16 && grad_dtype == CDSGD_GRAD_F32)) return CDSGD_ERR_PARAM;
         if (!aligned(t.weight, 16) || !aligned(t.weight16, 16) || !aligned(t.grad, 16) || !aligned(t.m, 16) || !aligned(t.v, 16))
             return CDSGD_ERR_ALIGN;
-        const size_t state = state_bits / 8 * t.n, blocks = cdsgd_state_blocks(t.n);
         for (void *p : {t.m, t.v}) buffers.add(p, state_bits / 8 * t.n, true);
         for (void *p : {t.m_scale, t.v_scale}) buffers.add(p, cdsgd_state_blocks(t.n), true);
         buffers.add(t.weight, t.n * 4, true);
