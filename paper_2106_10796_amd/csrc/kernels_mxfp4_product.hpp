@@ -34,17 +34,23 @@ __device__ __forceinline__ i4s buffer_of(const void *p, unsigned long long bytes
 // Every lane's 16 (4) bytes from `offset` of the buffer on to to + 16 (4) lane.  (The instruction's scalar offset takes no part in
 // the range check, so a place along the rows is a part of the buffer's address.)  The compiler does not know of these
 // loads: wait_for_loads<N> waits until all but the wave's last N of them are in LDS.  (Its own form of the instruction makes it wait
-// for all of them before the next read of any LDS.  m0 is a reserved register, which it sets next to its own uses.)
+// for all of them before the next read of any LDS.)  Nor does it look inside for the waits that gfx950 leaves to the program: one
+// state between a scalar write of m0 and a load to LDS, and five between a vector instruction that writes a word of the buffer's
+// description and the load; s_mov and s_nop are those five.  m0 is reserved, so the compiler warns that it will not save it, but it
+// takes the clobber for a write.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 template <int BYTES>
 __device__ __forceinline__ void load_to_lds(i4s buffer, CDSGD_LDS unsigned char *to, unsigned offset)
 {
     const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long long)to);
     static_assert(BYTES == 16 || BYTES == 4, "sizes in use");
     if constexpr (BYTES == 16)
-        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory", "m0");
     else
-        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(buffer) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 template <int N>
 __device__ __forceinline__ void wait_for_loads()
