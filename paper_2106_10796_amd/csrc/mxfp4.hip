@@ -48,7 +48,7 @@ constexpr unsigned long long kMostGroups = 0xFFFFFFFFull / 256;  // workgroups o
 template <int DT, typename F>
 void with_ring(const Product &how, size_t M, size_t N, F f)
 {
-    const auto ring = [&](auto kernel) { f(kernel, count_of(M, 16u * how.ring_rows) * count_of(N, 16), 64u * how.ring_waves); };
+    const auto ring = [&](auto kernel) { f(kernel, (unsigned)rings_of(how, M, N), 64u * how.ring_waves); };
     if (how.ring_rows == 1 && how.ring_waves == 8) ring(k_ring<DT, 1, 1, 2, 8>);
     else if (how.ring_rows == 1) ring(k_ring<DT, 1, 1, 2, 4>);
     else if (how.ring_rows == 2 && how.ring_waves == 8) ring(k_ring<DT, 2, 1, 2, 8>);
@@ -60,10 +60,10 @@ void with_ring(const Product &how, size_t M, size_t N, F f)
 template <int DT, typename F>
 void with_tiles(Tile tile, F f)
 {
-    if (tile == k64By64) f(k_tiles<DT, 64, 64, 2, 2, 4>, 256u);
-    else if (tile == k128By128) f(k_tiles<DT, 128, 128, 2, 2, 2>, 256u);
-    else if (tile == k128By256) f(k_tiles<DT, 128, 256, 2, 4, 3>, 512u);
-    else f(k_tiles<DT, 256, 256, 2, 4, 2>, 512u);
+    if (tile == k64By64) f(k_tiles<DT, 64, 64, 2, 2, 4>);
+    else if (tile == k128By128) f(k_tiles<DT, 128, 128, 2, 2, 2>);
+    else if (tile == k128By256) f(k_tiles<DT, 128, 256, 2, 4, 3>);
+    else f(k_tiles<DT, 256, 256, 2, 4, 2>);
 }
 
 }  // namespace
@@ -166,44 +166,34 @@ int cdsgd_mxfp4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const ui
         if (overlap2(out, ob, in[i], bytes[i]) || (want && overlap2(workspace, want, in[i], bytes[i]))) return CDSGD_ERR_ALIAS;
     if (want && overlap2(out, ob, workspace, want)) return CDSGD_ERR_ALIAS;
     const Product how = product_of(M, N, K);
-    int status = CDSGD_OK;
+    if (lanes_of(how, M, N) > 0xFFFFFFFFull) return CDSGD_ERR_SIZE;
     hipStream_t s = (hipStream_t)hip_stream;
     const unsigned m = (unsigned)M, n = (unsigned)N, groups = (unsigned)groups_of(K);
-    const auto fits = [&](unsigned long long count, unsigned lanes) {
-        if (count > 0xFFFFFFFFull / lanes) status = CDSGD_ERR_SIZE;
-        return status == CDSGD_OK;
-    };
     // rows [m0, m1) and columns [n0, n1) of the result, in tiles
     const auto tiles = [&](auto dt, Tile tile, size_t m0, size_t n0, size_t m1, size_t n1, auto *to, size_t row, int add) {
-        with_tiles<decltype(dt)::value>(tile, [&](auto kernel, unsigned lanes) {
-            const unsigned long long tiles_m = tiles_of(tile, m1 - m0, 1), tiles_n = tiles_of(tile, 1, n1 - n0), count = tiles_m * tiles_n * how.splits;
-            if (fits(count, lanes))
-                hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(lanes), 0, s, a_codes, a_scales, b_codes, b_scales, m, n, groups, to,
-                                   row, add, how.splits, (unsigned)m0, (unsigned)n0, (unsigned)tiles_m, (unsigned)tiles_n);
+        with_tiles<decltype(dt)::value>(tile, [&](auto kernel) {
+            const unsigned tiles_m = (unsigned)tiles_of(tile, m1 - m0, 1), tiles_n = (unsigned)tiles_of(tile, 1, n1 - n0);
+            hipLaunchKernelGGL(kernel, dim3(tiles_m * tiles_n * how.splits), dim3(lanes_of(tile)), 0, s, a_codes, a_scales, b_codes, b_scales,
+                               m, n, groups, to, row, add, how.splits, (unsigned)m0, (unsigned)n0, tiles_m, tiles_n);
         });
     };
     with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         Elem<DT> *const to = static_cast<Elem<DT> *>(out);
         if (how.ring_rows) {
-            with_ring<DT>(how, M, N, [&](auto kernel, unsigned long long count, unsigned lanes) {
-                if (fits(count, lanes))
-                    hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(lanes), 0, s, a_codes, a_scales, b_codes, b_scales, m, n, groups,
-                                       to, ld, accumulate);
+            with_ring<DT>(how, M, N, [&](auto kernel, unsigned count, unsigned lanes) {
+                hipLaunchKernelGGL(kernel, dim3(count), dim3(lanes), 0, s, a_codes, a_scales, b_codes, b_scales, m, n, groups, to, ld,
+                                   accumulate);
             });
         } else if (how.splits > 1) {
             float *const parts = static_cast<float *>(workspace);
-            const unsigned long long join = count_of(count_of(N, 4) * M, 256);
-            if (!fits(join, 256)) return;
             tiles(std::integral_constant<int, kGradF32>(), how.tile, 0, 0, M, N, parts, N, 0);
-            if (status == CDSGD_OK)
-                hipLaunchKernelGGL((k_join<DT>), dim3((unsigned)join), dim3(256), 0, s, parts, m, n, how.splits, to, ld, accumulate);
+            hipLaunchKernelGGL((k_join<DT>), dim3((unsigned)joins_of(M, N)), dim3(256), 0, s, parts, m, n, how.splits, to, ld, accumulate);
         } else {
             tiles(dt, how.tile, 0, 0, how.rest_m ? how.rest_m : M, how.rest_n ? how.rest_n : N, to, ld, accumulate);
-            if (how.rest_tile && status == CDSGD_OK) tiles(dt, how.rest_tile, how.rest_m, how.rest_n, M, N, to, ld, accumulate);
+            if (how.rest_tile) tiles(dt, how.rest_tile, how.rest_m, how.rest_n, M, N, to, ld, accumulate);
         }
     });
-    if (status != CDSGD_OK) return status;
     return launch_status();
 }
 

@@ -72,9 +72,11 @@ inline Product without_a_last_round(Product p, size_t M, size_t N)
 // and 128 by 128, two groups to a compute unit, whose stores and products overlap by themselves, but which read more:
 //   16384 x 8192 x 512  82.5, t128 92.3                          4096 x 25088 x 256 52, t128 60
 //   16384 x 8192 x 1024 125, t256 105                            2048 x 4096 x 25088 114, t128 106
+// Rings of so many columns that a launch would pass its 2^32 lanes (n16 groups of 256) leave them to tiles of 64.
 inline Product product_of(size_t M, size_t N, size_t K)
 {
     const unsigned long long n16 = count_of(N, 16);
+    if (M <= 32 && n16 >= 1ull << 24) return {0, 0, k64By64, 1};
     if (M <= 16) return {1, n16 <= 512 ? 8 : 4, kNoTile, 1};
     if (n16 * count_of(M, 32) <= 256) return {2, 8, kNoTile, 1};
     if (M <= 32) return {2, 4, kNoTile, 1};
@@ -87,6 +89,22 @@ inline Product product_of(size_t M, size_t N, size_t K)
     if (stages < 4) return {0, 0, k128By128, 1};
     const Product p = {0, 0, k256By256, 1};
     return stages < 8 ? p : without_a_last_round(p, M, N);
+}
+
+inline unsigned lanes_of(Tile t) { return t == k64By64 || t == k128By128 ? 256 : 512; }
+inline unsigned long long rings_of(const Product &p, size_t M, size_t N) { return count_of(M, 16u * p.ring_rows) * count_of(N, 16); }
+
+// Groups of 256 lanes that add up a sum's parts, four neighbouring results to a lane.
+inline unsigned long long joins_of(size_t M, size_t N) { return count_of(count_of(N, 4) * M, 256); }
+
+// Lanes of the largest launch.
+inline unsigned long long lanes_of(const Product &p, size_t M, size_t N)
+{
+    if (p.ring_rows) return rings_of(p, M, N) * 64 * p.ring_waves;
+    const unsigned long long tiles = tiles_of(p.tile, p.rest_m ? p.rest_m : M, p.rest_n ? p.rest_n : N) * p.splits * lanes_of(p.tile);
+    const unsigned long long rest = p.rest_tile ? tiles_of(p.rest_tile, M - p.rest_m, N - p.rest_n) * lanes_of(p.rest_tile) : 0;
+    const unsigned long long join = p.splits > 1 ? joins_of(M, N) * 256 : 0;
+    return tiles > rest ? (tiles > join ? tiles : join) : (rest > join ? rest : join);
 }
 
 }  // namespace
