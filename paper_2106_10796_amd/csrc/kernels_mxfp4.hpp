@@ -185,10 +185,10 @@ __device__ __forceinline__ void quantize_rows(const Elem<DT> *x, size_t ld, unsi
 
 template <int DT, int ROWS>
 __global__ __launch_bounds__(256) void k_quantize_rows(const Elem<DT> *__restrict__ x, size_t ld, unsigned rows, unsigned cols,
-                                                       uint8_t *__restrict__ codes, uint8_t *__restrict__ scales)
+                                                       uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, unsigned first)
 {
-    const unsigned col_blocks = (cols + kRowCols - 1) / kRowCols;
-    const unsigned r0 = (blockIdx.x / col_blocks * 4u + threadIdx.x / 64u) * ROWS, c0 = blockIdx.x % col_blocks * kRowCols;
+    const unsigned col_blocks = (cols + kRowCols - 1) / kRowCols, group = first + blockIdx.x;
+    const unsigned r0 = (group / col_blocks * 4u + threadIdx.x / 64u) * ROWS, c0 = group % col_blocks * kRowCols;
     if (r0 >= rows) return;
     const unsigned c = c0 + threadIdx.x % 64u * 8u;
     if (r0 + ROWS <= rows && c0 + kRowCols <= cols) quantize_rows<DT, ROWS, false>(x, ld, rows, cols, r0, c, codes, scales);
@@ -245,12 +245,13 @@ __device__ __forceinline__ void load_tile(const Elem<DT> *x, size_t ld, unsigned
 template <int DT, bool ROW>
 __global__ __launch_bounds__(kTileLanes<DT>) void k_quantize_tiles(const Elem<DT> *__restrict__ x, size_t ld, unsigned rows,
                                                                    unsigned cols, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
-                                                                   uint8_t *__restrict__ codes_t, uint8_t *__restrict__ scales_t)
+                                                                   uint8_t *__restrict__ codes_t, uint8_t *__restrict__ scales_t,
+                                                                   unsigned first)
 {
     __shared__ __align__(16) Elem<DT> tile[kTile * kTile];
     // Four tiles, two by two, run on one XCD (group b on XCD b % 8) one after the other, so that the halves of a line of codes that
     // neighbouring tiles write meet in one L2.
-    const unsigned supers_across = (cols + 2 * kTile - 1) / (2 * kTile), i = blockIdx.x / 8u, super = i / 4u * 8u + blockIdx.x % 8u;
+    const unsigned supers_across = (cols + 2 * kTile - 1) / (2 * kTile), group = first + blockIdx.x, i = group / 8u, super = i / 4u * 8u + group % 8u;
     const unsigned r0 = (super / supers_across * 2u + i / 2u % 2u) * kTile, c0 = (super % supers_across * 2u + i % 2u) * kTile;
     if (r0 >= rows || c0 >= cols) return;
     if (r0 + kTile <= rows && c0 + kTile <= cols) load_tile<DT, ROW, false>(x, ld, rows, cols, r0, c0, codes, scales, tile);
@@ -296,12 +297,12 @@ template <int DT>
 constexpr unsigned kValueCols = 64 * 16 / sizeof(Elem<DT>);
 template <int DT, int ROWS>
 __global__ __launch_bounds__(256) void k_dequantize(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
-                                                    unsigned rows, unsigned cols, Elem<DT> *__restrict__ out, size_t ld)
+                                                    unsigned rows, unsigned cols, Elem<DT> *__restrict__ out, size_t ld, unsigned first)
 {
     constexpr unsigned E = 16 / sizeof(Elem<DT>);
-    const unsigned col_blocks = (cols + kValueCols<DT> - 1) / kValueCols<DT>, groups = (cols + kGroup - 1) / kGroup;
-    const unsigned r0 = (blockIdx.x / col_blocks * 4u + threadIdx.x / 64u) * ROWS;
-    const unsigned c = blockIdx.x % col_blocks * kValueCols<DT> + threadIdx.x % 64u * E;
+    const unsigned col_blocks = (cols + kValueCols<DT> - 1) / kValueCols<DT>, groups = (cols + kGroup - 1) / kGroup, group = first + blockIdx.x;
+    const unsigned r0 = (group / col_blocks * 4u + threadIdx.x / 64u) * ROWS;
+    const unsigned c = group % col_blocks * kValueCols<DT> + threadIdx.x % 64u * E;
     if (r0 >= rows || c >= cols) return;
     unsigned w[ROWS], s[ROWS];
 #pragma unroll

@@ -42,7 +42,17 @@ inline int check_matrix(size_t rows, size_t cols)
     return CDSGD_OK;
 }
 
-constexpr unsigned long long kMostGroups = 0xFFFFFFFFull / 256;  // workgroups of 256 lanes in a launch
+// Calls launch(groups, number of the first) for launches below 2^32 lanes; all but the last hold a multiple of 32 groups, what
+// k_quantize_tiles numbers together.  (One but for matrices of 2^27 rows and more.)  The kernels number groups in 32 bits.
+template <typename F>
+int in_launches(unsigned long long groups, unsigned lanes, F launch)
+{
+    if (groups > 0xFFFFFFFFull) return CDSGD_ERR_SIZE;
+    const unsigned long long most = 0xFFFFFFFFull / lanes / 32 * 32;
+    for (unsigned long long first = 0; first < groups; first += most)
+        launch(dim3((unsigned)(groups - first < most ? groups - first : most)), (unsigned)first);
+    return launch_status();
+}
 
 // Calls f(kernel, groups, lanes) with the ring that `how` names, for results of type DT.
 template <int DT, typename F>
@@ -97,17 +107,19 @@ int cdsgd_mxfp4_quantize(const void *x, int dtype, size_t rows, size_t cols, siz
     const unsigned long long across = count_of(cols, kRowCols);
     const bool many = across * count_of(rows, 16) >= 256;
     const unsigned long long groups = codes_t ? tile_groups(rows, cols) : across * count_of(rows, many ? 16 : 4);
-    if (groups > kMostGroups / 2) return CDSGD_ERR_SIZE;
+    int status = CDSGD_OK;
     with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         const Elem<DT> *from = static_cast<const Elem<DT> *>(x);
-        const dim3 grid((unsigned)groups), block(codes_t ? kTileLanes<DT> : 256u);
-        if (!codes_t && many) hipLaunchKernelGGL((k_quantize_rows<DT, 4>), grid, block, 0, s, from, ld, r, c, codes, scales);
-        else if (!codes_t) hipLaunchKernelGGL((k_quantize_rows<DT, 1>), grid, block, 0, s, from, ld, r, c, codes, scales);
-        else if (codes) hipLaunchKernelGGL((k_quantize_tiles<DT, true>), grid, block, 0, s, from, ld, r, c, codes, scales, codes_t, scales_t);
-        else hipLaunchKernelGGL((k_quantize_tiles<DT, false>), grid, block, 0, s, from, ld, r, c, codes, scales, codes_t, scales_t);
+        const dim3 block(codes_t ? kTileLanes<DT> : 256u);
+        status = in_launches(groups, block.x, [&](dim3 grid, unsigned first) {
+            if (!codes_t && many) hipLaunchKernelGGL((k_quantize_rows<DT, 4>), grid, block, 0, s, from, ld, r, c, codes, scales, first);
+            else if (!codes_t) hipLaunchKernelGGL((k_quantize_rows<DT, 1>), grid, block, 0, s, from, ld, r, c, codes, scales, first);
+            else if (codes) hipLaunchKernelGGL((k_quantize_tiles<DT, true>), grid, block, 0, s, from, ld, r, c, codes, scales, codes_t, scales_t, first);
+            else hipLaunchKernelGGL((k_quantize_tiles<DT, false>), grid, block, 0, s, from, ld, r, c, codes, scales, codes_t, scales_t, first);
+        });
     });
-    return launch_status();
+    return status;
 }
 
 int cdsgd_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, size_t rows, size_t cols, void *out, int dtype, size_t ld,
@@ -125,17 +137,19 @@ int cdsgd_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, size_t r
     const unsigned long long across = count_of(cols, dtype == CDSGD_GRAD_F32 ? kValueCols<kGradF32> : kValueCols<kGradBF16>);
     const bool many = across * count_of(rows, 16) >= 256;
     const unsigned long long groups = across * count_of(rows, many ? 16 : 4);
-    if (groups > kMostGroups) return CDSGD_ERR_SIZE;
+    int status = CDSGD_OK;
     with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         const auto launch = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)hip_stream, codes, scales, (unsigned)rows,
-                               (unsigned)cols, static_cast<Elem<DT> *>(out), ld);
+            status = in_launches(groups, 256, [&](dim3 grid, unsigned first) {
+                hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)hip_stream, codes, scales, (unsigned)rows, (unsigned)cols,
+                                   static_cast<Elem<DT> *>(out), ld, first);
+            });
         };
         if (many) launch(k_dequantize<DT, 4>);
         else launch(k_dequantize<DT, 1>);
     });
-    return launch_status();
+    return status;
 }
 
 size_t cdsgd_mxfp4_matmul_workspace(size_t M, size_t N, size_t K)

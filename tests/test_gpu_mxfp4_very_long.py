@@ -21,3 +21,29 @@ def test_product_of_few_rows(M, K):
     want, size = other @ few.t().contiguous(), other.abs() @ few.abs().t().contiguous()
     # sums under one pair of scales are exact, those of the four blocks of 32 are rounded once each, and the result once to 16 bits
     assert bool(((out[:, at].double() - want).abs() <= 12 * 2.0 ** -24 * size + 2.0 ** -8 * want.abs()).all())
+
+
+def on_the_grid(shape, dtype, seed):
+    """Values that MXFP4 holds exactly; blocks of 32 along the last axis begin with a 4."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], device="cuda").to(dtype)[torch.randint(0, 8, shape, dtype=torch.uint8, device="cuda", generator=gen).int()]
+    x[..., ::32] = 4
+    return x
+
+
+def test_rows_there_and_back():
+    x = on_the_grid(((1 << 28) + 37, 3), torch.float16, 1)
+    q = B.new_mxfp4(*x.shape)
+    B.cdsgd_mxfp4_quantize(x, q)
+    out = torch.zeros_like(x)
+    B.cdsgd_mxfp4_dequantize(q, out)
+    assert torch.equal(out, x)
+
+
+def test_columns_there_and_back():
+    x = on_the_grid((1, (1 << 29) + 37), torch.float32, 2).t().contiguous()
+    q = B.new_mxfp4(1, x.shape[0])
+    B.cdsgd_mxfp4_quantize(x, None, q)
+    out = torch.zeros(1, x.shape[0], device="cuda")
+    B.cdsgd_mxfp4_dequantize(q, out)
+    assert torch.equal(out.t(), x)
