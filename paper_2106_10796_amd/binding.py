@@ -728,16 +728,32 @@ class _Mxfp4(NamedTuple):
     cols: int
 
 
+def _as_bytes(t, name):
+    """t, or a copy of it as uint8 where it holds bytes in integers of another type."""
+    if not (isinstance(t, torch.Tensor) and t.dtype in (torch.int16, torch.int32, torch.int64)):
+        return t
+    if bool(((t < 0) | (t > 255)).any()):
+        raise ValueError("%s holds integers that are not bytes" % name)
+    return t.to(torch.uint8).contiguous()
+
+
 class Mxfp4(_Mxfp4):
     """A matrix of `rows` by `cols` in microscaled 4-bit floating point (the layout is in include/cdsgd_ops.h):
     codes uint8 [rows, 64 g] and scales uint8 [g, rows, 4] with g = ceil(cols / 128), contiguous CUDA tensors, which are
-    kept as they are.  Bytes in integers of another type, as a quantiser written in torch leaves them, are converted here."""
+    kept as they are.  Bytes in integers of another type, as a quantiser written in torch leaves them, are looked over (on the host)
+    and copied: such a matrix is an operand, but nothing can be quantised into it."""
     __slots__ = ()
 
     def __new__(cls, codes, scales, rows, cols):
-        held = [t.to(torch.uint8).contiguous() if isinstance(t, torch.Tensor) and t.dtype in (torch.int16, torch.int32, torch.int64) else t
-                for t in (codes, scales)]
-        return super().__new__(cls, *held, int(rows), int(cols))
+        held = [_as_bytes(codes, "codes"), _as_bytes(scales, "scales")]
+        if cls is Mxfp4 and not (held[0] is codes and held[1] is scales):
+            cls = _Mxfp4Copy
+        return _Mxfp4.__new__(cls, *held, int(rows), int(cols))
+
+
+class _Mxfp4Copy(Mxfp4):
+    """A matrix whose buffers are copies of the caller's tensors."""
+    __slots__ = ()
 
 
 def new_mxfp4(rows: int, cols: int, device="cuda") -> Mxfp4:
@@ -782,6 +798,9 @@ def cdsgd_mxfp4_quantize(x, row=None, col=None):
     may be None."""
     st = _native().mxfp4_quantize(x, row, col, _stream)
     if st < 0:
+        for q, name in ((row, "row"), (col, "col")):
+            if isinstance(q, _Mxfp4Copy):
+                raise TypeError("%s holds copies of tensors that are not uint8: the caller's would not receive anything" % name)
         p, dtype, r, c, ld = _rows(x, "x")
         codes, scales = _mx(row, "row", r, c)
         codes_t, scales_t = _mx(col, "col", c, r)

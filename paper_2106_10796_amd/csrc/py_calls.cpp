@@ -296,9 +296,12 @@ struct Mx {
     size_t rows = 0, cols = 0;
 };
 
-Mx mx(PyObject *o)
+Mx mx(PyObject *o, bool written = false)
 {
-    if (!PyTuple_Check(o) || std::strcmp(Py_TYPE(o)->tp_name, "Mxfp4") != 0 || PyTuple_GET_SIZE(o) != 4) throw NotPlain();
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) throw NotPlain();
+    // (copies of the caller's tensors are read alone)
+    const char *kind = Py_TYPE(o)->tp_name;
+    if (std::strcmp(kind, "Mxfp4") != 0 && (written || std::strcmp(kind, "_Mxfp4Copy") != 0)) throw NotPlain();
     const long rows = whole(PyTuple_GET_ITEM(o, 2)), cols = whole(PyTuple_GET_ITEM(o, 3));
     if (rows < 1 || cols < 1 || rows > INT_MAX || cols > INT_MAX) throw NotPlain();
     const size_t groups = ((size_t)cols + 127) / 128;
@@ -342,7 +345,7 @@ PyObject *mxfp4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 4, [&] {
         const Matrix x = matrix(a[0]);
-        const Mx row = a[1] == Py_None ? Mx() : mx(a[1]), col = a[2] == Py_None ? Mx() : mx(a[2]);
+        const Mx row = a[1] == Py_None ? Mx() : mx(a[1], true), col = a[2] == Py_None ? Mx() : mx(a[2], true);
         if ((row.codes && (row.rows != x.rows || row.cols != x.cols)) || (col.codes && (col.rows != x.cols || col.cols != x.rows))) throw NotPlain();
         void *s = stream_of(a[3]);
         return unlocked([&] { return lib.mxfp4_quantize(x.p, x.dtype, x.rows, x.cols, x.ld, row.codes, row.scales, col.codes, col.scales, s); });
