@@ -303,7 +303,7 @@ int cdsgd_adamw_step(cdsgd_adamw_plan *plan, long step, double lr, double beta1,
         return CDSGD_ERR_PARAM;
     if (!aligned(clip, 4)) return CDSGD_ERR_ALIGN;
     StepFactors f;
-    f.lr = (float)lr;
+    f.lr = lr;
     f.beta1 = (float)beta1;
     f.one_minus_beta1 = (float)(1.0 - beta1);
     f.beta2 = (float)beta2;

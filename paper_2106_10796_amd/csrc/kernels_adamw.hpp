@@ -25,7 +25,8 @@ struct StepChunk {
 };
 
 struct StepFactors {
-    float lr, beta1, one_minus_beta1, beta2, one_minus_beta2, inv_sqrt_bias2, eps, lr_over_bias1, grad_scale;
+    double lr;
+    float beta1, one_minus_beta1, beta2, one_minus_beta2, inv_sqrt_bias2, eps, lr_over_bias1, grad_scale;
     unsigned seed;
 };
 
@@ -162,6 +163,9 @@ __device__ __forceinline__ unsigned narrow2(float a, float b)
 // ---------------------------------------------------------------------------
 // the step
 // ---------------------------------------------------------------------------
+// The factor that decays a tensor's weights, in 64 bits and rounded once, as the other factors are on the host.
+__device__ __forceinline__ float keep_of(const StepFactors &f, const StepChunk &c) { return (float)(1.0 - f.lr * (double)c.weight_decay); }
+
 // One element: m, v and the weight.
 __device__ __forceinline__ void adamw1(float g, float &m, float &v, float &w, const StepFactors &f, float keep)
 {
@@ -188,7 +192,7 @@ __device__ __forceinline__ void adamw32_piece(const StepChunk &c, unsigned first
     sm.load32(m);
     sv.load32(v);
     sw.load32(w);
-    const float keep = 1.0f - f.lr * c.weight_decay;
+    const float keep = keep_of(f, c);
 #pragma unroll
     for (int i = 0; i < E; ++i) adamw1(g[i] * gs, m[i], v[i], w[i], f, keep);
     sm.store32(m);
@@ -329,7 +333,7 @@ __device__ __forceinline__ void adamw8_piece(const StepChunk &c, unsigned piece,
         g[k].template load<RAGGED>(Span<E, LOAD, STORE>(c.grad, c.elems, grad_bytes<GT>(), first));
         Span<E, LOAD, STORE>(c.weight, c.elems, 4, first).load32(w[k]);
     }
-    const float keep = 1.0f - f.lr * c.weight_decay;
+    const float keep = keep_of(f, c);
     float m[B][E], v[B][E];
     unsigned most[B];
 #pragma unroll
