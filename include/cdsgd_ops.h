@@ -27,7 +27,7 @@ extern "C" {
  * fixed by the list.  A NaN or an infinity in the list makes out[0] not finite.
  *   grads, sizes  host arrays [num_tensors]: device pointers (16-byte aligned) and element counts (> 0)
  *   grad_dtype    a cdsgd_grad_dtype
- *   out           out fp32[2], 4-byte aligned
+ *   out           out fp32[2], 4-byte aligned, apart from the gradients (CDSGD_ERR_ALIAS)
  *   max_norm      > 0; INFINITY computes the norm alone (out[1] = 1)
  * The handle keeps a table and the partial sums in one device allocation and borrows the gradients: calls on
  * one handle must be ordered (same stream, or events).
@@ -77,7 +77,7 @@ int cdsgd_grad_norm_destroy(cdsgd_grad_norm *norm);
  * list.  The plan copies a table to the device and borrows the buffers; passes of one plan must be ordered.
  *   step          number of this step, from 1 on;  lr, betas, eps, grad_scale: finite, lr >= 0, 0 <= beta < 1,
  *                 eps >= 1e-37 (CDSGD_ERR_PARAM)
- *   clip          in  fp32[2] as cdsgd_grad_norm_compute writes it, or NULL
+ *   clip          in  fp32[2] as cdsgd_grad_norm_compute writes it, apart from what the step writes (CDSGD_ERR_ALIAS), or NULL
  */
 #define CDSGD_STATE_BLOCK 256
 typedef struct {

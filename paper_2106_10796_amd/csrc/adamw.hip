@@ -8,6 +8,7 @@
 #include <cstdint>
 #include <memory>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "cdsgd_ops.h"
@@ -99,12 +100,40 @@ struct Buffers {
     }
 };
 
+// Bytes that a handle's passes read, or write, against an argument of a call.
+struct Extents {
+    std::vector<std::pair<uintptr_t, uintptr_t>> all;
+
+    void add(const void *p, size_t bytes)
+    {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p) all.push_back({at, at + bytes});
+    }
+    void close()  // sorts, and joins what overlaps
+    {
+        std::sort(all.begin(), all.end());
+        size_t n = 0;
+        for (const auto &r : all) {
+            if (n && r.first <= all[n - 1].second) all[n - 1].second = std::max(all[n - 1].second, r.second);
+            else all[n++] = r;
+        }
+        all.resize(n);
+    }
+    bool touch(const void *p, size_t bytes) const
+    {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        const auto after = std::lower_bound(all.begin(), all.end(), std::make_pair(at + bytes, (uintptr_t)0));  // begins behind p's bytes
+        return p && after != all.begin() && (after - 1)->second > at;
+    }
+};
+
 inline bool good_rate(double x) { return std::isfinite(x) && std::isfinite((float)x); }
 
 }  // namespace
 
 struct cdsgd_grad_norm {
     Block block;
+    Extents read;
     NormChunk *chunks = nullptr;
     double *partial = nullptr;
     unsigned *done = nullptr;
@@ -116,6 +145,7 @@ struct cdsgd_adamw_plan {
     std::vector<StepChunk> host_chunks;
     std::vector<size_t> sizes;
     Block block;
+    Extents written;  // by a step
     cdsgd_grad_norm norm;
     unsigned long long elements = 0;
     int grad_dtype = 0, state_bits = kState32, readout_dtype = -1;
@@ -135,7 +165,9 @@ int norm_create(cdsgd_grad_norm &h, const void *const *grads, const size_t *size
         if (!aligned(grads[i], 16)) return CDSGD_ERR_ALIGN;
         total += pieces(sizes[i], norm_elems(grad_dtype));
         if (total > kMaxNormChunks) return CDSGD_ERR_SIZE;
+        h.read.add(grads[i], sizes[i] * bytes_of(grad_dtype));
     }
+    h.read.close();
     h.grad_dtype = grad_dtype;
     h.num_chunks = (unsigned)total;
     h.groups = norm_groups(h.num_chunks);
@@ -162,6 +194,7 @@ int norm_compute(const cdsgd_grad_norm &h, double grad_scale, double max_norm, f
     if (!out) return CDSGD_ERR_NULL;
     if (!std::isfinite(grad_scale) || !(max_norm > 0.0)) return CDSGD_ERR_PARAM;
     if (!aligned(out, 4)) return CDSGD_ERR_ALIGN;
+    if (h.read.touch(out, 2 * sizeof(float))) return CDSGD_ERR_ALIAS;
     hipStream_t s = (hipStream_t)hip_stream;
     const double scale = std::fabs(grad_scale);
 #define CDSGD_LAUNCH_NORM(GT)                                                                                   \
@@ -263,6 +296,10 @@ try {
         grads.push_back(t.grad);
         plan->sizes.push_back(t.n);
         plan->elements += t.n;
+        plan->written.add(t.weight, t.n * 4);
+        plan->written.add(t.weight16, t.n * 2);
+        for (void *p : {t.m, t.v}) plan->written.add(p, t.n * sb);
+        for (void *p : {t.m_scale, t.v_scale}) plan->written.add(p, cdsgd_state_blocks(t.n));
         for (size_t at = 0; at < t.n; at += kStepChunk) {
             StepChunk c{};
             c.weight = t.weight + at;
@@ -279,6 +316,7 @@ try {
         }
         counter += (unsigned)(cdsgd_state_blocks(t.n) * CDSGD_STATE_BLOCK);
     }
+    plan->written.close();
     rc = plan->block.fill(plan->host_chunks.data(), sizeof(StepChunk) * plan->host_chunks.size());
     if (rc == CDSGD_OK) rc = norm_create(plan->norm, grads.data(), plan->sizes.data(), num_tensors, grad_dtype);
     if (rc != CDSGD_OK) return rc;
@@ -302,6 +340,7 @@ int cdsgd_adamw_step(cdsgd_adamw_plan *plan, long step, double lr, double beta1,
         !good_rate(eps) || eps < 1e-37 || !good_rate(grad_scale))
         return CDSGD_ERR_PARAM;
     if (!aligned(clip, 4)) return CDSGD_ERR_ALIGN;
+    if (plan->written.touch(clip, 2 * sizeof(float))) return CDSGD_ERR_ALIAS;
     StepFactors f;
     f.lr = lr;
     f.beta1 = (float)beta1;
