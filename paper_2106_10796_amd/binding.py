@@ -769,9 +769,9 @@ def new_mxfp4_workspace(shapes, device="cuda"):
     return torch.empty(need, dtype=torch.uint8, device=device) if need else None
 
 
-def _mx(q, name, rows=None, cols=None):
-    """The addresses of a matrix: (codes, scales); (None, None) for None."""
-    if q is None:
+def _mx(q, name, rows=None, cols=None, optional=False):
+    """The addresses of a matrix: (codes, scales); (None, None) for None where it is optional."""
+    if q is None and optional:
         return None, None
     if not isinstance(q, Mxfp4):
         raise TypeError("%s must be an Mxfp4" % name)
@@ -802,8 +802,8 @@ def cdsgd_mxfp4_quantize(x, row=None, col=None):
             if isinstance(q, _Mxfp4Copy):
                 raise TypeError("%s holds copies of tensors that are not uint8: the caller's would not receive anything" % name)
         p, dtype, r, c, ld = _rows(x, "x")
-        codes, scales = _mx(row, "row", r, c)
-        codes_t, scales_t = _mx(col, "col", c, r)
+        codes, scales = _mx(row, "row", r, c, optional=True)
+        codes_t, scales_t = _mx(col, "col", c, r, optional=True)
         st = lib().cdsgd_mxfp4_quantize(p, dtype, r, c, ld, codes, scales, codes_t, scales_t, _stream())
     if st != OK:
         _check(st, "cdsgd_mxfp4_quantize")
@@ -826,7 +826,7 @@ def cdsgd_mxfp4_matmul(a, b, out, workspace=None, accumulate=False):
     st = _native().mxfp4_matmul(a, b, out, workspace, accumulate, _stream)
     if st < 0:
         ac, as_ = _mx(a, "a")
-        bc, bs = _mx(b, "b", b.rows, a.cols)
+        bc, bs = _mx(b, "b", getattr(b, "rows", 0), a.cols)
         p, dtype, M, N, ld = _rows(out, "out", a.rows, b.rows)
         st = lib().cdsgd_mxfp4_matmul(ac, as_, bc, bs, M, N, a.cols, p, dtype, ld, int(bool(accumulate)),
                                       _dev(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0,
