@@ -23,8 +23,9 @@ extern "C" {
  * Norm of a list of gradients, for clipping.  With s = grad_scale and the sum over every element of the list,
  *   out[0] = norm = sqrt(sum (s g)^2)
  *   out[1] = norm > max_norm ? max_norm / norm : 1
- * Squares and sums are formed in 64 bits, so no finite 32-bit gradient overflows them; the sum's order is
- * fixed by the list.  A NaN or an infinity in the list makes out[0] not finite.
+ * Squares, sums and both results are formed in 64 bits, where no finite 32-bit gradient overflows, and rounded once; the sum's
+ * order is fixed by the list.  out[0] is not finite if the list holds a NaN or an infinity, and also if the norm itself is above the
+ * largest fp32 number, though every gradient is finite; out[1] is right then, but a step that takes the two is skipped.
  *   grads, sizes  host arrays [num_tensors]: device pointers (16-byte aligned) and element counts (> 0)
  *   grad_dtype    a cdsgd_grad_dtype
  *   out           out fp32[2], 4-byte aligned, apart from the gradients (CDSGD_ERR_ALIAS)

@@ -1,4 +1,4 @@
-"""The factors of an AdamW step are formed in 64 bits and rounded once."""
+"""The factors of an AdamW step, and of a clip, are formed in 64 bits and rounded once."""
 import numpy as np
 import pytest
 import torch
@@ -32,3 +32,19 @@ def test_decay(bits):
         B.AdamWPlan(tensors, state_bits=bits).step(1, lr)
         for t, d in zip(tensors, decays):
             assert np.array_equal(t["weight"].cpu().numpy(), np.full(300, once(lr, d))), (lr, d)
+
+
+def test_a_norm_above_the_largest_number():
+    """Of finite gradients: infinite in 32 bits, its factor as it is in 64, and the step is skipped; under a scale it is a number again."""
+    g, n = 3e38, 1000
+    t = dict(weight=torch.ones(n, device="cuda"), grad=torch.full((n,), g, device="cuda"), m=torch.zeros(n, device="cuda"), v=torch.zeros(n, device="cuda"))
+    plan, out = B.AdamWPlan([t]), torch.zeros(2, device="cuda")
+    norm = float(np.float32(g)) * np.sqrt(n)
+    plan.grad_norm(out, max_norm=1e30)
+    assert out[0].item() == float("inf") and abs(out[1].item() / (1e30 / norm) - 1) < 1e-6
+    plan.step(1, 1e-3, clip=out)
+    assert bool((t["weight"] == 1).all()) and not t["m"].any() and not t["v"].any()
+    plan.grad_norm(out, grad_scale=2.0 ** -100, max_norm=1.0)
+    assert abs(out[0].item() / (norm * 2.0 ** -100) - 1) < 1e-6
+    plan.step(1, 1e-3, clip=out, grad_scale=2.0 ** -100)
+    assert bool((t["weight"] < 1).all()) and bool((t["m"] > 0).all())
