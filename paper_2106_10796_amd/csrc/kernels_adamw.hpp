@@ -177,8 +177,8 @@ __device__ __forceinline__ void adamw1(float g, float &m, float &v, float &w, co
     w = w * keep - (m * __builtin_amdgcn_rcpf(denom)) * f.lr_over_bias1;
 }
 
-// States in 32 bits: 26 to 30 bytes an element and some forty operations, bound by HBM: 25.6 M elements, bf16 gradients and a copy, 113 us,
-// 6.3 TB/s.  One wave per piece, one quad to a lane: every access of a wave is to whole lines in a row.
+// States in 32 bits: 26 to 28 bytes an element and some forty operations, bound by HBM: 25.6 M elements, bf16 gradients and a copy, 111 us,
+// 6.4 TB/s.  One wave per piece, one quad to a lane: every access of a wave is to whole lines in a row.
 constexpr unsigned kStepLanes = 64;
 template <int GT, bool COPY, bool RAGGED, int LOAD, int STORE>
 __device__ __forceinline__ void adamw32_piece(const StepChunk &c, unsigned first, const StepFactors &f, float gs)

@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const Elem<DT> *__restric
 // Blocks down the columns, and along the rows in the same pass if ROW.  A group takes a tile of 128 by 128: 64 bytes of every
 // row of either result, and the scale words of 128 of them in a row.  The tile goes through LDS in the matrix's own type; a band
 // of 32 rows is turned by 64 bytes against the one above, so that the lanes that read one column in four bands meet different banks.
-// Bound by HBM and by its stores of half lines: both forms of 4096 x 25088 in fp32 5.2 TB/s (99 us; 106 with neighbouring tiles on
+// Bound by HBM and by its stores of half lines: both forms of 4096 x 25088 in fp32 5.2 TB/s (100 us; 106 with neighbouring tiles on
 // different XCDs), of 2048 x 25088 in bf16 4.5 (35 us; 37.5).
 constexpr unsigned kTile = 128;
 template <int DT>
@@ -291,8 +291,8 @@ __global__ __launch_bounds__(kTileLanes<DT>) void k_quantize_tiles(const Elem<DT
 // ---------------------------------------------------------------------------
 // values
 // ---------------------------------------------------------------------------
-// 16 bytes of a row to a lane, so that a wave's store is to whole lines in a row, past the caches (fp32, 4096 x 25088: 7.0 TB/s, 88 us
-// at the default policy, 66 so; eight elements to a lane 160).
+// 16 bytes of a row to a lane, so that a wave's store is to whole lines in a row, past the caches (fp32, 4096 x 25088: 88 us
+// at the default policy, 66 so, 7.0 TB/s; eight elements to a lane 160.  In turn with the quantisation of such a matrix it takes 78).
 template <int DT>
 constexpr unsigned kValueCols = 64 * 16 / sizeof(Elem<DT>);
 template <int DT, int ROWS>

@@ -3,7 +3,7 @@
 // The kernels load codes and scale words from memory straight into LDS, a line of 128 bytes (256 elements) of a row at a time.
 // Eight lanes in a row ask for one line, which is what the path from L2 is fast at: the operand layout of the matrix
 // instructions puts neighbouring lanes in different rows, and loads in that order cost a compute unit 37 cycles each instead
-// of 16 (64 x 1000 x 4096: 8.1 us with operands straight from memory, 3.4 so).  The line's eight chunks of 16 bytes lie in LDS
+// of 16 (64 x 1000 x 4096: 8.1 us with operands straight from memory, 3.8 so).  The line's eight chunks of 16 bytes lie in LDS
 // turned by half the row's number (chunk c at c ^ (row / 2 % 8)), so that sixteen rows' reads of one chunk fill the banks.
 #pragma once
 
@@ -36,8 +36,8 @@ __device__ __forceinline__ i4s buffer_of(const void *p, unsigned long long bytes
 // loads: wait_for_loads<N> waits until all but the wave's last N of them are in LDS.  (Its own form of the instruction makes it wait
 // for all of them before the next read of any LDS.)  Nor does it look inside for the waits that gfx950 leaves to the program: one
 // state between a scalar write of m0 and a load to LDS, and five between a vector instruction that writes a word of the buffer's
-// description and the load; s_mov and s_nop are those five.  m0 is reserved, so the compiler warns that it will not save it, but it
-// takes the clobber for a write.
+// description and the load; s_mov and s_nop are those five (up to 3 % against s_nop 0, 64 x 4096 x 4096 4.9 -> 5.05 us, large
+// products the same).  m0 is reserved, so the compiler warns that it will not save it, but it takes the clobber for a write.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 template <int BYTES>
@@ -116,8 +116,8 @@ __device__ __forceinline__ void wave_sync()
 // few rows
 // ---------------------------------------------------------------------------
 // A group takes 16 FM rows of A and 16 FN of B; its W waves share the sum, line by line, and each has a ring of D slots in LDS of
-// its own, so that no wave waits for another before the end.  Bound by reading B: 1 x 4096 x 25088 9.9 us, 5.5 TB/s of the whole call,
-// 64 x 25088 x 4096 11.9 us, 4.9 TB/s; on small matrices by the launch (64 x 1000 x 4096: 3.4 us).
+// its own, so that no wave waits for another before the end.  Bound by reading B: 1 x 4096 x 25088 10.0 us, 5.5 TB/s of the whole call,
+// 64 x 25088 x 4096 11.6 us, 5.0 TB/s; on small matrices by the launch (64 x 1000 x 4096: 3.8 us).
 template <int FM, int FN>
 constexpr unsigned kRingSlot = (FN + FM) * 2048u + ((FN + 1) / 2 + (FM + 1) / 2) * 256u;
 
@@ -248,8 +248,8 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ partial,
 //   8192 x 4096 x 2048 fp32 65.2, 50.2, bf16 50.6, 44.9;  x 4096 fp32 95.0, 83.2, bf16 78.6, 75.8;  16384 x 8192 x 1024 bf16 115, 105;
 //   128 by 128 8192 x 4096 x 1024 bf16 37.6, 34.1;  spread over a half and over twice as long: 8192 x 4096 x 2048 fp32 58, 56, bf16 47, 45
 //
-// 8192 x 4096 x 4096 in bf16, call after call, takes 70 us, 3.9 PFLOP/s; bound by the card's power, not by any path: 58 us (and 57
-// without the spread) where all codes are the same.  256 by 256 with 4 waves 82, 128 by 128 82; the next tile's loads ahead of the
+// 8192 x 4096 x 4096 in bf16, call after call, takes 71 us, 3.9 PFLOP/s; bound by the card's power, not by any path: it draws 1385 of its
+// 1400 W at 1.82 GHz, and where all codes are the same 1190 W at 2.39 GHz for 57 us.  256 by 256 with 4 waves 82, 128 by 128 82; the next tile's loads ahead of the
 // stores, in groups that go from tile to tile, 74.
 template <int BM, int BN>
 constexpr unsigned kTileStage = (BM + BN) * 136u;
@@ -474,9 +474,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tiles(const uint8_t *__restric
     __syncthreads();
 
     // In the result's type through LDS, 32 rows of a wave at a time, so that rows are stored in pieces of 16 bytes to a lane: past
-    // the caches, which hold the operands (4096 x 25088 x 2048 in fp32: 204 us at the default policy, 185 so).  What is added to is
-    // read as the products lie, so that the sum is rounded once, from fp32; the loads of 32 rows are all under way before the first
-    // is used (8192 x 4096 x 4096 added to bf16: 90 us; one load and one store after the other, 106).
+    // the caches, which hold the operands (4096 x 25088 x 2048 in fp32: 204 us at the default policy, 185 so, 144 with what else is
+    // here).  What is added to is read as the products lie, so that the sum is rounded once, from fp32; the loads of 32 rows are all
+    // under way before the first is used (8192 x 4096 x 4096 added to one bf16 result call after call: 87 us, to three in turn 96;
+    // one load and one store after the other, 106).
     typedef Elem<DT> e4 __attribute__((ext_vector_type(4)));
     constexpr unsigned E = 16 / sizeof(Elem<DT>), kPerRow = TN / E, kAtOnce = 64 / kPerRow;
     CDSGD_LDS unsigned char *mine = lds + wave * (32u * kPitch);

@@ -55,7 +55,7 @@ inline Product without_a_last_round(Product p, size_t M, size_t N)
     return p;
 }
 
-// us, bf16 results, three sets of operands in turn; rWxF: rings of W waves, F fragments; t64, t128, t256: tiles of 64 by 64, 128 by 256,
+// us, bf16 results, three sets of operands in turn, without the wait states of the loads to LDS, which add up to 3 %; rWxF: rings of W waves, F fragments; t64, t128, t256: tiles of 64 by 64, 128 by 256,
 // 256 by 256; /S: split S ways
 //   16 x 8192 x 8192    r8x1 9.0, r4x1 10.6, t64 11.2            5 x 8192 x 300     r8x1 2.7, r4x1 2.5;  1 x 25088 x 512 6.1, 4.0
 //   32 x 8192 x 8192    r8x2 12.0, r4x2 10.7, t64 11.3           32 x 4096 x 4096   r8x2 3.4, r4x2 3.6
