@@ -129,7 +129,8 @@ int cdsgd_adamw_read_states(cdsgd_adamw_plan *plan, void *hip_stream);
  *                        elements (ld), and needs no more than its own type's alignment.
  * cdsgd_mxfp4_dequantize the values that a matrix stands for, rounded once if the type has not enough bits; out has rows
  *                        ld elements apart.
- * x and out have element type `dtype` (the values of cdsgd_grad_dtype).
+ * x and out have element type `dtype` (the values of cdsgd_grad_dtype); rows and cols are positive and below 2^31, ld at most 2^40
+ * (CDSGD_ERR_SIZE).
  */
 size_t cdsgd_mxfp4_code_bytes(size_t rows, size_t cols);
 size_t cdsgd_mxfp4_scale_bytes(size_t rows, size_t cols);
