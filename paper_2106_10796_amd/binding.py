@@ -60,6 +60,22 @@ class cdsgd_adamw_tensor(ctypes.Structure):
                 ("n", ctypes.c_size_t), ("weight_decay", ctypes.c_float)]
 
 
+class cdsgd_held(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("ld", ctypes.c_size_t), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class cdsgd_block_norm(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("stream_dtype", ctypes.c_int), ("rows", ctypes.c_size_t), ("cols", ctypes.c_size_t),
+                ("weight", ctypes.c_void_p), ("block_weight", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("scale", ctypes.c_double), ("eps", ctypes.c_double)]
+
+
+class cdsgd_attention(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("causal", ctypes.c_int), ("tokens_q", ctypes.c_size_t), ("tokens_k", ctypes.c_size_t),
+                ("num_seqs", ctypes.c_size_t), ("starts_q", ctypes.c_void_p), ("starts_k", ctypes.c_void_p), ("heads", ctypes.c_int),
+                ("kv_heads", ctypes.c_int), ("dim", ctypes.c_int), ("scale", ctypes.c_double)]
+
+
 class _Declines:
     """In the place of the native calls: every call declines."""
 
@@ -178,6 +194,7 @@ def lib():
         L.cdsgd_cost_period_mean.restype = i
         L.cdsgd_cost_period_mean.argtypes = [ctypes.POINTER(cdsgd_cost_params), ctypes.POINTER(cdsgd_cost)]
         _declare_ops(L)
+        _declare_block(L)
         _calls = _load_calls(L)
         _lib = L                       # last: another thread that sees it finds the calls bound
     return _lib
@@ -204,6 +221,28 @@ def _declare_ops(L):
             ("cdsgd_mxfp4_dequantize", i, [vp, vp, sz, sz, vp, i, sz, vp]),
             ("cdsgd_mxfp4_matmul_workspace", sz, [sz, sz, sz]),
             ("cdsgd_mxfp4_matmul", i, [vp, vp, vp, vp, sz, sz, sz, vp, i, sz, i, vp, sz, vp])):
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = restype, argtypes
+
+
+def _declare_block(L):
+    """The entry points of include/cdsgd_block.h."""
+    vp, sz, i = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
+    held, norm, batch = (ctypes.POINTER(t) for t in (cdsgd_held, cdsgd_block_norm, cdsgd_attention))
+    m = [vp, sz]                       # a matrix and its ld
+    for name, restype, argtypes in (
+            ("cdsgd_mxint8_code_bytes", sz, [sz, sz]),
+            ("cdsgd_mxint8_scale_bytes", sz, [sz, sz]),
+            ("cdsgd_mxint8_quantize", i, [vp, i, sz, sz, sz, vp, vp, vp]),
+            ("cdsgd_mxint8_dequantize", i, [vp, vp, sz, sz, vp, i, sz, vp]),
+            ("cdsgd_gated_forward", i, [i, i, sz, sz, *m * 3, vp, vp, vp, vp, vp]),
+            ("cdsgd_gated_backward", i, [i, i, sz, sz, *m, held, held, *m * 2, vp]),
+            ("cdsgd_block_norm_forward", i, [norm, *m * 4, vp, vp, vp, vp, vp, vp]),
+            ("cdsgd_block_norm_workspace", sz, [sz, sz]),
+            ("cdsgd_block_norm_backward", i, [norm, *m * 2, held, held, vp, *m * 2, vp, vp, vp, vp, sz, vp]),
+            ("cdsgd_attention_workspace", sz, [batch, i]),
+            ("cdsgd_attention_forward", i, [batch, *m * 4, vp, vp, sz, vp]),
+            ("cdsgd_attention_backward", i, [batch, *m * 5, vp, *m * 3, vp, sz, vp])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = restype, argtypes
 
@@ -833,3 +872,247 @@ def cdsgd_mxfp4_matmul(a, b, out, workspace=None, accumulate=False):
                                       _stream())
     if st != OK:
         _check(st, "cdsgd_mxfp4_matmul")
+
+
+# ---------------------------------------------------------------------------
+# include/cdsgd_block.h: attention, norms around a block, gated activations, activations in 8 bits
+# ---------------------------------------------------------------------------
+ACTS = {"silu": 0, "gelu_tanh": 1}   # cdsgd_act
+
+
+class Mxint8(NamedTuple):
+    """A matrix of `rows` by `cols` in 8 bits (the layout is in include/cdsgd_block.h): codes int8 [rows, 32 g] and scales uint8 [rows, g]
+    with g = ceil(cols / 32), contiguous CUDA tensors."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    rows: int
+    cols: int
+
+
+def new_mxint8(rows: int, cols: int, device="cuda") -> Mxint8:
+    """Room for a matrix; every byte of it is written by what saves into it."""
+    g = -(-cols // 32)
+    return Mxint8(torch.empty(rows, 32 * g, dtype=torch.int8, device=device), torch.empty(rows, g, dtype=torch.uint8, device=device), rows, cols)
+
+
+def _mx8(q, name, rows=None, cols=None, optional=False):
+    """The addresses of a matrix in 8 bits: (codes, scales); (None, None) for None where it is optional."""
+    if q is None and optional:
+        return None, None
+    if not isinstance(q, Mxint8):
+        raise TypeError("%s must be an Mxint8" % name)
+    if rows is not None and (q.rows, q.cols) != (rows, cols):
+        raise ValueError("%s is a matrix of %d by %d, expected %d by %d" % (name, q.rows, q.cols, rows, cols))
+    g = -(-q.cols // 32)
+    return _dev(q.codes, torch.int8, q.rows * 32 * g, name + ".codes"), _dev(q.scales, torch.uint8, q.rows * g, name + ".scales")
+
+
+def _rows_of(t, dtype, name, rows, cols, optional=False):
+    """(address, elements between two rows) of a matrix of that type; (None, 0) for None where it is optional."""
+    if t is None and optional:
+        return None, 0
+    p, kind, _, _, ld = _rows(t, name, rows, cols)
+    if kind != dtype:
+        raise TypeError("%s must have the type of the others" % name)
+    return p, ld
+
+
+def _held(x, dtype, name, rows, cols):
+    """A matrix that is read as it is or in 8 bits."""
+    if isinstance(x, Mxint8):
+        return cdsgd_held(None, 0, *_mx8(x, name, rows, cols))
+    return cdsgd_held(*_rows_of(x, dtype, name, rows, cols), None, None)
+
+
+def _on_this_device(*tensors):
+    """Calls work on the current device: that is where their tensors are."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if isinstance(t, Mxint8):
+            t = t.codes
+        if t is not None and t.device.index != here:
+            raise ValueError("a tensor is not on the current device")
+
+
+def cdsgd_mxint8_quantize(x, q):
+    """x [rows, cols] into q."""
+    p, dtype, r, c, ld = _rows(x, "x")
+    codes, scales = _mx8(q, "q", r, c)
+    _on_this_device(x, q)
+    _check(lib().cdsgd_mxint8_quantize(p, dtype, r, c, ld, codes, scales, _stream()), "cdsgd_mxint8_quantize")
+
+
+def cdsgd_mxint8_dequantize(q, out):
+    """The values that q stands for, into out [rows, cols]."""
+    codes, scales = _mx8(q, "q")
+    p, dtype, r, c, ld = _rows(out, "out", q.rows, q.cols)
+    _on_this_device(out, q)
+    _check(lib().cdsgd_mxint8_dequantize(codes, scales, r, c, p, dtype, ld, _stream()), "cdsgd_mxint8_dequantize")
+
+
+def _act(act):
+    if act not in ACTS:
+        raise ValueError("act must be one of %s" % ", ".join(sorted(ACTS)))
+    return ACTS[act]
+
+
+def cdsgd_gated_forward(a, u, y, a8=None, u8=None, act="silu"):
+    """y = act(a) * u, matrices of one type.  a8, u8 (Mxint8, both or none): a and u in 8 bits, for the backward pass."""
+    pa, dtype, r, c, ld_a = _rows(a, "a")
+    pu, ld_u = _rows_of(u, dtype, "u", r, c)
+    py, ld_y = _rows_of(y, dtype, "y", r, c)
+    saved = (*_mx8(a8, "a8", r, c, optional=True), *_mx8(u8, "u8", r, c, optional=True))
+    _on_this_device(a, u, y, a8, u8)
+    _check(lib().cdsgd_gated_forward(_act(act), dtype, r, c, pa, ld_a, pu, ld_u, py, ld_y, *saved, _stream()), "cdsgd_gated_forward")
+
+
+def cdsgd_gated_backward(dy, a, u, da, du, act="silu"):
+    """da and du from dy and from a and u: matrices, or Mxint8 as the forward pass saved them."""
+    p, dtype, r, c, ld = _rows(dy, "dy")
+    ha, hu = _held(a, dtype, "a", r, c), _held(u, dtype, "u", r, c)
+    pa, ld_a = _rows_of(da, dtype, "da", r, c)
+    pu, ld_u = _rows_of(du, dtype, "du", r, c)
+    _on_this_device(dy, a, u, da, du)
+    _check(lib().cdsgd_gated_backward(_act(act), dtype, r, c, p, ld, ctypes.byref(ha), ctypes.byref(hu), pa, ld_a, pu, ld_u, _stream()),
+           "cdsgd_gated_backward")
+
+
+def new_block_norm_workspace(rows: int, cols: int, device="cuda") -> torch.Tensor:
+    """Workspace for BlockNorm.backward on matrices of that size, or with fewer rows."""
+    return torch.empty(int(lib().cdsgd_block_norm_workspace(int(rows), int(cols))), dtype=torch.uint8, device=device)
+
+
+class BlockNorm:
+    """The end of one block and the beginning of the next: h_out = h + scale * gate * block_weight * normalised block,
+    y = weight * normalised h_out (include/cdsgd_block.h).  weight, block_weight and gate are float32 vectors, of which it keeps references; without
+    block_weight there is no norm after the block, without gate no gate."""
+
+    def __init__(self, weight, block_weight=None, gate=None, scale=1.0, eps=1e-6):
+        self.weight, self.block_weight, self.gate, self.scale, self.eps = weight, block_weight, gate, float(scale), float(eps)
+        self._cols = weight.numel()
+        self._at = [_dev(t, torch.float32, self._cols, name) for t, name in ((weight, "weight"), (block_weight, "block_weight"), (gate, "gate"))]
+
+    def _of(self, dtype, stream, rows, block):
+        weights = self._at if block else [self._at[0], None, None]
+        return cdsgd_block_norm(dtype, stream, rows, self._cols, *weights, self.scale, self.eps)
+
+    def _sizes(self, y, name, stream, stream_name):
+        """(address, type, rows, elements between two rows) of y, and the stream's type."""
+        p, dtype, r, c, ld = _rows(y, name)
+        if c != self._cols:
+            raise ValueError("%s has %d columns, expected %d" % (name, c, self._cols))
+        if not isinstance(stream, torch.Tensor) or stream.dtype not in GRAD_DTYPES:
+            raise TypeError("%s must be a CUDA matrix of float32, bfloat16 or float16" % stream_name)
+        return p, dtype, r, ld, GRAD_DTYPES[stream.dtype]
+
+    def forward(self, h, y, rstd, block=None, h_out=None, h8=None, block8=None):
+        """y (and, with a block's output, h_out) from h; rstd (float32 [2, rows]) receives the factors of both norms.  h8, block8 (Mxint8, optional):
+        h_out and block in 8 bits, for the backward pass.  Without a block y is the norm of h, and h8 is h in 8 bits."""
+        p, dtype, r, ld, stream = self._sizes(y, "y", h, "h")
+        c = self._cols
+        ph, ld_h = _rows_of(h, stream, "h", r, c)
+        pb, ld_b = _rows_of(block, dtype, "block", r, c, optional=True)
+        po, ld_o = _rows_of(h_out, stream, "h_out", r, c, optional=True)
+        saved = (*_mx8(h8, "h8", r, c, optional=True), *_mx8(block8, "block8", r, c, optional=True))
+        _on_this_device(h, y, rstd, block, h_out, h8, block8, self.weight, self.block_weight, self.gate)
+        of = self._of(dtype, stream, r, block is not None)
+        _check(lib().cdsgd_block_norm_forward(ctypes.byref(of), ph, ld_h, pb, ld_b, po, ld_o, p, ld, _dev(rstd, torch.float32, 2 * r, "rstd"),
+                                              *saved, _stream()), "cdsgd_block_norm_forward")
+
+    def backward(self, dy, h, rstd, dh, dweight, workspace, dh_out=None, block=None, dblock=None, dblock_weight=None, dgate=None):
+        """The gradients of h (dh), of the block's output (dblock) and of the weights, from those of y (dy) and of h_out (dh_out; None: 0), the
+        forward pass's rstd, and its h_out and block as they are or as Mxint8.  workspace: new_block_norm_workspace."""
+        p, dtype, r, ld, stream = self._sizes(dy, "dy", dh, "dh")
+        c = self._cols
+        pt, ld_t = _rows_of(dh_out, stream, "dh_out", r, c, optional=True)
+        ph, ld_h = _rows_of(dh, stream, "dh", r, c)
+        pb, ld_b = _rows_of(dblock, dtype, "dblock", r, c, optional=True)
+        held_h = _held(h, stream, "h", r, c)
+        held_b = cdsgd_held() if block is None else _held(block, dtype, "block", r, c)
+        _on_this_device(dy, h, rstd, dh, dweight, workspace, dh_out, block, dblock, dblock_weight, dgate, self.weight, self.block_weight, self.gate)
+        of = self._of(dtype, stream, r, block is not None)
+        _check(lib().cdsgd_block_norm_backward(
+            ctypes.byref(of), p, ld, pt, ld_t, ctypes.byref(held_h), ctypes.byref(held_b), _dev(rstd, torch.float32, 2 * r, "rstd"), ph, ld_h, pb, ld_b,
+            _dev(dweight, torch.float32, c, "dweight"), _dev(dblock_weight, torch.float32, c, "dblock_weight"),
+            _dev(dgate, torch.float32, c, "dgate"), _dev(workspace, torch.uint8, None, "workspace"),
+            workspace.numel() if workspace is not None else 0, _stream()), "cdsgd_block_norm_backward")
+
+
+ATTENTION_DTYPES = {torch.bfloat16: 1, torch.float16: 2}
+
+
+def _heads(t, name, dtype=None, shape=None):
+    """(address, elements between two tokens) of [tokens, heads, dim] with a token's heads in a row."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in ATTENTION_DTYPES):
+        raise TypeError("%s must be a CUDA tensor [tokens, heads, dim] of bfloat16 or float16" % name)
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError("%s must have the type of the others" % name)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    n, h, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d) or (n > 1 and t.stride(0) < h * d):
+        raise TypeError("the heads of a token of %s must lie in a row, and tokens must not overlap" % name)
+    return t.data_ptr(), t.stride(0) if n > 1 else h * d
+
+
+def _starts(t, name, seqs=None):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.numel() >= 2):
+        raise TypeError("%s must be a contiguous CUDA vector of int32 with an entry more than there are sequences" % name)
+    if seqs is not None and t.numel() != seqs + 1:
+        raise ValueError("%s has %d entries, expected %d" % (name, t.numel(), seqs + 1))
+    return t.data_ptr()
+
+
+def _batch(q, k, starts, starts_k, causal, scale):
+    if starts is None and starts_k is not None:
+        raise ValueError("starts_k without starts")
+    if q.shape[2] != k.shape[2]:
+        raise ValueError("q and k have heads of %d and of %d elements" % (q.shape[2], k.shape[2]))
+    seqs = 1 if starts is None else starts.numel() - 1
+    return cdsgd_attention(ATTENTION_DTYPES[q.dtype], int(bool(causal)), q.shape[0], k.shape[0], seqs,
+                           None if starts is None else _starts(starts, "starts"), None if starts_k is None else _starts(starts_k, "starts_k", seqs),
+                           q.shape[1], k.shape[1], q.shape[2], float(q.shape[2]) ** -0.5 if scale is None else float(scale))
+
+
+def new_attention_workspace(q, k, seqs=1, train=False):
+    """Workspace for attention on q and k in `seqs` sequences, of the forward pass and with `train` of the backward pass too: a uint8 tensor, or
+    None where none is needed."""
+    _heads(q, "q")
+    _heads(k, "k", q.dtype)
+    b = _batch(q, k, None, None, True, None)
+    b.num_seqs = int(seqs)
+    if seqs != 1:                        # (the addresses of the starts do not matter, but that there are some)
+        b.starts_q = 16
+    need = max(int(lib().cdsgd_attention_workspace(ctypes.byref(b), i)) for i in range(2 if train else 1))
+    return torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+
+
+def cdsgd_attention_forward(q, k, v, out, lse=None, starts=None, starts_k=None, causal=True, scale=None, workspace=None):
+    """out = softmax(scale q k^T) v over a packed batch: q, out [tokens, heads, dim], k, v [tokens, kv_heads, dim], bfloat16 or float16.
+    starts, starts_k (int32 [sequences + 1] on the GPU): where the sequences' queries and keys begin and end; None: one sequence, or the same for both.
+    lse (float32 [heads, tokens], optional): for the backward pass.  scale: None is dim ** -0.5.  workspace: new_attention_workspace."""
+    pq, ld_q = _heads(q, "q")
+    pk, ld_k = _heads(k, "k", q.dtype)
+    pv, ld_v = _heads(v, "v", q.dtype, k.shape)
+    po, ld_o = _heads(out, "out", q.dtype, q.shape)
+    b = _batch(q, k, starts, starts_k, causal, scale)
+    _on_this_device(q, k, v, out, lse, starts, starts_k, workspace)
+    _check(lib().cdsgd_attention_forward(ctypes.byref(b), pq, ld_q, pk, ld_k, pv, ld_v, po, ld_o,
+                                         _dev(lse, torch.float32, q.shape[0] * q.shape[1], "lse"), _dev(workspace, torch.uint8, None, "workspace"),
+                                         workspace.numel() if workspace is not None else 0, _stream()), "cdsgd_attention_forward")
+
+
+def cdsgd_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, starts=None, starts_k=None, causal=True, scale=None, workspace=None):
+    """dq, dk and dv from dout, the inputs, and the forward pass's out and lse.  workspace: new_attention_workspace with train."""
+    pq, ld_q = _heads(q, "q")
+    pk, ld_k = _heads(k, "k", q.dtype)
+    at = []
+    for t, name, like in ((v, "v", k), (out, "out", q), (dout, "dout", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k)):
+        at.append(_heads(t, name, q.dtype, like.shape))
+    (pv, ld_v), (po, ld_o), (pd, ld_d), (pdq, ld_dq), (pdk, ld_dk), (pdv, ld_dv) = at
+    b = _batch(q, k, starts, starts_k, causal, scale)
+    _on_this_device(q, k, v, out, lse, dout, dq, dk, dv, starts, starts_k, workspace)
+    _check(lib().cdsgd_attention_backward(ctypes.byref(b), pd, ld_d, pq, ld_q, pk, ld_k, pv, ld_v, po, ld_o,
+                                          _dev(lse, torch.float32, q.shape[0] * q.shape[1], "lse"), pdq, ld_dq, pdk, ld_dk, pdv, ld_dv,
+                                          _dev(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0,
+                                          _stream()), "cdsgd_attention_backward")

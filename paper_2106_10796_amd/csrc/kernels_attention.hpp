@@ -1,0 +1,588 @@
+// Attention over packed sequences (include/cdsgd_block.h), forward and backward.
+//
+// The heads that share a key head are rows of one matrix: row i of a sequence is query i / G under head i % G of the group's G, so that a
+// tile of keys and values serves all of them, and a single query's heads share its instructions.  A wave takes 32 rows (or, for the gradients of
+// keys and values, 32 keys) and keeps what belongs to them in registers; what it runs over goes through LDS, a tile at a time.
+//
+// Matrix instructions (32 x 32 x 16): lane l holds of the first operand row l % 32, of the second column l % 32, elements 8 (l / 32) ... + 7 of
+// the axis that is summed over, and of the result rows 8 (r / 4) + 4 (l / 32) + r % 4, r = 0 ... 15, of column l % 32.  Products are taken so that a
+// lane's results are already its elements of the next product's second operand: S^T = K Q^T has a query in every lane (the sum and the largest
+// of its row need one exchange between two lanes), and the sum over keys in O^T = V^T P^T may run in any order, as long as both operands
+// have the same one: slot e of lane l / 32 = h is key 4 h + e, or 4 + 4 h + e from e = 4 on, which is where S^T left it.  V^T comes from LDS by the
+// reads that transpose: four lanes' 8 bytes of four rows each become four rows' elements of one column.
+#pragma once
+
+#include "device_matrix.hpp"
+
+namespace {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef short s8v __attribute__((ext_vector_type(8)));
+
+#define CDSGD_LDS __attribute__((address_space(3)))
+
+constexpr float kLog2e = 1.44269504088896f;
+constexpr float kInfinity = __builtin_inff();
+constexpr unsigned kRecords = 0x40000000u, kOutside = 0x7FFFFFF0u;  // of a buffer; a place behind every buffer's end, which loads 0
+
+// Probabilities of fp16 tensors are operands of the second products times 2^15, the largest power of two that 1 can be multiplied with there: numbers
+// below 2^-14 lose bits in fp16, and a row of 2^14 keys has no others.
+template <int DT>
+constexpr float kLift = DT == kGradF16 ? 15.0f : 0.0f;
+template <int DT>
+constexpr float kLifted = DT == kGradF16 ? 32768.0f : 1.0f;
+
+constexpr unsigned kTileRows = 128;  // rows of a group of the forward pass and of dq, and keys of a group of dk and dv
+constexpr unsigned kTileKeys = 64;   // what a group takes at a time of the other side
+
+template <int DT>
+__device__ __forceinline__ f16v mfma(s8v a, s8v b, f16v c)
+{
+    if constexpr (DT == kGradBF16) {
+        typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+    } else {
+        typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+    }
+}
+
+// The row of a result's element r.
+__device__ __forceinline__ constexpr unsigned row_of(unsigned r, unsigned half) { return 8u * (r / 4u) + 4u * half + r % 4u; }
+
+struct AttentionSizes {
+    unsigned tokens_q, tokens_k, num_seqs, kv_heads, group, dim;
+    const int *starts_q, *starts_k;
+    int causal;
+    float scale;
+};
+
+template <typename T>
+struct Heads {
+    T *p;
+    unsigned ld;  // elements from one token to the next
+};
+
+// A sequence, cut to the tensors: its first rows and its lengths.
+struct Sequence {
+    unsigned q0, queries, k0, keys;
+};
+
+__device__ __forceinline__ unsigned cut(int at, unsigned from, unsigned to)
+{
+    const unsigned a = at < 0 ? 0u : (unsigned)at;
+    return a < from ? from : a > to ? to : a;
+}
+
+__device__ __forceinline__ Sequence sequence_of(const AttentionSizes &z, unsigned s)
+{
+    Sequence x = {0u, z.tokens_q, 0u, z.tokens_k};
+    if (z.starts_q) {
+        x.q0 = cut(z.starts_q[s], 0u, z.tokens_q);
+        x.queries = cut(z.starts_q[s + 1u], x.q0, z.tokens_q) - x.q0;
+        const int *k = z.starts_k ? z.starts_k : z.starts_q;
+        x.k0 = cut(k[s], 0u, z.tokens_k);
+        x.keys = cut(k[s + 1u], x.k0, z.tokens_k) - x.k0;
+    }
+    return x;
+}
+
+// Tiles of a packed batch are numbered without a table: sequence s, whose rows are `each` for one of its tokens, begins at number
+// starts[s] * each / tile + s, which leaves it a number for each of its tiles and at most one too many.  The search takes 64 sequences a step.
+struct Tile {
+    unsigned seq;
+    unsigned long long at;  // in its sequence
+};
+__device__ __forceinline__ Tile tile_of(const int *starts, unsigned tokens, unsigned num_seqs, unsigned each, unsigned tile, unsigned long long number)
+{
+    if (!starts) return {0u, number * tile};
+    const auto first = [&](unsigned s) { return (unsigned long long)cut(starts[s], 0u, tokens) * each / tile + s; };
+    unsigned lo = 0, left = num_seqs;
+    while (left > 1u) {
+        const unsigned step = (left + 63u) / 64u, s = lo + threadIdx.x % 64u * step;
+        const bool there = threadIdx.x % 64u * step < left && first(s < num_seqs ? s : 0u) <= number;
+        const unsigned before = (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(there));
+        lo += (before ? before - 1u : 0u) * step;
+        left = step < num_seqs - lo ? step : num_seqs - lo;
+        if (step == 1u) break;
+    }
+    lo = (unsigned)__builtin_amdgcn_readfirstlane((int)lo);
+    const unsigned long long begin = first(lo);
+    return {lo, number < begin ? ~0ull : (number - begin) * tile};
+}
+
+__device__ __forceinline__ unsigned long long tiles_over(unsigned tokens, unsigned num_seqs, unsigned each, unsigned tile)
+{
+    return (unsigned long long)tokens * each / tile + num_seqs;
+}
+
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(T *p)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)kRecords, kBufferFlags);
+}
+
+__device__ __forceinline__ s8v load16(__amdgpu_buffer_rsrc_t from, unsigned bytes)
+{
+    typedef unsigned u4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(s8v, (u4)__builtin_amdgcn_raw_buffer_load_b128(from, (int)bytes, 0, 0));
+}
+
+// Byte offset of elements d ... of row `row` (of `rows`) behind the tile's first token.
+__device__ __forceinline__ unsigned row_offset(unsigned row, unsigned rows, unsigned group, unsigned ld, unsigned d, unsigned dim)
+{
+    return row < rows && d < dim ? (row / group * ld + row % group * dim + d) * 2u : kOutside;
+}
+
+// ---------------------------------------------------------------------------
+// tiles in LDS: rows of DP elements, in chunks of 16 bytes, turned so that neither sixteen rows' reads of one chunk nor the
+// transposing reads of four chunks of four rows meet in a bank
+// ---------------------------------------------------------------------------
+template <int DP>
+__device__ __forceinline__ unsigned turned(unsigned row, unsigned chunk)
+{
+    if constexpr (DP == 128) return chunk ^ ((row & 3u) << 2 | (row >> 2 & 3u));
+    else return chunk ^ ((row >> 1 & 1u) << 2 | (row >> 2 & 3u));
+}
+
+template <int DP>
+__device__ __forceinline__ unsigned lds_chunk(unsigned row, unsigned chunk) { return row * (DP * 2u) + turned<DP>(row, chunk) * 16u; }
+
+// Row l % 32 (from `row0` on), elements 16 k + 8 (l / 32) ... + 7: a first operand.
+template <int DP>
+__device__ __forceinline__ s8v rows_operand(const unsigned char *tile, unsigned row0, unsigned k)
+{
+    const unsigned l = threadIdx.x % 64u;
+    return *reinterpret_cast<const s8v *>(__builtin_assume_aligned(tile + lds_chunk<DP>(row0 + l % 32u, 2u * k + l / 32u), 16));
+}
+
+// Column 32 d + l % 32 of rows row0 + 4 (l / 32) ... + 3 and row0 + 8 + 4 (l / 32) ... + 3: a first operand, transposed.
+template <int DP>
+__device__ __forceinline__ s8v columns_operand(const unsigned char *tile, unsigned row0, unsigned d)
+{
+    const unsigned l = threadIdx.x % 64u, row = row0 + 4u * (l / 32u) + l % 16u / 4u, at = 32u * d + 16u * (l / 16u % 2u) + 4u * (l % 4u);
+    const unsigned in = at % 8u * 2u;
+    typedef s4v CDSGD_LDS *Four;
+    const s4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(tile + lds_chunk<DP>(row, at / 8u) + in));
+    const s4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(tile + lds_chunk<DP>(row + 8u, at / 8u) + in));
+    return s8v{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+}
+
+// A tile of ROWS rows on its way to LDS, by 256 lanes.
+template <int DP, int ROWS>
+struct Staged {
+    static constexpr unsigned kChunks = DP / 8, kLoads = ROWS * kChunks / 256;
+    s8v v[kLoads];
+
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, unsigned rows, unsigned group, unsigned ld, unsigned dim)
+    {
+#pragma unroll
+        for (unsigned i = 0; i < kLoads; ++i) {
+            const unsigned at = i * 256u + threadIdx.x;
+            v[i] = load16(from, row_offset(at / kChunks, rows, group, ld, at % kChunks * 8u, dim));
+        }
+    }
+    __device__ __forceinline__ void store(unsigned char *tile) const
+    {
+#pragma unroll
+        for (unsigned i = 0; i < kLoads; ++i) {
+            const unsigned at = i * 256u + threadIdx.x;
+            *reinterpret_cast<s8v *>(__builtin_assume_aligned(tile + lds_chunk<DP>(at / kChunks, at % kChunks), 16)) = v[i];
+        }
+    }
+};
+
+// Of the 32 rows of a result, 16 from 16 t on, rounded: a second operand.
+template <int DT>
+__device__ __forceinline__ s8v rounded(const f16v &x, unsigned t)
+{
+    Elem<DT> e[8];
+#pragma unroll
+    for (unsigned i = 0; i < 8; ++i) e[i] = (Elem<DT>)x[8 * t + i];
+    return __builtin_bit_cast(s8v, e);
+}
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// A row's results, which lie in two lanes four elements at a time, times f and rounded.
+template <int DT, int DP>
+__device__ __forceinline__ void store_row(Elem<DT> *row, const f16v (&acc)[DP / 32], float f, unsigned dim)
+{
+    typedef Elem<DT> e4 __attribute__((ext_vector_type(4)));
+    const unsigned half = threadIdx.x % 64u / 32u;
+#pragma unroll
+    for (unsigned d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (unsigned q = 0; q < 4; ++q) {
+            const unsigned at = 32u * d + 8u * q + 4u * half;
+            if (at < dim)
+                *reinterpret_cast<e4 *>(__builtin_assume_aligned(row + at, 8)) =
+                    e4{(Elem<DT>)(acc[d][4 * q] * f), (Elem<DT>)(acc[d][4 * q + 1] * f), (Elem<DT>)(acc[d][4 * q + 2] * f), (Elem<DT>)(acc[d][4 * q + 3] * f)};
+        }
+}
+
+// ---------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------
+// parts, part_lse: where several groups share a row's keys (`splits`), each leaves its own result, [splits][row of all][DP] in fp32 and
+// [splits][row of all]; rows of all are numbered [kv head][query][head of the group].
+template <int DT, int DP>
+__global__ __launch_bounds__(256) void k_attention_forward(AttentionSizes z, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k, Heads<const Elem<DT>> v,
+                                                           Heads<Elem<DT>> out, float *__restrict__ lse, unsigned splits, float *__restrict__ parts,
+                                                           float *__restrict__ part_lse)
+{
+    __shared__ __align__(1024) unsigned char tile_k[kTileKeys * DP * 2], tile_v[kTileKeys * DP * 2];
+    const unsigned kv = blockIdx.x % z.kv_heads, split = blockIdx.x / z.kv_heads % splits;
+    // (the last tiles of a sequence see the most keys: they go first)
+    const Tile t = tile_of(z.starts_q, z.tokens_q, z.num_seqs, z.group, kTileRows,
+                           tiles_over(z.tokens_q, z.num_seqs, z.group, kTileRows) - 1u - blockIdx.x / z.kv_heads / splits);
+    const Sequence s = sequence_of(z, t.seq);
+    const unsigned long long all_rows = (unsigned long long)s.queries * z.group;
+    if (t.at >= all_rows) return;
+    const unsigned first_query = (unsigned)(t.at / z.group), skip = (unsigned)(t.at % z.group);  // the tile's rows begin `skip` rows into its first query's
+    const unsigned rows = all_rows - t.at < kTileRows ? (unsigned)(all_rows - t.at) : kTileRows;
+    const unsigned wave = threadIdx.x / 64u, l = threadIdx.x % 64u, half = l / 32u, row = wave * 32u + l % 32u;
+    const long long hidden_from = (long long)s.keys - s.queries + 1;  // query i sees keys below i + this
+
+    const unsigned head0 = kv * z.group;
+    const __amdgpu_buffer_rsrc_t from_q = buffer_at(q.p + (size_t)(s.q0 + first_query) * q.ld + head0 * z.dim);
+    s8v bq[DP / 16];
+#pragma unroll
+    for (unsigned i = 0; i < DP / 16; ++i) bq[i] = load16(from_q, row_offset(skip + row, skip + rows, z.group, q.ld, 16u * i + 8u * half, z.dim));
+
+    // keys that a row sees, that all of the tile's together see, and that each of the wave's sees
+    const auto seen = [&](unsigned r) -> unsigned {
+        if (!z.causal) return s.keys;
+        const long long n = (long long)(first_query + (skip + r) / z.group) + hidden_from;
+        return n < 0 ? 0u : n < (long long)s.keys ? (unsigned)n : s.keys;
+    };
+    const unsigned mine = row < rows ? seen(row) : 0u, all = seen(rows - 1u), least = (unsigned)__builtin_amdgcn_readfirstlane((int)seen(wave * 32u));
+    unsigned from = 0, to = all;
+    if (splits > 1u) {
+        const unsigned tiles = (s.keys + kTileKeys - 1u) / kTileKeys, each = (tiles + splits - 1u) / splits * kTileKeys;
+        from = split * each < to ? split * each : to;
+        to = to - from < each ? to : from + each;
+    }
+
+    f16v acc[DP / 32] = {};
+    float most = -kInfinity, total = 0.0f;
+    const float c = z.scale * kLog2e;
+    Staged<DP, kTileKeys> sk, sv;
+    const auto ask = [&](unsigned j) {
+        const unsigned left = s.keys - j;
+        sk.load(buffer_at(k.p + (size_t)(s.k0 + j) * k.ld + kv * z.dim), left, 1u, k.ld, z.dim);
+        sv.load(buffer_at(v.p + (size_t)(s.k0 + j) * v.ld + kv * z.dim), left, 1u, v.ld, z.dim);
+    };
+    if (from < to) ask(from);
+    for (unsigned j = from; j < to; j += kTileKeys) {
+        __syncthreads();
+        sk.store(tile_k);
+        sv.store(tile_v);
+        __syncthreads();
+        if (j + kTileKeys < to) ask(j + kTileKeys);
+        if (wave * 32u >= rows) continue;
+        f16v x[2] = {};
+#pragma unroll
+        for (unsigned b = 0; b < 2; ++b)
+#pragma unroll
+            for (unsigned i = 0; i < DP / 16; ++i) x[b] = mfma<DT>(rows_operand<DP>(tile_k, 32u * b, i), bq[i], x[b]);
+        if (j + kTileKeys > least) {
+#pragma unroll
+            for (unsigned b = 0; b < 2; ++b)
+#pragma unroll
+                for (unsigned r = 0; r < 16; ++r)
+                    if (j + 32u * b + row_of(r, half) >= mine) x[b][r] = -kInfinity;
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (unsigned r = 1; r < 32; ++r) top = __builtin_fmaxf(top, x[r / 16][r % 16]);
+        top = __builtin_fmaxf(top, other_half(top));
+        // (differences first: of logits far from 0 the product with c would lose more than what is left)
+        const float now = __builtin_fmaxf(most, top), base = now == -kInfinity ? 0.0f : now;
+        const float keep = __builtin_amdgcn_exp2f((most - base) * c);
+        most = now;
+        float sum = 0.0f;
+#pragma unroll
+        for (unsigned b = 0; b < 2; ++b)
+#pragma unroll
+            for (unsigned r = 0; r < 16; ++r) {
+                x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r] - base, c, kLift<DT>));
+                sum += x[b][r];
+            }
+        total = __builtin_fmaf(total, keep, sum);
+#pragma unroll
+        for (unsigned d = 0; d < DP / 32; ++d) acc[d] *= keep;
+#pragma unroll
+        for (unsigned b = 0; b < 2; ++b)
+#pragma unroll
+            for (unsigned h = 0; h < 2; ++h) {
+                const s8v p = rounded<DT>(x[b], h);
+#pragma unroll
+                for (unsigned d = 0; d < DP / 32; ++d) acc[d] = mfma<DT>(columns_operand<DP>(tile_v, 32u * b + 16u * h, d), p, acc[d]);
+            }
+    }
+    total += other_half(total);
+    if (row >= rows) return;
+    const unsigned query = first_query + (skip + row) / z.group, head = head0 + (skip + row) % z.group;
+    const float f = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total, log_sum = total == 0.0f ? -kInfinity : most * z.scale + __builtin_logf(total * (1.0f / kLifted<DT>));
+    if (splits > 1u) {
+        const size_t at = (((size_t)split * z.kv_heads + kv) * z.tokens_q + s.q0 + query) * z.group + head - head0;
+        store_row<kGradF32, DP>(parts + at * DP, acc, f, DP);
+        if (half == 0u) part_lse[at] = log_sum;
+    } else {
+        store_row<DT, DP>(out.p + (size_t)(s.q0 + query) * out.ld + head * z.dim, acc, f, z.dim);
+        if (lse && half == 0u) lse[(size_t)head * z.tokens_q + s.q0 + query] = log_sum;
+    }
+}
+
+// A row's parts, joined: a wave to a row.
+template <int DT, int DP>
+__global__ __launch_bounds__(256) void k_attention_join(AttentionSizes z, Heads<Elem<DT>> out, float *__restrict__ lse, unsigned splits,
+                                                        const float *__restrict__ parts, const float *__restrict__ part_lse)
+{
+    const size_t rows = (size_t)z.kv_heads * z.tokens_q * z.group, row = (size_t)blockIdx.x * 4u + threadIdx.x / 64u;
+    if (row >= rows) return;
+    const unsigned lane = threadIdx.x % 64u, query = (unsigned)(row / z.group % z.tokens_q);
+    const unsigned head = (unsigned)(row / z.group / z.tokens_q) * z.group + (unsigned)(row % z.group);
+    if (z.starts_q && (query < cut(z.starts_q[0], 0u, z.tokens_q) || query >= cut(z.starts_q[z.num_seqs], 0u, z.tokens_q))) return;
+    float most = -kInfinity;
+    for (unsigned i = 0; i < splits; ++i) most = __builtin_fmaxf(most, part_lse[i * rows + row]);
+    const float base = most == -kInfinity ? 0.0f : most;
+    float total = 0.0f, sum[DP / 64] = {};
+    for (unsigned i = 0; i < splits; ++i) {
+        const float w = __builtin_amdgcn_exp2f((part_lse[i * rows + row] - base) * kLog2e);
+        total += w;
+#pragma unroll
+        for (unsigned k = 0; k < DP / 64; ++k) sum[k] = __builtin_fmaf(w, parts[(i * rows + row) * DP + k * 64u + lane], sum[k]);
+    }
+    const float f = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+#pragma unroll
+    for (unsigned k = 0; k < DP / 64; ++k)
+        if (k * 64u + lane < z.dim) out.p[(size_t)query * out.ld + head * z.dim + k * 64u + lane] = (Elem<DT>)(sum[k] * f);
+    if (lse && lane == 0u) lse[(size_t)head * z.tokens_q + query] = total == 0.0f ? -kInfinity : base + __builtin_logf(total);
+}
+
+// ---------------------------------------------------------------------------
+// backward
+// ---------------------------------------------------------------------------
+// A power of two that brings numbers up to `most` to about 1 (1 where most is 0 or not finite).
+__device__ __forceinline__ float to_one(float most)
+{
+    const unsigned e = __builtin_bit_cast(unsigned, most) >> 23 & 0xFFu;
+    return e == 0u || e > 253u ? 1.0f : __builtin_bit_cast(float, (254u - e) << 23);
+}
+
+// dq.  delta receives dout . out of every row, and size (of fp16 tensors) the largest magnitude in dout, both [heads][tokens_q].
+template <int DT, int DP>
+__global__ __launch_bounds__(256) void k_attention_dq(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
+                                                      Heads<const Elem<DT>> v, Heads<const Elem<DT>> out, const float *__restrict__ lse,
+                                                      Heads<Elem<DT>> dq, float *__restrict__ delta, float *__restrict__ size)
+{
+    __shared__ __align__(1024) unsigned char tile_k[kTileKeys * DP * 2], tile_v[kTileKeys * DP * 2];
+    const unsigned kv = blockIdx.x % z.kv_heads;
+    const Tile t = tile_of(z.starts_q, z.tokens_q, z.num_seqs, z.group, kTileRows,
+                           tiles_over(z.tokens_q, z.num_seqs, z.group, kTileRows) - 1u - blockIdx.x / z.kv_heads);
+    const Sequence s = sequence_of(z, t.seq);
+    const unsigned long long all_rows = (unsigned long long)s.queries * z.group;
+    if (t.at >= all_rows) return;
+    const unsigned first_query = (unsigned)(t.at / z.group), skip = (unsigned)(t.at % z.group);
+    const unsigned rows = all_rows - t.at < kTileRows ? (unsigned)(all_rows - t.at) : kTileRows;
+    const unsigned wave = threadIdx.x / 64u, l = threadIdx.x % 64u, half = l / 32u, row = wave * 32u + l % 32u;
+    const long long hidden_from = (long long)s.keys - s.queries + 1;
+    const unsigned head0 = kv * z.group, query = first_query + (skip + row) / z.group, head = head0 + (skip + row) % z.group;
+    const size_t token = s.q0 + first_query, at = (size_t)head * z.tokens_q + s.q0 + query;
+
+    const __amdgpu_buffer_rsrc_t from_q = buffer_at(q.p + token * q.ld + head0 * z.dim);
+    const __amdgpu_buffer_rsrc_t from_d = buffer_at(dout.p + token * dout.ld + head0 * z.dim);
+    const __amdgpu_buffer_rsrc_t from_o = buffer_at(out.p + token * out.ld + head0 * z.dim);
+    s8v bq[DP / 16], bd[DP / 16];
+    float sum = 0.0f, largest = 0.0f;
+#pragma unroll
+    for (unsigned i = 0; i < DP / 16; ++i) {
+        typedef Elem<DT> e8 __attribute__((ext_vector_type(8)));
+        const unsigned d = 16u * i + 8u * half;
+        bq[i] = load16(from_q, row_offset(skip + row, skip + rows, z.group, q.ld, d, z.dim));
+        bd[i] = load16(from_d, row_offset(skip + row, skip + rows, z.group, dout.ld, d, z.dim));
+        const e8 o = __builtin_bit_cast(e8, load16(from_o, row_offset(skip + row, skip + rows, z.group, out.ld, d, z.dim)));
+        const e8 g = __builtin_bit_cast(e8, bd[i]);
+#pragma unroll
+        for (unsigned e = 0; e < 8; ++e) {
+            sum = __builtin_fmaf((float)g[e], (float)o[e], sum);
+            largest = __builtin_fmaxf(largest, __builtin_fabsf((float)g[e]));
+        }
+    }
+    sum += other_half(sum);
+    largest = __builtin_fmaxf(largest, other_half(largest));
+    // (a row that sees nothing, and one that is not there, has no share in anything)
+    const float log_sum = row < rows ? lse[at] : kInfinity, base = log_sum == -kInfinity ? kInfinity : log_sum * kLog2e;
+    const float up = DT == kGradF16 ? to_one(largest) : 1.0f;
+    if (row < rows && half == 0u) {
+        delta[at] = sum;
+        if (DT == kGradF16) size[at] = largest;
+    }
+
+    const auto seen = [&](unsigned r) -> unsigned {
+        if (!z.causal) return s.keys;
+        const long long n = (long long)(first_query + (skip + r) / z.group) + hidden_from;
+        return n < 0 ? 0u : n < (long long)s.keys ? (unsigned)n : s.keys;
+    };
+    const unsigned mine = row < rows ? seen(row) : 0u, to = seen(rows - 1u), least = (unsigned)__builtin_amdgcn_readfirstlane((int)seen(wave * 32u));
+    f16v acc[DP / 32] = {};
+    const float c = z.scale * kLog2e;
+    Staged<DP, kTileKeys> sk, sv;
+    const auto ask = [&](unsigned j) {
+        const unsigned left = s.keys - j;
+        sk.load(buffer_at(k.p + (size_t)(s.k0 + j) * k.ld + kv * z.dim), left, 1u, k.ld, z.dim);
+        sv.load(buffer_at(v.p + (size_t)(s.k0 + j) * v.ld + kv * z.dim), left, 1u, v.ld, z.dim);
+    };
+    if (to) ask(0);
+    for (unsigned j = 0; j < to; j += kTileKeys) {
+        __syncthreads();
+        sk.store(tile_k);
+        sv.store(tile_v);
+        __syncthreads();
+        if (j + kTileKeys < to) ask(j + kTileKeys);
+        if (wave * 32u >= rows) continue;
+#pragma unroll
+        for (unsigned b = 0; b < 2; ++b) {
+            f16v x = {}, y = {};
+#pragma unroll
+            for (unsigned i = 0; i < DP / 16; ++i) x = mfma<DT>(rows_operand<DP>(tile_k, 32u * b, i), bq[i], x);
+#pragma unroll
+            for (unsigned i = 0; i < DP / 16; ++i) y = mfma<DT>(rows_operand<DP>(tile_v, 32u * b, i), bd[i], y);
+#pragma unroll
+            for (unsigned r = 0; r < 16; ++r) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -base));
+                y[r] = j + kTileKeys > least && j + 32u * b + row_of(r, half) >= mine ? 0.0f : p * ((y[r] - sum) * up);
+            }
+#pragma unroll
+            for (unsigned h = 0; h < 2; ++h) {
+                const s8v ds = rounded<DT>(y, h);
+#pragma unroll
+                for (unsigned d = 0; d < DP / 32; ++d) acc[d] = mfma<DT>(columns_operand<DP>(tile_k, 32u * b + 16u * h, d), ds, acc[d]);
+            }
+        }
+    }
+    if (row < rows) store_row<DT, DP>(dq.p + (size_t)(s.q0 + query) * dq.ld + head * z.dim, acc, z.scale / up, z.dim);
+}
+
+// dk and dv: a group takes 128 keys of one key head, and runs over the rows that see them.
+template <int DT, int DP>
+__global__ __launch_bounds__(256) void k_attention_dkv(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
+                                                       Heads<const Elem<DT>> v, const float *__restrict__ lse, const float *__restrict__ delta,
+                                                       const float *__restrict__ size, Heads<Elem<DT>> dk, Heads<Elem<DT>> dv)
+{
+    constexpr unsigned kRows = kTileKeys;  // of queries at a time
+    __shared__ __align__(1024) unsigned char tile_q[kRows * DP * 2], tile_d[kRows * DP * 2];
+    __shared__ __align__(16) float row_lse[kRows], row_delta[kRows], row_size[kRows];
+    const unsigned kv = blockIdx.x % z.kv_heads;
+    const int *starts = z.starts_k ? z.starts_k : z.starts_q;
+    const Tile t = tile_of(starts, z.tokens_k, z.num_seqs, 1u, kTileRows, blockIdx.x / z.kv_heads);
+    const Sequence s = sequence_of(z, t.seq);
+    if (t.at >= s.keys) return;
+    const unsigned key0 = (unsigned)t.at, keys = s.keys - key0 < kTileRows ? s.keys - key0 : kTileRows;
+    const unsigned wave = threadIdx.x / 64u, l = threadIdx.x % 64u, half = l / 32u, key = wave * 32u + l % 32u, head0 = kv * z.group;
+
+    const __amdgpu_buffer_rsrc_t from_k = buffer_at(k.p + (size_t)(s.k0 + key0) * k.ld + kv * z.dim);
+    const __amdgpu_buffer_rsrc_t from_v = buffer_at(v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim);
+    s8v bk[DP / 16], bv[DP / 16];
+#pragma unroll
+    for (unsigned i = 0; i < DP / 16; ++i) {
+        bk[i] = load16(from_k, row_offset(key, keys, 1u, k.ld, 16u * i + 8u * half, z.dim));
+        bv[i] = load16(from_v, row_offset(key, keys, 1u, v.ld, 16u * i + 8u * half, z.dim));
+    }
+    // the first query that sees key j is j - (keys - queries)
+    const long long later = (long long)s.queries - s.keys;
+    const auto first_of = [&](unsigned j) -> unsigned {
+        const long long i = (long long)j + later;
+        return !z.causal || i < 0 ? 0u : i < (long long)s.queries ? (unsigned)i : s.queries;
+    };
+    f16v acc_k[DP / 32] = {}, acc_v[DP / 32] = {};
+    const float c = z.scale * kLog2e;
+    float up = 1.0f;
+    bool begun = false;
+    // queries at a time: as many as have kRows rows at most, or a part of one query's heads
+    const unsigned group = z.group, at_once = group < kRows ? kRows / group : 1u;
+    Staged<DP, kRows> sq, sd;
+    float next_lse = 0.0f, next_delta = 0.0f, next_size = 0.0f;
+    const auto ask = [&](unsigned i, unsigned part) {
+        const unsigned queries = s.queries - i < at_once ? s.queries - i : at_once, left = group - part < kRows ? group - part : kRows;
+        const unsigned rows = group < kRows ? queries * group : left;
+        sq.load(buffer_at(q.p + (size_t)(s.q0 + i) * q.ld + (head0 + part) * z.dim), rows, group, q.ld, z.dim);
+        sd.load(buffer_at(dout.p + (size_t)(s.q0 + i) * dout.ld + (head0 + part) * z.dim), rows, group, dout.ld, z.dim);
+        if (threadIdx.x < kRows) {
+            const unsigned r = threadIdx.x;
+            const size_t at = (size_t)(head0 + part + r % group) * z.tokens_q + s.q0 + i + r / group;
+            const float x = r < rows ? lse[at] : kInfinity;
+            next_lse = x == -kInfinity ? kInfinity : x * kLog2e - kLift<DT>;
+            next_delta = r < rows ? delta[at] : 0.0f;
+            next_size = DT == kGradF16 && r < rows ? size[at] : 0.0f;
+        }
+    };
+    unsigned i = first_of(key0), part = 0;
+    if (i < s.queries) ask(i, part);
+    while (i < s.queries) {
+        __syncthreads();
+        sq.store(tile_q);
+        sd.store(tile_d);
+        if (threadIdx.x < kRows) {
+            row_lse[threadIdx.x] = next_lse;
+            row_delta[threadIdx.x] = next_delta;
+            row_size[threadIdx.x] = next_size;
+        }
+        __syncthreads();
+        const unsigned now = i;
+        if (group < kRows || part + kRows >= group) i += at_once, part = 0;
+        else part += kRows;
+        if (i < s.queries) ask(i, part);
+        if (wave * 32u >= keys) continue;
+        if constexpr (DT == kGradF16) {
+            static_assert(kRows == 64, "a lane looks at a row");
+            float largest = row_size[l];
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) largest = __builtin_fmaxf(largest, __shfl_xor(largest, m));
+            const float want = to_one(largest);
+            if (largest > 0.0f && (!begun || want < up)) {
+                if (begun) {
+#pragma unroll
+                    for (unsigned d = 0; d < DP / 32; ++d) acc_k[d] *= want / up;
+                }
+                up = want;
+                begun = true;
+            }
+        }
+        // (every row of the tile sees every key of the wave, but for causal tiles on the border)
+        const bool border = z.causal && first_of(key0 + wave * 32u + 31u) > now;
+#pragma unroll
+        for (unsigned b = 0; b < kRows / 32; ++b) {
+            f16v x = {}, y = {};
+#pragma unroll
+            for (unsigned e = 0; e < DP / 16; ++e) x = mfma<DT>(rows_operand<DP>(tile_q, 32u * b, e), bk[e], x);
+#pragma unroll
+            for (unsigned e = 0; e < DP / 16; ++e) y = mfma<DT>(rows_operand<DP>(tile_d, 32u * b, e), bv[e], y);
+#pragma unroll
+            for (unsigned r = 0; r < 16; ++r) {
+                const unsigned row = 32u * b + row_of(r, half);
+                const bool hidden = border && now + (group < kRows ? row / group : 0u) < first_of(key0 + key);
+                x[r] = hidden ? 0.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -row_lse[row]));
+                y[r] = hidden ? 0.0f : x[r] * ((y[r] - row_delta[row]) * (up * (1.0f / kLifted<DT>)));
+            }
+#pragma unroll
+            for (unsigned h = 0; h < 2; ++h) {
+                const s8v p = rounded<DT>(x, h), ds = rounded<DT>(y, h);
+#pragma unroll
+                for (unsigned d = 0; d < DP / 32; ++d) {
+                    acc_v[d] = mfma<DT>(columns_operand<DP>(tile_d, 32u * b + 16u * h, d), p, acc_v[d]);
+                    acc_k[d] = mfma<DT>(columns_operand<DP>(tile_q, 32u * b + 16u * h, d), ds, acc_k[d]);
+                }
+            }
+        }
+    }
+    if (key >= keys) return;
+    const size_t token = s.k0 + key0 + key;
+    store_row<DT, DP>(dk.p + token * dk.ld + kv * z.dim, acc_k, z.scale / up, z.dim);
+    store_row<DT, DP>(dv.p + token * dv.ld + kv * z.dim, acc_v, 1.0f / kLifted<DT>, z.dim);
+}
+
+}  // namespace

@@ -1,6 +1,8 @@
 // Matrices in microscaled 4-bit floating point: quantisation along rows and columns, values, the matrix instruction.
 #pragma once
 
+#include "device_matrix.hpp"
+
 namespace {
 
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
@@ -8,10 +10,6 @@ typedef unsigned u4_by2 __attribute__((ext_vector_type(4), aligned(2)));  // 16 
 typedef unsigned u4_by4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr unsigned kGroup = 128;  // elements of a row that one scale word covers
-
-// Element types of matrices in ordinary floating point.
-template <int DT>
-using Elem = typename std::conditional<DT == kGradF32, float, typename std::conditional<DT == kGradBF16, __bf16, _Float16>::type>::type;
 
 // Eight elements in a row, at any address that is a multiple of the type's size.
 template <int DT>

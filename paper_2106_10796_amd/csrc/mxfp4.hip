@@ -11,6 +11,7 @@
 #include "host_common.hpp"
 #include "tuning.hpp"
 #include "device_common.hpp"
+#include "host_matrix.hpp"
 #include "mxfp4_choice.hpp"
 
 #include "kernels_mxfp4.hpp"
@@ -18,40 +19,13 @@
 
 namespace {
 
-inline bool good_dtype(int t) { return t == CDSGD_GRAD_F32 || t == CDSGD_GRAD_BF16 || t == CDSGD_GRAD_F16; }
-inline size_t bytes_of(int dtype) { return dtype == CDSGD_GRAD_F32 ? 4u : 2u; }
 inline size_t groups_of(size_t cols) { return (cols + kGroup - 1) / kGroup; }
-inline bool good_extent(size_t n) { return n > 0 && n <= 0x7FFFFFFFu; }
-
-// Bytes from the first element of a matrix to the last, both included.
-inline size_t extent_bytes(size_t rows, size_t cols, size_t ld, size_t elem) { return ((rows - 1) * ld + cols) * elem; }
-
-// Calls f(std::integral_constant<int, element type>).
-template <typename F>
-void with_dtype(int dtype, F f)
-{
-    if (dtype == CDSGD_GRAD_BF16) f(std::integral_constant<int, kGradBF16>());
-    else if (dtype == CDSGD_GRAD_F16) f(std::integral_constant<int, kGradF16>());
-    else f(std::integral_constant<int, kGradF32>());
-}
 
 // Of a matrix in MXFP4 and its place in a launch: sizes that the kernels hold in 32 bits.
 inline int check_matrix(size_t rows, size_t cols)
 {
     if (!good_extent(rows) || !good_extent(cols)) return CDSGD_ERR_SIZE;
     return CDSGD_OK;
-}
-
-// Calls launch(groups, number of the first) for launches below 2^32 lanes; all but the last hold a multiple of 32 groups, what
-// k_quantize_tiles numbers together.  (One but for matrices of 2^27 rows and more.)  The kernels number groups in 32 bits.
-template <typename F>
-int in_launches(unsigned long long groups, unsigned lanes, F launch)
-{
-    if (groups > 0xFFFFFFFFull) return CDSGD_ERR_SIZE;
-    const unsigned long long most = 0xFFFFFFFFull / lanes / 32 * 32;
-    for (unsigned long long first = 0; first < groups; first += most)
-        launch(dim3((unsigned)(groups - first < most ? groups - first : most)), (unsigned)first);
-    return launch_status();
 }
 
 // Calls f(kernel, groups, lanes) with the ring that `how` names, for results of type DT.

@@ -1,0 +1,393 @@
+"""Attention over packed sequences on the GPU against plain implementations in 64 bits.
+
+Tolerances count roundings.  With u half a step of the tensors' type and U that of fp32, and sums of n terms in fp32 in any order off by at most n 2 U of
+the terms' magnitudes:
+  a logit is off by e_S = 2 U (dim A + 4 (|S| + |lse|) + 8), A = scale sum |q| |k| (the product's sum; scale and lse, each times log2 e, taken
+  from one another; the power), a probability by e_P = 2 e_S of itself;
+  out by sum P |v| (u + e_P + 2 U keys) + u |out|, for P is rounded once and the result once;
+  dS by P |dP - delta| (u + e_P) + 2 U dim P (sum |dout| |v| + sum |dout| |out|), in fp16 also by a step of its smallest numbers under
+  the power of two by which it is divided, 2^-24 of the largest magnitude in dout;
+  dq by scale sum |k| e_dS + 2 U keys scale sum |dS| |k| + u |dq|, dk and dv alike;
+  and a result of fp16 below its smallest normal number by 2^-25, a probability there, which is rounded times 2^15, by 2^-40.
+Numbers whose exponents fp32 (and bf16) have no normal place for, below SMALL = 2^-126, may be 0: P, dS, what they are rounded to, and the results, so that
+SMALL comes on top of the error of each of them, and as a factor of what multiplies it.
+The backward pass is held to its formula at the out and lse that it is given."""
+import itertools
+
+import pytest
+import torch
+
+from paper_2106_10796_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16}
+U = 2.0 ** -24
+SMALL = 2.0 ** -126
+
+
+def starts_of(lens, first=0):
+    return torch.tensor([first + sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32, device="cuda")
+
+
+def inputs(lens_q, lens_k, heads, kv, dim, dtype, seed=0, size=1.0, behind=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda n, h: (torch.randn(n, h, dim, device="cuda", generator=gen) * size).to(TYPES[dtype])  # noqa: E731
+    T, K = sum(lens_q) + behind, sum(lens_k) + behind
+    return rnd(T, heads), rnd(K, kv), rnd(K, kv), rnd(T, heads)
+
+
+def half_step(t):
+    return torch.finfo(t.dtype).eps / 2
+
+
+def tiny(t):
+    return 2.0 ** -25 if t.dtype == torch.float16 else SMALL
+
+
+def tiny_p(t):
+    return 2.0 ** -40 if t.dtype == torch.float16 else 0.0
+
+
+def reference(q, k, v, lens_q, lens_k, causal, scale, first_q=0, first_k=0):
+    """For every sequence and key head: the logits, their magnitudes, lse and out in 64 bits."""
+    group, q0, k0 = q.shape[1] // k.shape[1], first_q, first_k
+    for nq, nk in zip(lens_q, lens_k):
+        for h in range(k.shape[1]):
+            mine = slice(h * group, (h + 1) * group)
+            x, y, z = (t.double().contiguous() for t in (q[q0:q0 + nq, mine].transpose(0, 1), k[k0:k0 + nk, h], v[k0:k0 + nk, h]))
+            s = torch.matmul(x, y.t().contiguous()) * scale
+            size = torch.matmul(x.abs(), y.abs().t().contiguous()) * scale
+            if causal:
+                i, j = torch.arange(nq, device="cuda")[:, None], torch.arange(nk, device="cuda")
+                s = s.masked_fill(j > i + nk - nq, float("-inf"))
+            yield slice(q0, q0 + nq), slice(k0, k0 + nk), h, mine, s, size, x, y, z
+        q0, k0 = q0 + nq, k0 + nk
+
+
+def probabilities(s, lse):
+    return torch.where(torch.isinf(s), 0.0, torch.exp(s - torch.where(torch.isinf(lse), 0.0, lse)[..., None]))
+
+
+def logit_error(s, size, lse, dim):
+    s, lse = torch.where(torch.isinf(s), 0.0, s), torch.where(torch.isinf(lse), 0.0, lse)
+    return 2 * U * (dim * size + 4 * (s.abs() + lse.abs()[..., None]) + 8)
+
+
+def close(got, want, error, what):
+    near = (got.double() - want).abs() <= error
+    if got.dtype == torch.float16:          # 65520 and more, halfway from the largest number to the next power of two, is rounded to infinity
+        near |= torch.isinf(got) & (torch.sign(got) == torch.sign(want)) & (want.abs() + error >= 65520)
+    got, bad = got.double(), ~near
+    assert not bool(bad.any()), "%s: %d of %d, first at %s: got %r, want %r within %r" % (
+        what, int(bad.sum()), bad.numel(), bad.nonzero()[0].tolist(), float(got[bad][0]), float(want[bad][0]), float(error.expand_as(want)[bad][0]))
+
+
+def check_forward(q, k, v, out, lse, lens_q, lens_k, causal, scale, first_q=0, first_k=0):
+    u, dim = half_step(q), q.shape[2]
+    for rows, _, _, mine, s, size, x, y, z in reference(q, k, v, lens_q, lens_k, causal, scale, first_q, first_k):
+        if not s.shape[1]:
+            continue
+        want_lse = torch.logsumexp(s, 2) if s.shape[2] else torch.full(s.shape[:2], float("-inf"), dtype=torch.float64, device="cuda")
+        p = probabilities(s, want_lse)
+        e = logit_error(s, size, want_lse, dim)
+        if lse is not None:
+            got = lse[mine, rows].double()
+            empty = torch.isinf(want_lse)
+            assert torch.equal(torch.isinf(got), empty) and bool((got[empty] < 0).all())
+            worst = e.amax(2) if s.shape[2] else torch.zeros_like(want_lse)
+            close(torch.where(empty, 0.0, got), torch.where(empty, 0.0, want_lse), worst + 2 * U * (s.shape[2] + 4 * want_lse.masked_fill(empty, 0).abs()),
+                  "lse")
+        want = torch.matmul(p, z)
+        error = torch.matmul(p * (u + 2 * e + 2 * U * s.shape[2]) + 2 * SMALL + tiny_p(q), z.abs()) + u * want.abs() + tiny(q)
+        close(out[rows, mine].transpose(0, 1), want, error, "out")
+
+
+def check_backward(dout, q, k, v, out, lse, dq, dk, dv, lens_q, lens_k, causal, scale, first_q=0, first_k=0):
+    u, dim = half_step(q), q.shape[2]
+    for rows, cols, h, mine, s, size, x, y, z in reference(q, k, v, lens_q, lens_k, causal, scale, first_q, first_k):
+        nq, nk = s.shape[1], s.shape[2]
+        do, o = (t[rows, mine].double().transpose(0, 1).contiguous() for t in (dout, out))
+        at = lse[mine, rows].double()
+        p, e_p = probabilities(s, at), 2 * logit_error(s, size, at, dim)
+        dp, delta = torch.matmul(do, z.t().contiguous()), (do * o).sum(2, keepdim=True)
+        ds = p * (dp - delta)
+        e_ds = ds.abs() * (u + e_p) + 2 * U * dim * p * (torch.matmul(do.abs(), z.abs().t().contiguous()) + (do * o).abs().sum(2, keepdim=True))
+        e_ds = e_ds + 2 * SMALL * (1 + (dp - delta).abs())
+        if q.dtype == torch.float16 and do.numel():
+            e_ds = e_ds + 2.0 ** -24 * float(dout.abs().max()) * (p > 0)
+        want = scale * torch.matmul(ds, y)
+        close(dq[rows, mine].transpose(0, 1), want,
+              scale * torch.matmul(e_ds + 2 * U * nk * ds.abs(), y.abs()) + u * want.abs() + tiny(q), "dq")
+        n = nq * s.shape[0]
+        for got, w, e_w, other, what, f in ((dk, ds, e_ds, x, "dk", scale), (dv, p, p * (u + e_p) + 2 * SMALL + tiny_p(q), do, "dv", 1.0)):
+            flat = lambda t: t.reshape(n, t.shape[2])  # noqa: E731
+            want = f * torch.matmul(flat(w).t().contiguous(), flat(other))
+            error = f * torch.matmul((flat(e_w) + 2 * U * n * flat(w).abs()).t().contiguous(), flat(other).abs()) + u * want.abs() + tiny(q)
+            close(got[cols, h], want, error, what)
+
+
+def go(q, k, v, dout, lens_q, lens_k, causal, scale=None, first=0, plain_starts=False):
+    """Both passes, with guards behind the sequences looked at."""
+    same = plain_starts or lens_q == lens_k
+    starts = None if plain_starts else starts_of(lens_q, first)
+    starts_k = None if same else starts_of(lens_k, first)
+    scale_ = q.shape[2] ** -0.5 if scale is None else scale
+    room = B.new_attention_workspace(q, k, seqs=len(lens_q), train=True)
+    out, lse = torch.full_like(q, 7.0), torch.full((q.shape[1], q.shape[0]), 7.0, device="cuda")
+    B.cdsgd_attention_forward(q, k, v, out, lse, starts, starts_k, causal, scale, room)
+    check_forward(q, k, v, out, lse, lens_q, lens_k, causal, scale_, first, first)
+    grads = [torch.full_like(t, 7.0) for t in (q, k, v)]
+    B.cdsgd_attention_backward(dout, q, k, v, out, lse, *grads, starts, starts_k, causal, scale, room)
+    check_backward(dout, q, k, v, out, lse, *grads, lens_q, lens_k, causal, scale_, first, first)
+    for t, lens in ((out, lens_q), (grads[0], lens_q), (grads[1], lens_k), (grads[2], lens_k)):
+        end = first + sum(lens)
+        assert bool((t[:first] == 7.0).all()) and bool((t[end:] == 7.0).all())
+    assert bool((lse[:, :first] == 7.0).all()) and bool((lse[:, first + sum(lens_q):] == 7.0).all())
+    return out, lse, grads
+
+
+LENGTHS = [[1], [2], [17], [31, 32, 33], [64, 65], [127, 1, 128, 129], [0, 3, 0, 0, 200, 0], [300], [1] * 70, [5, 513]]
+
+
+@pytest.mark.parametrize("lens", LENGTHS, ids=lambda x: "-".join(map(str, x[:6])))
+@pytest.mark.parametrize("heads,kv,dim", [(2, 1, 64), (3, 3, 128), (8, 2, 40), (4, 4, 8)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_packed(lens, heads, kv, dim, causal):
+    go(*inputs(lens, lens, heads, kv, dim, "bf16", seed=sum(lens) + dim), lens, lens, causal)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("heads,kv,dim", [(1, 1, 16), (6, 2, 72), (7, 1, 96), (16, 2, 128), (12, 4, 64), (65, 1, 64), (130, 1, 16), (64, 1, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_heads_and_types(dtype, heads, kv, dim, causal):
+    lens = [40, 1, 150]
+    go(*inputs(lens, lens, heads, kv, dim, dtype, seed=heads + dim), lens, lens, causal)
+
+
+@pytest.mark.parametrize("lens_q,lens_k", [([1], [1000]), ([3, 1], [70, 129]), ([100], [40]), ([10, 200, 5], [0, 130, 5]), ([130, 0], [129, 7]),
+                                           ([64, 64], [1, 2]), ([33], [4000]), ([1] * 5, [600, 1, 64, 63, 2000])], ids=str)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_more_or_fewer_keys(lens_q, lens_k, causal, dtype):
+    """A prompt continued, a single token, and queries before the first key, which see nothing."""
+    go(*inputs(lens_q, lens_k, 6, 2, 64, dtype, seed=5), lens_q, lens_k, causal)
+
+
+@pytest.mark.parametrize("lens_k", [[20000], [300, 9000, 1]], ids=str)
+@pytest.mark.parametrize("heads,kv,dim", [(8, 2, 128), (1, 1, 64), (40, 8, 80)])
+def test_single_tokens(lens_k, heads, kv, dim):
+    """Few rows and many keys: the keys are split over groups and their parts joined."""
+    lens_q = [1] * len(lens_k)
+    q, k, v, _ = inputs(lens_q, lens_k, heads, kv, dim, "bf16", seed=3)
+    out, lse = torch.empty_like(q), torch.empty(heads, len(lens_q), device="cuda")
+    room = B.new_attention_workspace(q, k, seqs=len(lens_q))
+    B.cdsgd_attention_forward(q, k, v, out, lse, starts_of(lens_q), starts_of(lens_k), workspace=room)
+    check_forward(q, k, v, out, lse, lens_q, lens_k, True, dim ** -0.5)
+    again = torch.empty_like(q)
+    B.cdsgd_attention_forward(q, k, v, again, None, starts_of(lens_q), starts_of(lens_k), workspace=room)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("first,behind", [(0, 30), (9, 0), (129, 70)])
+def test_rows_of_no_sequence_are_left(first, behind):
+    lens = [50, 0, 90]
+    q, k, v, dout = inputs(lens, lens, 4, 2, 64, "bf16", behind=first + behind)
+    for t in (q, k, v, dout):                                   # they are not read either
+        t[:first], t[first + sum(lens):] = float("nan"), float("nan")
+    go(q, k, v, dout, lens, lens, True, first=first)
+
+
+def test_one_sequence_without_starts():
+    lens = [333]
+    q, k, v, dout = inputs(lens, lens, 4, 2, 128, "bf16")
+    a = go(q, k, v, dout, lens, lens, True, plain_starts=True)
+    b = go(q, k, v, dout, lens, lens, True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and all(torch.equal(x, y) for x, y in zip(a[2], b[2]))
+    short = inputs([7], [100], 4, 2, 128, "bf16", seed=2)
+    go(*short, [7], [100], True, plain_starts=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_slices_of_one_projection(dtype):
+    """q, k and v, and their gradients, as slices of one matrix [tokens, (heads + 2 kv) dim] each, with more behind them."""
+    lens, heads, kv, dim = [70, 131], 6, 2, 72
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    wide = lambda: torch.randn(sum(lens), (heads + 2 * kv) * dim + 24, device="cuda", generator=gen).to(TYPES[dtype])  # noqa: E731
+    x, dx = wide(), torch.zeros_like(wide())
+
+    def slices(t):
+        at = [0, heads * dim, (heads + kv) * dim, (heads + 2 * kv) * dim]
+        return [t[:, a:b].unflatten(1, (-1, dim)) for a, b in zip(at, at[1:])]
+    q, k, v = slices(x)
+    dout = torch.randn(sum(lens), heads, dim, device="cuda", generator=gen).to(TYPES[dtype])
+    out, lse, room = torch.empty_like(dout), torch.empty(heads, sum(lens), device="cuda"), B.new_attention_workspace(q, k, seqs=2, train=True)
+    B.cdsgd_attention_forward(q, k, v, out, lse, starts_of(lens), workspace=room)
+    check_forward(q, k, v, out, lse, lens, lens, True, dim ** -0.5)
+    B.cdsgd_attention_backward(dout, q, k, v, out, lse, *slices(dx), starts_of(lens), workspace=room)
+    check_backward(dout, q, k, v, out, lse, *slices(dx), lens, lens, True, dim ** -0.5)
+    assert bool((dx[:, -24:] == 0).all())
+    whole = [t.contiguous() for t in (q, k, v)]
+    grads = [torch.empty_like(t) for t in whole]
+    B.cdsgd_attention_backward(dout, *whole, out, lse, *grads, starts_of(lens), workspace=room)
+    assert all(torch.equal(a, b) for a, b in zip(grads, slices(dx)))
+
+
+@pytest.mark.parametrize("dtype,size", [("bf16", 8.0), ("bf16", 1e-3), ("f16", 8.0), ("f16", 1e-2)])
+def test_sharp_and_flat_rows(dtype, size):
+    lens = [100, 260]
+    go(*inputs(lens, lens, 4, 2, 64, dtype, size=size), lens, lens, True)
+
+
+@pytest.mark.parametrize("scale", [1.0, 1e-3, 0.3])
+def test_scales(scale):
+    lens = [130]
+    go(*inputs(lens, lens, 2, 2, 64, "bf16"), lens, lens, True, scale=scale)
+
+
+@pytest.mark.parametrize("size", [1e-6, 1e-4, 1e4])
+def test_gradients_of_any_size_in_fp16(size):
+    """dS has a power of two of its own: small gradients are not lost, and large ones do not overflow on the way."""
+    lens = [40, 300]
+    q, k, v, dout = inputs(lens, lens, 4, 2, 64, "f16", seed=7)
+    v = v * 0.01 if size > 1 else v
+    dout = (dout.float() * size).half()
+    dout[-50:] = 0
+    go(q, k, v, dout, lens, lens, True)
+
+
+def test_infinities_and_nan_stay_where_they_are():
+    """A NaN or an infinity of a key reaches the rows of its sequence from 192 before it on, and none of other sequences and heads; what lies
+    behind a sequence's end reaches none."""
+    lens = [400, 40]
+    q, k, v, dout = inputs(lens, lens, 4, 2, 64, "bf16")
+    starts = starts_of(lens)
+    clean, lse, clean_grads = go(q, k, v, dout, lens, lens, True)
+    room = B.new_attention_workspace(q, k, seqs=2, train=True)
+    hit = torch.zeros(sum(lens), 4, dtype=torch.bool, device="cuda")
+    hit[390 - 192:400, 2:] = True
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        for t in (k, v):
+            was = t[390, 1].clone()
+            t[390, 1, 3] = bad
+            out, lse_bad, grads = torch.empty_like(q), torch.empty(4, sum(lens), device="cuda"), [torch.empty_like(x) for x in (q, k, v)]
+            B.cdsgd_attention_forward(q, k, v, out, lse_bad, starts, workspace=room)
+            B.cdsgd_attention_backward(dout, q, k, v, out, lse_bad, *grads, starts, workspace=room)
+            assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse_bad.t()[~hit], lse.t()[~hit]) and torch.equal(grads[0][~hit], clean_grads[0][~hit])
+            assert all(torch.equal(a[400:], b[400:]) and torch.equal(a[:, 0], b[:, 0]) for a, b in zip(grads[1:], clean_grads[1:]))
+            t[390, 1] = was
+
+
+def test_the_lowest_numbers_as_logits():
+    """Logits of about -1e38 and 1e38 in one row, and rows that are far below 0 throughout."""
+    lens = [70]
+    q, k, v, dout = inputs(lens, lens, 2, 2, 64, "bf16")
+    q = q * 0 + 1e19
+    k = torch.where(torch.arange(70, device="cuda")[:, None, None] % 3 == 0, -1e16, -1e17).to(torch.bfloat16).expand_as(k).contiguous()
+    out, lse = torch.empty_like(q), torch.empty(2, 70, device="cuda")
+    B.cdsgd_attention_forward(q, k, v, out, lse, starts_of(lens), workspace=None)
+    # row i has the mean of the values of keys 0, 3, ... up to i
+    take = (torch.arange(70, device="cuda") % 3 == 0).double()
+    want = torch.cumsum(v.double() * take[:, None, None], 0) / torch.cumsum(take, 0)[:, None, None]
+    bound = torch.cumsum(v.double().abs() * take[:, None, None], 0) / torch.cumsum(take, 0)[:, None, None]
+    close(out, want, 2.0 ** -8 * (want.abs() + bound) + 2 * U * 70 * bound, "out")
+    assert bool(torch.isfinite(lse).all())
+
+
+def test_same_bits_from_run_to_run_and_in_any_batch():
+    """What a sequence's results are does not depend on the sequences beside it."""
+    lens = [200, 77, 130]
+    q, k, v, dout = inputs(lens, lens, 8, 2, 128, "bf16")
+    a = go(q, k, v, dout, lens, lens, True)
+    b = go(q, k, v, dout, lens, lens, True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and all(torch.equal(x, y) for x, y in zip(a[2], b[2]))
+    cut = slice(200, 277)
+    c = go(q[cut].contiguous(), k[cut].contiguous(), v[cut].contiguous(), dout[cut].contiguous(), [77], [77], True)
+    assert torch.equal(a[1][:, cut], c[1]) and torch.equal(a[0][cut], c[0]) and torch.equal(a[2][1][cut], c[2][1]) and torch.equal(a[2][2][cut], c[2][2])
+
+
+def test_starts_out_of_range_touch_nothing_outside():
+    """What is not in range is cut; what falls has no meaning, but stays inside the tensors."""
+    q, k, v, dout = inputs([100], [100], 4, 2, 64, "bf16")
+    out, lse, room = torch.zeros_like(q), torch.zeros(4, 100, device="cuda"), B.new_attention_workspace(q, k, seqs=2, train=True)
+    B.cdsgd_attention_forward(q, k, v, out, lse, torch.tensor([-5, 60, 1000], dtype=torch.int32, device="cuda"), workspace=room)
+    check_forward(q, k, v, out, lse, [60, 40], [60, 40], True, 0.125)
+    around = [torch.full((300, *t.shape[1:]), 7.0, dtype=t.dtype, device="cuda") for t in (q, q, k, v)]
+    inner = [t[100:200] for t in around]
+    for bad in ([50, 20, 90], [2 ** 31 - 1, -2 ** 31, 50], [90, 90, 10]):
+        starts = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        B.cdsgd_attention_forward(q, k, v, inner[0], lse, starts, workspace=room)
+        B.cdsgd_attention_backward(dout, q, k, v, inner[0], lse, *inner[1:], starts, workspace=room)
+        assert all(bool((t[:100] == 7.0).all()) and bool((t[200:] == 7.0).all()) for t in around)
+
+
+def test_other_streams_and_a_graph():
+    """Both passes captured once and replayed on other inputs, with eager calls between the replays, on a stream that is not the default one."""
+    lens = [60, 130]
+    q, k, v, dout = inputs(lens, lens, 4, 2, 64, "bf16")
+    starts, room = starts_of(lens), B.new_attention_workspace(q, k, seqs=2, train=True)
+    out, lse, grads = torch.empty_like(q), torch.empty(4, 190, device="cuda"), [torch.empty_like(t) for t in (q, k, v)]
+
+    def step():
+        B.cdsgd_attention_forward(q, k, v, out, lse, starts, workspace=room)
+        B.cdsgd_attention_backward(dout, q, k, v, out, lse, *grads, starts, workspace=room)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        step()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        for seed in range(3):
+            for t, new in zip((q, k, v, dout), inputs(lens, lens, 4, 2, 64, "bf16", seed=seed + 20)):
+                t.copy_(new)
+            graph.replay()
+            got = [t.clone() for t in (out, lse, *grads)]
+            for t in (out, lse, *grads):
+                t.fill_(3.0)
+            step()
+            side.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, (out, lse, *grads)))
+            check_backward(dout, q, k, v, out, lse, *grads, lens, lens, True, 0.125)
+
+
+def test_long_sequences_past_32_bits():
+    """A cache whose last keys lie past 2^32 bytes from its first."""
+    held, kv, dim = 1 << 18, 8, 128
+    ld = 1 << 14                                                # elements from token to token: 2^18 tokens are 8 GiB
+    cache = torch.zeros(held, ld, dtype=torch.bfloat16, device="cuda")
+    k, v = (cache[:, i * kv * dim:(i + 1) * kv * dim].unflatten(1, (kv, dim)) for i in range(2))
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    lens_k = [held - 700, 700]
+    k[-700:] = torch.randn(700, kv, dim, device="cuda", generator=gen).bfloat16()
+    v[-700:] = torch.randn(700, kv, dim, device="cuda", generator=gen).bfloat16()
+    q = torch.randn(2, 2 * kv, dim, device="cuda", generator=gen).bfloat16()
+    out, lse = torch.empty_like(q), torch.empty(2 * kv, 2, device="cuda")
+    B.cdsgd_attention_forward(q, k, v, out, lse, starts_of([1, 1]), starts_of(lens_k), workspace=B.new_attention_workspace(q, k, seqs=2))
+    check_forward(q[1:], k[-700:], v[-700:], out[1:], lse[:, 1:], [1], [700], True, dim ** -0.5)
+    close(lse[:, 0].double(), torch.full((2 * kv,), float(held - 700), dtype=torch.float64, device="cuda").log(),
+          torch.full((2 * kv,), 1e-3, dtype=torch.float64, device="cuda"), "lse of equal logits")
+
+
+def test_formula_against_differences():
+    """The gradients that the checks above hold the kernels to are those of the forward formula: central differences in 64 bits."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v, do = (torch.randn(n, h, 8, dtype=torch.float64, device="cuda", generator=gen) for n, h in ((5, 2), (6, 1), (6, 1), (5, 2)))
+
+    def loss(q, k, v):
+        total = 0.0
+        for rows, _, _, mine, s, _, x, y, z in reference(q, k, v, [5], [6], True, 0.4):
+            total = total + (torch.matmul(torch.softmax(s, 2), z) * do[rows, mine].transpose(0, 1)).sum()
+        return total
+    for _, _, _, _, s, _, x, y, z in reference(q, k, v, [5], [6], True, 0.4):
+        g = do.transpose(0, 1).contiguous()
+        p = probabilities(s, torch.logsumexp(s, 2))
+        ds = p * (torch.matmul(g, z.t()) - (g * torch.matmul(p, z)).sum(2, keepdim=True))
+        want = [0.4 * torch.matmul(ds, y).transpose(0, 1), 0.4 * torch.einsum("gij,gid->jd", ds, x)[:, None], torch.einsum("gij,gid->jd", p, g)[:, None]]
+    for which, at in itertools.product(range(3), range(0, 40, 7)):
+        args = [q, k, v]
+        e = torch.zeros_like(args[which])
+        e.view(-1)[at] = 1e-5
+        up, down = ([t + e if i == which else t for i, t in enumerate(args)], [t - e if i == which else t for i, t in enumerate(args)])
+        diff = float((loss(*up) - loss(*down)) / 2e-5)
+        assert abs(diff - float(want[which].reshape(-1)[at])) <= 1e-8
