@@ -11,6 +11,7 @@
 #include "tuning.hpp"
 #include "device_common.hpp"
 #include "host_matrix.hpp"
+#include "mxfp4_choice.hpp"
 
 #include "kernels_attention.hpp"
 
@@ -29,6 +30,7 @@ inline unsigned splits_of(const cdsgd_attention &b)
     const unsigned long long groups = groups_over(b.tokens_q, b.num_seqs, (size_t)(b.heads / b.kv_heads), (size_t)b.kv_heads);
     if (groups >= 256) return 1;
     const unsigned long long want = (511 + groups) / groups, most = b.tokens_k / b.num_seqs / (4 * kTileKeys);
+    static_assert(kMostSplits >= 512, "of 512 groups all may share one row's keys");
     return (unsigned)(want < most ? want : most < 1 ? 1 : most);
 }
 
@@ -104,7 +106,7 @@ size_t cdsgd_attention_workspace(const cdsgd_attention *batch, int backward)
 {
     if (check_batch(batch) != CDSGD_OK) return 0;
     const size_t rows = batch->tokens_q * (size_t)batch->heads;
-    if (backward) return rows * 2 * sizeof(float) + 15u & ~(size_t)15u;
+    if (backward) return (rows * 3 * sizeof(float) + 15u) & ~(size_t)15u;
     const unsigned splits = splits_of(*batch);
     return splits > 1 ? (splits * rows * (size_t)(padded_dim(batch->dim) + 1) * sizeof(float) + 15u) & ~(size_t)15u : 0;
 }
@@ -138,7 +140,7 @@ int cdsgd_attention_forward(const cdsgd_attention *batch, const void *q, size_t 
         hipLaunchKernelGGL((k_attention_forward<DT, DP>), dim3(groups), dim3(256), 0, stream, z, read_of<DT>(q, ld_q), read_of<DT>(k, ld_k),
                            read_of<DT>(v, ld_v), write_of<DT>(out, ld_out), lse, splits, parts, part_lse);
         if (parts)
-            hipLaunchKernelGGL((k_attention_join<DT, DP>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, z, write_of<DT>(out, ld_out), lse,
+            hipLaunchKernelGGL((k_attention_join<DT, DP>), dim3((unsigned)rows), dim3(256), 0, stream, z, write_of<DT>(out, ld_out), lse,
                                splits, (const float *)parts, (const float *)part_lse);
     });
     return launch_status();
@@ -169,13 +171,13 @@ int cdsgd_attention_backward(const cdsgd_attention *batch, const void *dout, siz
     hipStream_t stream = (hipStream_t)hip_stream;
     with_kernel(a, [&](auto dt, auto dim) {
         constexpr int DT = decltype(dt)::value, DP = decltype(dim)::value;
-        float *const delta = static_cast<float *>(workspace), *const size = delta + rows;
+        float *const row_lse = static_cast<float *>(workspace), *const delta = row_lse + rows, *const size = delta + rows;
         hipLaunchKernelGGL((k_attention_dq<DT, DP>), dim3((unsigned)groups_over(a.tokens_q, a.num_seqs, z.group, z.kv_heads)), dim3(256), 0, stream, z,
                            read_of<DT>(dout, ld_dout), read_of<DT>(q, ld_q), read_of<DT>(k, ld_k), read_of<DT>(v, ld_v), read_of<DT>(out, ld_out), lse,
-                           write_of<DT>(dq, ld_dq), delta, size);
+                           write_of<DT>(dq, ld_dq), row_lse, delta, size);
         hipLaunchKernelGGL((k_attention_dkv<DT, DP>), dim3((unsigned)groups_over(a.tokens_k, a.num_seqs, 1, z.kv_heads)), dim3(256), 0, stream, z,
-                           read_of<DT>(dout, ld_dout), read_of<DT>(q, ld_q), read_of<DT>(k, ld_k), read_of<DT>(v, ld_v), lse, (const float *)delta,
-                           (const float *)size, write_of<DT>(dk, ld_dk), write_of<DT>(dv, ld_dv));
+                           read_of<DT>(dout, ld_dout), read_of<DT>(q, ld_q), read_of<DT>(k, ld_k), read_of<DT>(v, ld_v), (const float *)row_lse,
+                           (const float *)delta, (const float *)size, write_of<DT>(dk, ld_dk), write_of<DT>(dv, ld_dv));
     });
     return launch_status();
 }

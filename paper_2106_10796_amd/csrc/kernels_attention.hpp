@@ -13,27 +13,31 @@
 #pragma once
 
 #include "device_matrix.hpp"
+#include "kernels_mxfp4.hpp"
+#include "kernels_mxfp4_product.hpp"  // loads to LDS
 
 namespace {
 
-typedef float f16v __attribute__((ext_vector_type(16)));
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef short s8v __attribute__((ext_vector_type(8)));
-
-#define CDSGD_LDS __attribute__((address_space(3)))
 
 constexpr float kLog2e = 1.44269504088896f;
 constexpr float kInfinity = __builtin_inff();
 constexpr unsigned kRecords = 0x40000000u, kOutside = 0x7FFFFFF0u;  // of a buffer; a place behind every buffer's end, which loads 0
 
-// Probabilities of fp16 tensors are operands of the second products times 2^15, the largest power of two that 1 can be multiplied with there: numbers
-// below 2^-14 lose bits in fp16, and a row of 2^14 keys has no others.
+// Probabilities of fp16 tensors are operands of the second products times a power of two, 2^15 being the largest that 1 can be multiplied with
+// there: numbers below 2^-14 lose bits in fp16, and a row of 2^14 keys has no others.  The forward pass leaves room for kSlack.
+constexpr float kSlack = 8.0f;
+constexpr float kFar = 1048576.0f;
 template <int DT>
-constexpr float kLift = DT == kGradF16 ? 15.0f : 0.0f;
+constexpr float kLift = DT == kGradF16 ? 7.0f : 0.0f;
+template <int DT>
+constexpr float kLiftBack = DT == kGradF16 ? 15.0f : 0.0f;
 template <int DT>
 constexpr float kLifted = DT == kGradF16 ? 32768.0f : 1.0f;
 
 constexpr unsigned kTileRows = 128;  // rows of a group of the forward pass and of dq, and keys of a group of dk and dv
+constexpr unsigned kMostSplits = 512;
 constexpr unsigned kTileKeys = 64;   // what a group takes at a time of the other side
 
 template <int DT>
@@ -79,25 +83,26 @@ __device__ __forceinline__ Sequence sequence_of(const AttentionSizes &z, unsigne
 {
     Sequence x = {0u, z.tokens_q, 0u, z.tokens_k};
     if (z.starts_q) {
-        x.q0 = cut(z.starts_q[s], 0u, z.tokens_q);
-        x.queries = cut(z.starts_q[s + 1u], x.q0, z.tokens_q) - x.q0;
+        const auto at = [](const int *p) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(*p); };
         const int *k = z.starts_k ? z.starts_k : z.starts_q;
-        x.k0 = cut(k[s], 0u, z.tokens_k);
-        x.keys = cut(k[s + 1u], x.k0, z.tokens_k) - x.k0;
+        x.q0 = cut(at(z.starts_q + s), 0u, z.tokens_q);
+        x.queries = cut(at(z.starts_q + s + 1u), x.q0, z.tokens_q) - x.q0;
+        x.k0 = cut(at(k + s), 0u, z.tokens_k);
+        x.keys = cut(at(k + s + 1u), x.k0, z.tokens_k) - x.k0;
     }
     return x;
 }
 
 // Tiles of a packed batch are numbered without a table: sequence s, whose rows are `each` for one of its tokens, begins at number
 // starts[s] * each / tile + s, which leaves it a number for each of its tiles and at most one too many.  The search takes 64 sequences a step.
-struct Tile {
+struct TileAt {
     unsigned seq;
     unsigned long long at;  // in its sequence
 };
-__device__ __forceinline__ Tile tile_of(const int *starts, unsigned tokens, unsigned num_seqs, unsigned each, unsigned tile, unsigned long long number)
+__device__ __forceinline__ TileAt tile_of(const int *starts, unsigned tokens, unsigned num_seqs, unsigned each, unsigned tile, unsigned long long number)
 {
     if (!starts) return {0u, number * tile};
-    const auto first = [&](unsigned s) { return (unsigned long long)cut(starts[s], 0u, tokens) * each / tile + s; };
+    const auto first = [&](unsigned s) __attribute__((always_inline)) { return (unsigned long long)cut(starts[s], 0u, tokens) * each / tile + s; };
     unsigned lo = 0, left = num_seqs;
     while (left > 1u) {
         const unsigned step = (left + 63u) / 64u, s = lo + threadIdx.x % 64u * step;
@@ -108,7 +113,7 @@ __device__ __forceinline__ Tile tile_of(const int *starts, unsigned tokens, unsi
         if (step == 1u) break;
     }
     lo = (unsigned)__builtin_amdgcn_readfirstlane((int)lo);
-    const unsigned long long begin = first(lo);
+    const unsigned long long begin = (unsigned long long)cut(__builtin_amdgcn_readfirstlane(starts[lo]), 0u, tokens) * each / tile + lo;
     return {lo, number < begin ? ~0ull : (number - begin) * tile};
 }
 
@@ -149,47 +154,55 @@ __device__ __forceinline__ unsigned turned(unsigned row, unsigned chunk)
 template <int DP>
 __device__ __forceinline__ unsigned lds_chunk(unsigned row, unsigned chunk) { return row * (DP * 2u) + turned<DP>(row, chunk) * 16u; }
 
+typedef CDSGD_LDS unsigned char *Lds;
+
 // Row l % 32 (from `row0` on), elements 16 k + 8 (l / 32) ... + 7: a first operand.
 template <int DP>
-__device__ __forceinline__ s8v rows_operand(const unsigned char *tile, unsigned row0, unsigned k)
+__device__ __forceinline__ s8v rows_operand(Lds tile, unsigned row0, unsigned k)
 {
     const unsigned l = threadIdx.x % 64u;
-    return *reinterpret_cast<const s8v *>(__builtin_assume_aligned(tile + lds_chunk<DP>(row0 + l % 32u, 2u * k + l / 32u), 16));
+    return *(const CDSGD_LDS s8v *)(tile + row0 * (DP * 2u) + lds_chunk<DP>(l % 32u, 2u * k + l / 32u));
 }
 
 // Column 32 d + l % 32 of rows row0 + 4 (l / 32) ... + 3 and row0 + 8 + 4 (l / 32) ... + 3: a first operand, transposed.
 template <int DP>
-__device__ __forceinline__ s8v columns_operand(const unsigned char *tile, unsigned row0, unsigned d)
+__device__ __forceinline__ s8v columns_operand(Lds tile, unsigned row0, unsigned d)
 {
-    const unsigned l = threadIdx.x % 64u, row = row0 + 4u * (l / 32u) + l % 16u / 4u, at = 32u * d + 16u * (l / 16u % 2u) + 4u * (l % 4u);
+    const unsigned l = threadIdx.x % 64u, row = 4u * (l / 32u) + l % 16u / 4u, at = 32u * d + 16u * (l / 16u % 2u) + 4u * (l % 4u);
     const unsigned in = at % 8u * 2u;
-    typedef s4v CDSGD_LDS *Four;
-    const s4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(tile + lds_chunk<DP>(row, at / 8u) + in));
-    const s4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(tile + lds_chunk<DP>(row + 8u, at / 8u) + in));
+    typedef CDSGD_LDS s4v *Four;
+    const s4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(tile + row0 * (DP * 2u) + lds_chunk<DP>(row, at / 8u) + in));
+    const s4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(tile + row0 * (DP * 2u) + lds_chunk<DP>(row + 8u, at / 8u) + in));
     return s8v{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 }
 
-// A tile of ROWS rows on its way to LDS, by 256 lanes.
-template <int DP, int ROWS>
-struct Staged {
-    static constexpr unsigned kChunks = DP / 8, kLoads = ROWS * kChunks / 256;
-    s8v v[kLoads];
+// A buffer's description, in scalar registers.
+__device__ __forceinline__ i4s same_in_all(i4s x)
+{
+    return i4s{__builtin_amdgcn_readfirstlane(x.x), __builtin_amdgcn_readfirstlane(x.y), __builtin_amdgcn_readfirstlane(x.z), x.w};
+}
 
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, unsigned rows, unsigned group, unsigned ld, unsigned dim)
+// A tile of ROWS rows on its way to LDS, by WAVES waves: row i is head i % group of token i / group.  What the buffer does not hold, and
+// elements behind `dim`, arrive as 0.
+template <int DP, int ROWS, int WAVES>
+struct TileLoads {
+    static constexpr unsigned kLoads = ROWS * DP * 2 / 1024 / WAVES;
+    unsigned at[kLoads];
+
+    __device__ __forceinline__ TileLoads(unsigned wave, unsigned group, unsigned ld, unsigned dim)
     {
+        const unsigned l = threadIdx.x % 64u;
 #pragma unroll
         for (unsigned i = 0; i < kLoads; ++i) {
-            const unsigned at = i * 256u + threadIdx.x;
-            v[i] = load16(from, row_offset(at / kChunks, rows, group, ld, at % kChunks * 8u, dim));
+            const unsigned row = (wave * kLoads + i) * (512u / DP) + l / (DP / 8u), d = turned<DP>(row, l % (DP / 8u)) * 8u;
+            at[i] = d < dim ? (row / group * ld + row % group * dim + d) * 2u : kOutside;
         }
     }
-    __device__ __forceinline__ void store(unsigned char *tile) const
+    __device__ __forceinline__ void ask(Lds tile, unsigned wave, const void *from, unsigned bytes) const
     {
+        const i4s buffer = same_in_all(buffer_of(from, bytes));
 #pragma unroll
-        for (unsigned i = 0; i < kLoads; ++i) {
-            const unsigned at = i * 256u + threadIdx.x;
-            *reinterpret_cast<s8v *>(__builtin_assume_aligned(tile + lds_chunk<DP>(at / kChunks, at % kChunks), 16)) = v[i];
-        }
+        for (unsigned i = 0; i < kLoads; ++i) load_to_lds<16>(buffer, tile + (wave * kLoads + i) * 1024u, at[i]);
     }
 };
 
@@ -228,21 +241,23 @@ __device__ __forceinline__ void store_row(Elem<DT> *row, const f16v (&acc)[DP / 
 // parts, part_lse: where several groups share a row's keys (`splits`), each leaves its own result, [splits][row of all][DP] in fp32 and
 // [splits][row of all]; rows of all are numbered [kv head][query][head of the group].
 template <int DT, int DP>
-__global__ __launch_bounds__(256) void k_attention_forward(AttentionSizes z, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k, Heads<const Elem<DT>> v,
+__global__ __launch_bounds__(256, 2) void k_attention_forward(AttentionSizes z, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k, Heads<const Elem<DT>> v,
                                                            Heads<Elem<DT>> out, float *__restrict__ lse, unsigned splits, float *__restrict__ parts,
                                                            float *__restrict__ part_lse)
 {
-    __shared__ __align__(1024) unsigned char tile_k[kTileKeys * DP * 2], tile_v[kTileKeys * DP * 2];
+    constexpr unsigned kTile = kTileKeys * DP * 2;
+    __shared__ __align__(1024) unsigned char smem[4 * kTile];  // two tiles of keys and of values
+    const Lds lds = (Lds)smem;
     const unsigned kv = blockIdx.x % z.kv_heads, split = blockIdx.x / z.kv_heads % splits;
     // (the last tiles of a sequence see the most keys: they go first)
-    const Tile t = tile_of(z.starts_q, z.tokens_q, z.num_seqs, z.group, kTileRows,
+    const TileAt t = tile_of(z.starts_q, z.tokens_q, z.num_seqs, z.group, kTileRows,
                            tiles_over(z.tokens_q, z.num_seqs, z.group, kTileRows) - 1u - blockIdx.x / z.kv_heads / splits);
     const Sequence s = sequence_of(z, t.seq);
     const unsigned long long all_rows = (unsigned long long)s.queries * z.group;
     if (t.at >= all_rows) return;
     const unsigned first_query = (unsigned)(t.at / z.group), skip = (unsigned)(t.at % z.group);  // the tile's rows begin `skip` rows into its first query's
     const unsigned rows = all_rows - t.at < kTileRows ? (unsigned)(all_rows - t.at) : kTileRows;
-    const unsigned wave = threadIdx.x / 64u, l = threadIdx.x % 64u, half = l / 32u, row = wave * 32u + l % 32u;
+    const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), l = threadIdx.x % 64u, half = l / 32u, row = wave * 32u + l % 32u;
     const long long hidden_from = (long long)s.keys - s.queries + 1;  // query i sees keys below i + this
 
     const unsigned head0 = kv * z.group;
@@ -252,7 +267,7 @@ __global__ __launch_bounds__(256) void k_attention_forward(AttentionSizes z, Hea
     for (unsigned i = 0; i < DP / 16; ++i) bq[i] = load16(from_q, row_offset(skip + row, skip + rows, z.group, q.ld, 16u * i + 8u * half, z.dim));
 
     // keys that a row sees, that all of the tile's together see, and that each of the wave's sees
-    const auto seen = [&](unsigned r) -> unsigned {
+    const auto seen = [&](unsigned r) __attribute__((always_inline)) -> unsigned {
         if (!z.causal) return s.keys;
         const long long n = (long long)(first_query + (skip + r) / z.group) + hidden_from;
         return n < 0 ? 0u : n < (long long)s.keys ? (unsigned)n : s.keys;
@@ -266,27 +281,30 @@ __global__ __launch_bounds__(256) void k_attention_forward(AttentionSizes z, Hea
     }
 
     f16v acc[DP / 32] = {};
-    float most = -kInfinity, total = 0.0f;
-    const float c = z.scale * kLog2e;
-    Staged<DP, kTileKeys> sk, sv;
-    const auto ask = [&](unsigned j) {
-        const unsigned left = s.keys - j;
-        sk.load(buffer_at(k.p + (size_t)(s.k0 + j) * k.ld + kv * z.dim), left, 1u, k.ld, z.dim);
-        sv.load(buffer_at(v.p + (size_t)(s.k0 + j) * v.ld + kv * z.dim), left, 1u, v.ld, z.dim);
+    // P is formed as 2^(S c + shift), shift = lift - top c with the row's largest S so far: `top` stays where it is until a row has one that is
+    // larger by more than a factor of 2^kSlack, so that what is there has to be multiplied in the first tiles alone.
+    float top = -kInfinity, shift = 0.0f, total = 0.0f;
+    const float c = z.scale * kLog2e, slack = kSlack / c;
+    const TileLoads<DP, kTileKeys, 4> loads_k(wave, 1u, k.ld, z.dim), loads_v(wave, 1u, v.ld, z.dim);
+    const auto ask = [&](unsigned j, unsigned b) __attribute__((always_inline)) {
+        const unsigned left = s.keys - j < kTileKeys ? s.keys - j : kTileKeys;
+        loads_k.ask(lds + b * 2u * kTile, wave, k.p + (size_t)(s.k0 + j) * k.ld + kv * z.dim, ((left - 1u) * k.ld + z.dim) * 2u);
+        loads_v.ask(lds + b * 2u * kTile + kTile, wave, v.p + (size_t)(s.k0 + j) * v.ld + kv * z.dim, ((left - 1u) * v.ld + z.dim) * 2u);
     };
-    if (from < to) ask(from);
+    unsigned buffer = 0;
+    if (from < to) ask(from, 0);
     for (unsigned j = from; j < to; j += kTileKeys) {
+        wait_for_loads<0>();
         __syncthreads();
-        sk.store(tile_k);
-        sv.store(tile_v);
-        __syncthreads();
-        if (j + kTileKeys < to) ask(j + kTileKeys);
+        if (j + kTileKeys < to) ask(j + kTileKeys, buffer ^ 1u);
+        const Lds tile_k = lds + buffer * 2u * kTile, tile_v = tile_k + kTile;
+        buffer ^= 1u;
         if (wave * 32u >= rows) continue;
         f16v x[2] = {};
 #pragma unroll
-        for (unsigned b = 0; b < 2; ++b)
+        for (unsigned i = 0; i < DP / 16; ++i)
 #pragma unroll
-            for (unsigned i = 0; i < DP / 16; ++i) x[b] = mfma<DT>(rows_operand<DP>(tile_k, 32u * b, i), bq[i], x[b]);
+            for (unsigned b = 0; b < 2; ++b) x[b] = mfma<DT>(rows_operand<DP>(tile_k, 32u * b, i), bq[i], x[b]);
         if (j + kTileKeys > least) {
 #pragma unroll
             for (unsigned b = 0; b < 2; ++b)
@@ -294,29 +312,35 @@ __global__ __launch_bounds__(256) void k_attention_forward(AttentionSizes z, Hea
                 for (unsigned r = 0; r < 16; ++r)
                     if (j + 32u * b + row_of(r, half) >= mine) x[b][r] = -kInfinity;
         }
-        float top = x[0][0];
+        float most = x[0][0];
 #pragma unroll
-        for (unsigned r = 1; r < 32; ++r) top = __builtin_fmaxf(top, x[r / 16][r % 16]);
-        top = __builtin_fmaxf(top, other_half(top));
-        // (differences first: of logits far from 0 the product with c would lose more than what is left)
-        const float now = __builtin_fmaxf(most, top), base = now == -kInfinity ? 0.0f : now;
-        const float keep = __builtin_amdgcn_exp2f((most - base) * c);
-        most = now;
-        float sum = 0.0f;
+        for (unsigned r = 1; r < 32; ++r) most = __builtin_fmaxf(most, x[r / 16][r % 16]);
+        most = __builtin_fmaxf(most, other_half(most));
+        if (__builtin_amdgcn_ballot_w64(!(most <= top + slack)) != 0) {
+            const float now = __builtin_fmaxf(most, top), next = now == -kInfinity ? 0.0f : kLift<DT> - now * c;
+            // (of logits far from 0 the product with c loses more than what is left: differences first)
+            const float keep = top == -kInfinity ? 0.0f : __builtin_fabsf(next) > kFar ? __builtin_amdgcn_exp2f((top - now) * c) : __builtin_amdgcn_exp2f(next - shift);
+            top = now, shift = next;
+            total *= keep;
 #pragma unroll
-        for (unsigned b = 0; b < 2; ++b)
+            for (unsigned d = 0; d < DP / 32; ++d) acc[d] *= keep;
+        }
+        float add = shift;
+        if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(shift) > kFar) != 0) {
+            const float base = top == -kInfinity ? 0.0f : top;
+            add = kLift<DT>;
 #pragma unroll
-            for (unsigned r = 0; r < 16; ++r) {
-                x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r] - base, c, kLift<DT>));
-                sum += x[b][r];
-            }
-        total = __builtin_fmaf(total, keep, sum);
-#pragma unroll
-        for (unsigned d = 0; d < DP / 32; ++d) acc[d] *= keep;
+            for (unsigned r = 0; r < 32; ++r) x[r / 16][r % 16] -= base;
+        }
 #pragma unroll
         for (unsigned b = 0; b < 2; ++b)
 #pragma unroll
             for (unsigned h = 0; h < 2; ++h) {
+#pragma unroll
+                for (unsigned r = 8 * h; r < 8 * h + 8; ++r) {
+                    x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r], c, add));
+                    total += x[b][r];
+                }
                 const s8v p = rounded<DT>(x[b], h);
 #pragma unroll
                 for (unsigned d = 0; d < DP / 32; ++d) acc[d] = mfma<DT>(columns_operand<DP>(tile_v, 32u * b + 16u * h, d), p, acc[d]);
@@ -325,7 +349,8 @@ __global__ __launch_bounds__(256) void k_attention_forward(AttentionSizes z, Hea
     total += other_half(total);
     if (row >= rows) return;
     const unsigned query = first_query + (skip + row) / z.group, head = head0 + (skip + row) % z.group;
-    const float f = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total, log_sum = total == 0.0f ? -kInfinity : most * z.scale + __builtin_logf(total * (1.0f / kLifted<DT>));
+    const float f = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+    const float log_sum = total == 0.0f ? -kInfinity : (__builtin_log2f(total) - shift) * 0.693147180559945f;
     if (splits > 1u) {
         const size_t at = (((size_t)split * z.kv_heads + kv) * z.tokens_q + s.q0 + query) * z.group + head - head0;
         store_row<kGradF32, DP>(parts + at * DP, acc, f, DP);
@@ -336,31 +361,52 @@ __global__ __launch_bounds__(256) void k_attention_forward(AttentionSizes z, Hea
     }
 }
 
-// A row's parts, joined: a wave to a row.
+// A row's parts, joined: a group to a row, whose waves take every fourth part each.
 template <int DT, int DP>
 __global__ __launch_bounds__(256) void k_attention_join(AttentionSizes z, Heads<Elem<DT>> out, float *__restrict__ lse, unsigned splits,
                                                         const float *__restrict__ parts, const float *__restrict__ part_lse)
 {
-    const size_t rows = (size_t)z.kv_heads * z.tokens_q * z.group, row = (size_t)blockIdx.x * 4u + threadIdx.x / 64u;
-    if (row >= rows) return;
-    const unsigned lane = threadIdx.x % 64u, query = (unsigned)(row / z.group % z.tokens_q);
+    constexpr unsigned kEach = DP / 64;
+    __shared__ float weight[kMostSplits], sums[4][DP];
+    const size_t rows = (size_t)z.kv_heads * z.tokens_q * z.group, row = blockIdx.x;
+    const unsigned wave = threadIdx.x / 64u, lane = threadIdx.x % 64u, query = (unsigned)(row / z.group % z.tokens_q);
     const unsigned head = (unsigned)(row / z.group / z.tokens_q) * z.group + (unsigned)(row % z.group);
     if (z.starts_q && (query < cut(z.starts_q[0], 0u, z.tokens_q) || query >= cut(z.starts_q[z.num_seqs], 0u, z.tokens_q))) return;
-    float most = -kInfinity;
-    for (unsigned i = 0; i < splits; ++i) most = __builtin_fmaxf(most, part_lse[i * rows + row]);
-    const float base = most == -kInfinity ? 0.0f : most;
-    float total = 0.0f, sum[DP / 64] = {};
-    for (unsigned i = 0; i < splits; ++i) {
-        const float w = __builtin_amdgcn_exp2f((part_lse[i * rows + row] - base) * kLog2e);
-        total += w;
+    float mine[kMostSplits / 64], most = -kInfinity, total = 0.0f;
 #pragma unroll
-        for (unsigned k = 0; k < DP / 64; ++k) sum[k] = __builtin_fmaf(w, parts[(i * rows + row) * DP + k * 64u + lane], sum[k]);
+    for (unsigned i = 0; i < kMostSplits / 64; ++i) {
+        const unsigned p = i * 64u + lane;
+        mine[i] = p < splits ? part_lse[p * rows + row] : -kInfinity;
+        most = __builtin_fmaxf(most, mine[i]);
     }
-    const float f = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
 #pragma unroll
-    for (unsigned k = 0; k < DP / 64; ++k)
-        if (k * 64u + lane < z.dim) out.p[(size_t)query * out.ld + head * z.dim + k * 64u + lane] = (Elem<DT>)(sum[k] * f);
-    if (lse && lane == 0u) lse[(size_t)head * z.tokens_q + query] = total == 0.0f ? -kInfinity : base + __builtin_logf(total);
+    for (int m = 1; m < 64; m *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, m));
+    const float base = most == -kInfinity ? 0.0f : most;
+#pragma unroll
+    for (unsigned i = 0; i < kMostSplits / 64; ++i) {
+        mine[i] = __builtin_amdgcn_exp2f((mine[i] - base) * kLog2e);
+        total += mine[i];
+        if (wave == 0u) weight[i * 64u + lane] = mine[i];
+    }
+    total = wave_sum(total);
+    __syncthreads();
+    float sum[kEach] = {};
+    const float *at = parts + row * DP + lane * kEach;
+#pragma unroll 8
+    for (unsigned i = wave; i < splits; i += 4u) {
+        const Few<kGradF32, (int)kEach> x = *reinterpret_cast<const Few<kGradF32, (int)kEach> *>(at + i * rows * DP);
+#pragma unroll
+        for (unsigned k = 0; k < kEach; ++k) sum[k] = __builtin_fmaf(weight[i], x.v[k], sum[k]);
+    }
+#pragma unroll
+    for (unsigned k = 0; k < kEach; ++k) sums[wave][lane * kEach + k] = sum[k];
+    __syncthreads();
+    const unsigned d = threadIdx.x;
+    if (d < z.dim) {
+        const float f = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+        out.p[(size_t)query * out.ld + head * z.dim + d] = (Elem<DT>)((sums[0][d] + sums[1][d] + (sums[2][d] + sums[3][d])) * f);
+    }
+    if (lse && d == 0u) lse[(size_t)head * z.tokens_q + query] = total == 0.0f ? -kInfinity : base + __builtin_logf(total);
 }
 
 // ---------------------------------------------------------------------------
@@ -373,22 +419,26 @@ __device__ __forceinline__ float to_one(float most)
     return e == 0u || e > 253u ? 1.0f : __builtin_bit_cast(float, (254u - e) << 23);
 }
 
-// dq.  delta receives dout . out of every row, and size (of fp16 tensors) the largest magnitude in dout, both [heads][tokens_q].
+// dq.  For the next kernel row_lse receives lse of every row, times log2 e and less the lift, delta dout . out, and size (of fp16 tensors) the
+// largest magnitude in dout, all [kv head][token][head of the group].
 template <int DT, int DP>
-__global__ __launch_bounds__(256) void k_attention_dq(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
+__global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
                                                       Heads<const Elem<DT>> v, Heads<const Elem<DT>> out, const float *__restrict__ lse,
-                                                      Heads<Elem<DT>> dq, float *__restrict__ delta, float *__restrict__ size)
+                                                      Heads<Elem<DT>> dq, float *__restrict__ row_lse, float *__restrict__ delta,
+                                                      float *__restrict__ size)
 {
-    __shared__ __align__(1024) unsigned char tile_k[kTileKeys * DP * 2], tile_v[kTileKeys * DP * 2];
+    constexpr unsigned kTile = kTileKeys * DP * 2;
+    __shared__ __align__(1024) unsigned char smem[4 * kTile];  // two tiles of keys and of values
+    const Lds lds = (Lds)smem;
     const unsigned kv = blockIdx.x % z.kv_heads;
-    const Tile t = tile_of(z.starts_q, z.tokens_q, z.num_seqs, z.group, kTileRows,
+    const TileAt t = tile_of(z.starts_q, z.tokens_q, z.num_seqs, z.group, kTileRows,
                            tiles_over(z.tokens_q, z.num_seqs, z.group, kTileRows) - 1u - blockIdx.x / z.kv_heads);
     const Sequence s = sequence_of(z, t.seq);
     const unsigned long long all_rows = (unsigned long long)s.queries * z.group;
     if (t.at >= all_rows) return;
     const unsigned first_query = (unsigned)(t.at / z.group), skip = (unsigned)(t.at % z.group);
     const unsigned rows = all_rows - t.at < kTileRows ? (unsigned)(all_rows - t.at) : kTileRows;
-    const unsigned wave = threadIdx.x / 64u, l = threadIdx.x % 64u, half = l / 32u, row = wave * 32u + l % 32u;
+    const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), l = threadIdx.x % 64u, half = l / 32u, row = wave * 32u + l % 32u;
     const long long hidden_from = (long long)s.keys - s.queries + 1;
     const unsigned head0 = kv * z.group, query = first_query + (skip + row) / z.group, head = head0 + (skip + row) % z.group;
     const size_t token = s.q0 + first_query, at = (size_t)head * z.tokens_q + s.q0 + query;
@@ -418,11 +468,13 @@ __global__ __launch_bounds__(256) void k_attention_dq(AttentionSizes z, Heads<co
     const float log_sum = row < rows ? lse[at] : kInfinity, base = log_sum == -kInfinity ? kInfinity : log_sum * kLog2e;
     const float up = DT == kGradF16 ? to_one(largest) : 1.0f;
     if (row < rows && half == 0u) {
-        delta[at] = sum;
-        if (DT == kGradF16) size[at] = largest;
+        const size_t place = ((size_t)kv * z.tokens_q + s.q0 + query) * z.group + head - head0;
+        row_lse[place] = base - kLiftBack<DT>;
+        delta[place] = sum;
+        if (DT == kGradF16) size[place] = largest;
     }
 
-    const auto seen = [&](unsigned r) -> unsigned {
+    const auto seen = [&](unsigned r) __attribute__((always_inline)) -> unsigned {
         if (!z.causal) return s.keys;
         const long long n = (long long)(first_query + (skip + r) / z.group) + hidden_from;
         return n < 0 ? 0u : n < (long long)s.keys ? (unsigned)n : s.keys;
@@ -430,19 +482,20 @@ __global__ __launch_bounds__(256) void k_attention_dq(AttentionSizes z, Heads<co
     const unsigned mine = row < rows ? seen(row) : 0u, to = seen(rows - 1u), least = (unsigned)__builtin_amdgcn_readfirstlane((int)seen(wave * 32u));
     f16v acc[DP / 32] = {};
     const float c = z.scale * kLog2e;
-    Staged<DP, kTileKeys> sk, sv;
-    const auto ask = [&](unsigned j) {
-        const unsigned left = s.keys - j;
-        sk.load(buffer_at(k.p + (size_t)(s.k0 + j) * k.ld + kv * z.dim), left, 1u, k.ld, z.dim);
-        sv.load(buffer_at(v.p + (size_t)(s.k0 + j) * v.ld + kv * z.dim), left, 1u, v.ld, z.dim);
+    const TileLoads<DP, kTileKeys, 4> loads_k(wave, 1u, k.ld, z.dim), loads_v(wave, 1u, v.ld, z.dim);
+    const auto ask = [&](unsigned j, unsigned b) __attribute__((always_inline)) {
+        const unsigned left = s.keys - j < kTileKeys ? s.keys - j : kTileKeys;
+        loads_k.ask(lds + b * 2u * kTile, wave, k.p + (size_t)(s.k0 + j) * k.ld + kv * z.dim, ((left - 1u) * k.ld + z.dim) * 2u);
+        loads_v.ask(lds + b * 2u * kTile + kTile, wave, v.p + (size_t)(s.k0 + j) * v.ld + kv * z.dim, ((left - 1u) * v.ld + z.dim) * 2u);
     };
-    if (to) ask(0);
+    unsigned buffer = 0;
+    if (to) ask(0, 0);
     for (unsigned j = 0; j < to; j += kTileKeys) {
+        wait_for_loads<0>();
         __syncthreads();
-        sk.store(tile_k);
-        sv.store(tile_v);
-        __syncthreads();
-        if (j + kTileKeys < to) ask(j + kTileKeys);
+        if (j + kTileKeys < to) ask(j + kTileKeys, buffer ^ 1u);
+        const Lds tile_k = lds + buffer * 2u * kTile, tile_v = tile_k + kTile;
+        buffer ^= 1u;
         if (wave * 32u >= rows) continue;
 #pragma unroll
         for (unsigned b = 0; b < 2; ++b) {
@@ -451,10 +504,14 @@ __global__ __launch_bounds__(256) void k_attention_dq(AttentionSizes z, Heads<co
             for (unsigned i = 0; i < DP / 16; ++i) x = mfma<DT>(rows_operand<DP>(tile_k, 32u * b, i), bq[i], x);
 #pragma unroll
             for (unsigned i = 0; i < DP / 16; ++i) y = mfma<DT>(rows_operand<DP>(tile_v, 32u * b, i), bd[i], y);
+            if (j + kTileKeys > least) {
+#pragma unroll
+                for (unsigned r = 0; r < 16; ++r)
+                    if (j + 32u * b + row_of(r, half) >= mine) x[r] = -kInfinity, y[r] = 0.0f;
+            }
 #pragma unroll
             for (unsigned r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -base));
-                y[r] = j + kTileKeys > least && j + 32u * b + row_of(r, half) >= mine ? 0.0f : p * ((y[r] - sum) * up);
+                y[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -base)) * ((y[r] - sum) * up);
             }
 #pragma unroll
             for (unsigned h = 0; h < 2; ++h) {
@@ -469,32 +526,45 @@ __global__ __launch_bounds__(256) void k_attention_dq(AttentionSizes z, Heads<co
 
 // dk and dv: a group takes 128 keys of one key head, and runs over the rows that see them.
 template <int DT, int DP>
-__global__ __launch_bounds__(256) void k_attention_dkv(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
-                                                       Heads<const Elem<DT>> v, const float *__restrict__ lse, const float *__restrict__ delta,
+__global__ __launch_bounds__(256, 2) void k_attention_dkv(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
+                                                       Heads<const Elem<DT>> v, const float *__restrict__ all_lse, const float *__restrict__ delta,
                                                        const float *__restrict__ size, Heads<Elem<DT>> dk, Heads<Elem<DT>> dv)
 {
-    constexpr unsigned kRows = kTileKeys;  // of queries at a time
-    __shared__ __align__(1024) unsigned char tile_q[kRows * DP * 2], tile_d[kRows * DP * 2];
-    __shared__ __align__(16) float row_lse[kRows], row_delta[kRows], row_size[kRows];
+    // Two groups to a compute unit: of 128 elements a head, a wave's registers hold its keys and both results, but not its values too, which are
+    // read from LDS, where the rows of queries make room for them.
+    constexpr bool kValuesInLds = DP == 128;
+    constexpr unsigned kRows = kValuesInLds ? 32 : 64;  // of queries at a time
+    constexpr unsigned kTile = kRows * DP * 2, kStage = 2 * kTile + 1024;
+    __shared__ __align__(1024) unsigned char smem[2 * kStage + (kValuesInLds ? kTileRows * DP * 2 : 0)];  // twice a tile of q, one of dout, and three numbers of each row
+    const Lds lds = (Lds)smem, values = lds + 2u * kStage;
     const unsigned kv = blockIdx.x % z.kv_heads;
     const int *starts = z.starts_k ? z.starts_k : z.starts_q;
-    const Tile t = tile_of(starts, z.tokens_k, z.num_seqs, 1u, kTileRows, blockIdx.x / z.kv_heads);
+    const TileAt t = tile_of(starts, z.tokens_k, z.num_seqs, 1u, kTileRows, blockIdx.x / z.kv_heads);
     const Sequence s = sequence_of(z, t.seq);
     if (t.at >= s.keys) return;
     const unsigned key0 = (unsigned)t.at, keys = s.keys - key0 < kTileRows ? s.keys - key0 : kTileRows;
-    const unsigned wave = threadIdx.x / 64u, l = threadIdx.x % 64u, half = l / 32u, key = wave * 32u + l % 32u, head0 = kv * z.group;
+    const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), l = threadIdx.x % 64u, half = l / 32u, key = wave * 32u + l % 32u;
+    const unsigned head0 = kv * z.group;
 
     const __amdgpu_buffer_rsrc_t from_k = buffer_at(k.p + (size_t)(s.k0 + key0) * k.ld + kv * z.dim);
     const __amdgpu_buffer_rsrc_t from_v = buffer_at(v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim);
-    s8v bk[DP / 16], bv[DP / 16];
+    s8v bk[DP / 16], bv[kValuesInLds ? 1 : DP / 16];
 #pragma unroll
     for (unsigned i = 0; i < DP / 16; ++i) {
         bk[i] = load16(from_k, row_offset(key, keys, 1u, k.ld, 16u * i + 8u * half, z.dim));
-        bv[i] = load16(from_v, row_offset(key, keys, 1u, v.ld, 16u * i + 8u * half, z.dim));
+        if constexpr (!kValuesInLds) bv[i] = load16(from_v, row_offset(key, keys, 1u, v.ld, 16u * i + 8u * half, z.dim));
     }
+    if constexpr (kValuesInLds) {
+        const TileLoads<DP, kTileRows, 4> loads_v(wave, 1u, v.ld, z.dim);
+        loads_v.ask(values, wave, v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim, ((keys - 1u) * v.ld + z.dim) * 2u);
+    }
+    const auto value = [&](unsigned i) __attribute__((always_inline)) {
+        if constexpr (kValuesInLds) return rows_operand<DP>(values, wave * 32u, i);
+        else return bv[i];
+    };
     // the first query that sees key j is j - (keys - queries)
     const long long later = (long long)s.queries - s.keys;
-    const auto first_of = [&](unsigned j) -> unsigned {
+    const auto first_of = [&](unsigned j) __attribute__((always_inline)) -> unsigned {
         const long long i = (long long)j + later;
         return !z.causal || i < 0 ? 0u : i < (long long)s.queries ? (unsigned)i : s.queries;
     };
@@ -504,44 +574,37 @@ __global__ __launch_bounds__(256) void k_attention_dkv(AttentionSizes z, Heads<c
     bool begun = false;
     // queries at a time: as many as have kRows rows at most, or a part of one query's heads
     const unsigned group = z.group, at_once = group < kRows ? kRows / group : 1u;
-    Staged<DP, kRows> sq, sd;
-    float next_lse = 0.0f, next_delta = 0.0f, next_size = 0.0f;
-    const auto ask = [&](unsigned i, unsigned part) {
-        const unsigned queries = s.queries - i < at_once ? s.queries - i : at_once, left = group - part < kRows ? group - part : kRows;
-        const unsigned rows = group < kRows ? queries * group : left;
-        sq.load(buffer_at(q.p + (size_t)(s.q0 + i) * q.ld + (head0 + part) * z.dim), rows, group, q.ld, z.dim);
-        sd.load(buffer_at(dout.p + (size_t)(s.q0 + i) * dout.ld + (head0 + part) * z.dim), rows, group, dout.ld, z.dim);
-        if (threadIdx.x < kRows) {
-            const unsigned r = threadIdx.x;
-            const size_t at = (size_t)(head0 + part + r % group) * z.tokens_q + s.q0 + i + r / group;
-            const float x = r < rows ? lse[at] : kInfinity;
-            next_lse = x == -kInfinity ? kInfinity : x * kLog2e - kLift<DT>;
-            next_delta = r < rows ? delta[at] : 0.0f;
-            next_size = DT == kGradF16 && r < rows ? size[at] : 0.0f;
+    const TileLoads<DP, kRows, 4> loads_q(wave, group, q.ld, z.dim), loads_d(wave, group, dout.ld, z.dim);
+    // (values, not one of three variables: the compiler would keep those in memory)
+    const float *const numbers = wave == 0u ? +all_lse : wave == 1u ? +delta : +size;
+    const auto ask = [&](unsigned i, unsigned part, unsigned b) __attribute__((always_inline)) {
+        const unsigned queries = s.queries - i < at_once ? s.queries - i : at_once, heads = group - part < kRows ? group - part : kRows;
+        const Lds to = lds + b * kStage;
+        loads_q.ask(to, wave, q.p + (size_t)(s.q0 + i) * q.ld + (head0 + part) * z.dim, ((queries - 1u) * q.ld + heads * z.dim) * 2u);
+        loads_d.ask(to + kTile, wave, dout.p + (size_t)(s.q0 + i) * dout.ld + (head0 + part) * z.dim, ((queries - 1u) * dout.ld + heads * z.dim) * 2u);
+        if (wave < (DT == kGradF16 ? 3u : 2u)) {
+            load_to_lds<4>(same_in_all(buffer_of(numbers + ((size_t)kv * z.tokens_q + s.q0 + i) * group + part, queries * heads * 4u)), to + 2u * kTile + wave * 256u, l * 4u);
         }
     };
-    unsigned i = first_of(key0), part = 0;
-    if (i < s.queries) ask(i, part);
+    unsigned i = first_of(key0), part = 0, buffer = 0;
+    if (i < s.queries) ask(i, part, 0);
     while (i < s.queries) {
-        __syncthreads();
-        sq.store(tile_q);
-        sd.store(tile_d);
-        if (threadIdx.x < kRows) {
-            row_lse[threadIdx.x] = next_lse;
-            row_delta[threadIdx.x] = next_delta;
-            row_size[threadIdx.x] = next_size;
-        }
+        wait_for_loads<0>();
         __syncthreads();
         const unsigned now = i;
         if (group < kRows || part + kRows >= group) i += at_once, part = 0;
         else part += kRows;
-        if (i < s.queries) ask(i, part);
+        if (i < s.queries) ask(i, part, buffer ^ 1u);
+        const Lds tile_q = lds + buffer * kStage, tile_d = tile_q + kTile;
+        const CDSGD_LDS float *row_lse = (const CDSGD_LDS float *)(tile_d + kTile), *row_delta = row_lse + 64, *row_size = row_lse + 128;
+        buffer ^= 1u;
         if (wave * 32u >= keys) continue;
         if constexpr (DT == kGradF16) {
-            static_assert(kRows == 64, "a lane looks at a row");
-            float largest = row_size[l];
+            static_assert(kRows <= 64, "a lane looks at a row");
+            float largest = row_size[l % kRows];
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) largest = __builtin_fmaxf(largest, __shfl_xor(largest, m));
+            largest = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, largest)));
             const float want = to_one(largest);
             if (largest > 0.0f && (!begun || want < up)) {
                 if (begun) {
@@ -554,19 +617,28 @@ __global__ __launch_bounds__(256) void k_attention_dkv(AttentionSizes z, Heads<c
         }
         // (every row of the tile sees every key of the wave, but for causal tiles on the border)
         const bool border = z.causal && first_of(key0 + wave * 32u + 31u) > now;
+        const unsigned first = first_of(key0 + key), hidden = first <= now ? 0u : group < kRows ? (first - now) * group : kRows;  // rows of the tile
 #pragma unroll
         for (unsigned b = 0; b < kRows / 32; ++b) {
             f16v x = {}, y = {};
 #pragma unroll
             for (unsigned e = 0; e < DP / 16; ++e) x = mfma<DT>(rows_operand<DP>(tile_q, 32u * b, e), bk[e], x);
 #pragma unroll
-            for (unsigned e = 0; e < DP / 16; ++e) y = mfma<DT>(rows_operand<DP>(tile_d, 32u * b, e), bv[e], y);
+            for (unsigned e = 0; e < DP / 16; ++e) y = mfma<DT>(rows_operand<DP>(tile_d, 32u * b, e), value(e), y);
+            if (border) {
 #pragma unroll
-            for (unsigned r = 0; r < 16; ++r) {
-                const unsigned row = 32u * b + row_of(r, half);
-                const bool hidden = border && now + (group < kRows ? row / group : 0u) < first_of(key0 + key);
-                x[r] = hidden ? 0.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -row_lse[row]));
-                y[r] = hidden ? 0.0f : x[r] * ((y[r] - row_delta[row]) * (up * (1.0f / kLifted<DT>)));
+                for (unsigned r = 0; r < 16; ++r)
+                    if (32u * b + row_of(r, half) < hidden) x[r] = -kInfinity, y[r] = 0.0f;
+            }
+            const float down = up * (1.0f / kLifted<DT>);
+#pragma unroll
+            for (unsigned r = 0; r < 16; r += 4) {
+                const f4 base = *(const CDSGD_LDS f4 *)(row_lse + 32u * b + row_of(r, half)), sum = *(const CDSGD_LDS f4 *)(row_delta + 32u * b + row_of(r, half));
+#pragma unroll
+                for (unsigned e = 0; e < 4; ++e) {
+                    x[r + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r + e], c, -base[e]));
+                    y[r + e] = x[r + e] * ((y[r + e] - sum[e]) * down);
+                }
             }
 #pragma unroll
             for (unsigned h = 0; h < 2; ++h) {

@@ -161,11 +161,11 @@ def test_attention_forward_refuses(L, want, batch, over):
 
 @pytest.mark.parametrize("want,batch,over", [(w, b, {}) for w, b in BAD_BATCHES] + [(w, {}, o) for w, o in [
     (B.ERR_NULL, dict(dout=None)), (B.ERR_NULL, dict(out=None)), (B.ERR_NULL, dict(lse=None)), (B.ERR_NULL, dict(dq=None)), (B.ERR_NULL, dict(dk=None)),
-    (B.ERR_NULL, dict(dv=None)), (B.ERR_NULL, dict(room=None)), (B.ERR_SIZE, dict(room_bytes=100 * 8 * 8 - 1)), (B.ERR_ALIGN, dict(room=at(9) + 8)),
+    (B.ERR_NULL, dict(dv=None)), (B.ERR_NULL, dict(room=None)), (B.ERR_SIZE, dict(room_bytes=100 * 8 * 12 - 1)), (B.ERR_ALIGN, dict(room=at(9) + 8)),
     (B.ERR_ALIAS, dict(dq=at(5))), (B.ERR_ALIAS, dict(dk=at(7))), (B.ERR_ALIAS, dict(dk=at(8) + 128)), (B.ERR_ALIAS, dict(dv=at(0))), (B.ERR_ALIAS, dict(dk=at(4))),
     (B.ERR_ALIAS, dict(room=at(3))), (B.ERR_ALIAS, dict(dk=at(30)))]])
 def test_attention_backward_refuses(L, want, batch, over):
-    v = dict(q=at(0), k=at(1), v=at(2), out=at(3), lse=at(4), dout=at(5), dq=at(6), dk=at(7), dv=at(8), room=at(9), room_bytes=100 * 8 * 8)
+    v = dict(q=at(0), k=at(1), v=at(2), out=at(3), lse=at(4), dout=at(5), dq=at(6), dk=at(7), dv=at(8), room=at(9), room_bytes=100 * 8 * 12)
     v.update(over)
     if over == dict(dk=at(7)):
         v["dq"] = at(7)

@@ -8,7 +8,8 @@ the terms' magnitudes:
   dS by P |dP - delta| (u + e_P) + 2 U dim P (sum |dout| |v| + sum |dout| |out|), in fp16 also by a step of its smallest numbers under
   the power of two by which it is divided, 2^-24 of the largest magnitude in dout;
   dq by scale sum |k| e_dS + 2 U keys scale sum |dS| |k| + u |dq|, dk and dv alike;
-  and a result of fp16 below its smallest normal number by 2^-25, a probability there, which is rounded times 2^15, by 2^-40.
+  and a result of fp16 below its smallest normal number by 2^-25, a probability there, which is rounded times 2^7
+  in the forward pass and 2^15 in the backward pass, by 2^-32 and 2^-40.
 Numbers whose exponents fp32 (and bf16) have no normal place for, below SMALL = 2^-126, may be 0: P, dS, what they are rounded to, and the results, so that
 SMALL comes on top of the error of each of them, and as a factor of what multiplies it.
 The backward pass is held to its formula at the out and lse that it is given."""
@@ -45,8 +46,8 @@ def tiny(t):
     return 2.0 ** -25 if t.dtype == torch.float16 else SMALL
 
 
-def tiny_p(t):
-    return 2.0 ** -40 if t.dtype == torch.float16 else 0.0
+def tiny_p(t, lift):
+    return 2.0 ** -(25 + lift) if t.dtype == torch.float16 else 0.0
 
 
 def reference(q, k, v, lens_q, lens_k, causal, scale, first_q=0, first_k=0):
@@ -99,7 +100,7 @@ def check_forward(q, k, v, out, lse, lens_q, lens_k, causal, scale, first_q=0, f
             close(torch.where(empty, 0.0, got), torch.where(empty, 0.0, want_lse), worst + 2 * U * (s.shape[2] + 4 * want_lse.masked_fill(empty, 0).abs()),
                   "lse")
         want = torch.matmul(p, z)
-        error = torch.matmul(p * (u + 2 * e + 2 * U * s.shape[2]) + 2 * SMALL + tiny_p(q), z.abs()) + u * want.abs() + tiny(q)
+        error = torch.matmul(p * (u + 2 * e + 2 * U * s.shape[2]) + 2 * SMALL + tiny_p(q, 7), z.abs()) + u * want.abs() + tiny(q)
         close(out[rows, mine].transpose(0, 1), want, error, "out")
 
 
@@ -120,7 +121,7 @@ def check_backward(dout, q, k, v, out, lse, dq, dk, dv, lens_q, lens_k, causal, 
         close(dq[rows, mine].transpose(0, 1), want,
               scale * torch.matmul(e_ds + 2 * U * nk * ds.abs(), y.abs()) + u * want.abs() + tiny(q), "dq")
         n = nq * s.shape[0]
-        for got, w, e_w, other, what, f in ((dk, ds, e_ds, x, "dk", scale), (dv, p, p * (u + e_p) + 2 * SMALL + tiny_p(q), do, "dv", 1.0)):
+        for got, w, e_w, other, what, f in ((dk, ds, e_ds, x, "dk", scale), (dv, p, p * (u + e_p) + 2 * SMALL + tiny_p(q, 15), do, "dv", 1.0)):
             flat = lambda t: t.reshape(n, t.shape[2])  # noqa: E731
             want = f * torch.matmul(flat(w).t().contiguous(), flat(other))
             error = f * torch.matmul((flat(e_w) + 2 * U * n * flat(w).abs()).t().contiguous(), flat(other).abs()) + u * want.abs() + tiny(q)
