@@ -134,6 +134,15 @@ __device__ __forceinline__ s8v load16(__amdgpu_buffer_rsrc_t from, unsigned byte
     return __builtin_bit_cast(s8v, (u4)__builtin_amdgcn_raw_buffer_load_b128(from, (int)bytes, 0, 0));
 }
 
+// What was loaded is there: the compiler, which does not count the loads to LDS, would wait for it where it is first used, and for all of
+// those with it, in every turn of a loop.
+template <int N>
+__device__ __forceinline__ void landed(s8v (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+
 // Byte offset of elements d ... of row `row` (of `rows`) behind the tile's first token.
 __device__ __forceinline__ unsigned row_offset(unsigned row, unsigned rows, unsigned group, unsigned ld, unsigned d, unsigned dim)
 {
@@ -216,7 +225,26 @@ __device__ __forceinline__ s8v rounded(const f16v &x, unsigned t)
     return __builtin_bit_cast(s8v, e);
 }
 
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// x of lane l % 32, and of lane 32 + l % 32.
+struct Halves {
+    float low, high;
+};
+__device__ __forceinline__ Halves halves(float x)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned low = both[0], high = both[1];  // (a cast of an element's bits is one of the first element's to this compiler)
+    return {__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
+}
+__device__ __forceinline__ float sum_of_halves(float x)
+{
+    const Halves h = halves(x);
+    return h.low + h.high;
+}
+__device__ __forceinline__ float larger_half(float x)
+{
+    const Halves h = halves(x);
+    return __builtin_fmaxf(h.low, h.high);
+}
 
 // A row's results, which lie in two lanes four elements at a time, times f and rounded.
 template <int DT, int DP>
@@ -265,6 +293,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(AttentionSizes z, 
     s8v bq[DP / 16];
 #pragma unroll
     for (unsigned i = 0; i < DP / 16; ++i) bq[i] = load16(from_q, row_offset(skip + row, skip + rows, z.group, q.ld, 16u * i + 8u * half, z.dim));
+
+    landed(bq);
 
     // keys that a row sees, that all of the tile's together see, and that each of the wave's sees
     const auto seen = [&](unsigned r) __attribute__((always_inline)) -> unsigned {
@@ -315,7 +345,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(AttentionSizes z, 
         float most = x[0][0];
 #pragma unroll
         for (unsigned r = 1; r < 32; ++r) most = __builtin_fmaxf(most, x[r / 16][r % 16]);
-        most = __builtin_fmaxf(most, other_half(most));
+        most = larger_half(most);
         if (__builtin_amdgcn_ballot_w64(!(most <= top + slack)) != 0) {
             const float now = __builtin_fmaxf(most, top), next = now == -kInfinity ? 0.0f : kLift<DT> - now * c;
             // (of logits far from 0 the product with c loses more than what is left: differences first)
@@ -346,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(AttentionSizes z, 
                 for (unsigned d = 0; d < DP / 32; ++d) acc[d] = mfma<DT>(columns_operand<DP>(tile_v, 32u * b + 16u * h, d), p, acc[d]);
             }
     }
-    total += other_half(total);
+    total = sum_of_halves(total);
     if (row >= rows) return;
     const unsigned query = first_query + (skip + row) / z.group, head = head0 + (skip + row) % z.group;
     const float f = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
@@ -462,11 +492,13 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
             largest = __builtin_fmaxf(largest, __builtin_fabsf((float)g[e]));
         }
     }
-    sum += other_half(sum);
-    largest = __builtin_fmaxf(largest, other_half(largest));
+    sum = sum_of_halves(sum);
+    largest = larger_half(largest);
     // (a row that sees nothing, and one that is not there, has no share in anything)
     const float log_sum = row < rows ? lse[at] : kInfinity, base = log_sum == -kInfinity ? kInfinity : log_sum * kLog2e;
     const float up = DT == kGradF16 ? to_one(largest) : 1.0f;
+    landed(bq);
+    landed(bd);
     if (row < rows && half == 0u) {
         const size_t place = ((size_t)kv * z.tokens_q + s.q0 + query) * z.group + head - head0;
         row_lse[place] = base - kLiftBack<DT>;
@@ -562,6 +594,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttentionSizes z, Head
         if constexpr (kValuesInLds) return rows_operand<DP>(values, wave * 32u, i);
         else return bv[i];
     };
+    landed(bk);
+    if constexpr (!kValuesInLds) landed(bv);
     // the first query that sees key j is j - (keys - queries)
     const long long later = (long long)s.queries - s.keys;
     const auto first_of = [&](unsigned j) __attribute__((always_inline)) -> unsigned {
