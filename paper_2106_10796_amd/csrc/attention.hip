@@ -18,16 +18,16 @@
 namespace {
 
 // Groups in a row of tiles: a launch's, for one split.
-inline unsigned long long groups_over(size_t tokens, size_t num_seqs, size_t each, size_t kv_heads)
+inline unsigned long long groups_over(size_t tokens, size_t num_seqs, size_t each, size_t tile, size_t kv_heads)
 {
-    return ((unsigned long long)tokens * each / kTileRows + num_seqs) * kv_heads;
+    return ((unsigned long long)tokens * each / tile + num_seqs) * kv_heads;
 }
 
 // Over how many groups the keys of a row are split: where the rows alone do not fill the card, as many as fill it twice, none of them
 // with fewer keys (of a sequence of ordinary length) than four tiles.
 inline unsigned splits_of(const cdsgd_attention &b)
 {
-    const unsigned long long groups = groups_over(b.tokens_q, b.num_seqs, (size_t)(b.heads / b.kv_heads), (size_t)b.kv_heads);
+    const unsigned long long groups = groups_over(b.tokens_q, b.num_seqs, (size_t)(b.heads / b.kv_heads), kTileRows, (size_t)b.kv_heads);
     if (groups >= 256) return 1;
     const unsigned long long want = (511 + groups) / groups, most = b.tokens_k / b.num_seqs / (4 * kTileKeys);
     static_assert(kMostSplits >= 512, "of 512 groups all may share one row's keys");
@@ -48,8 +48,8 @@ int check_batch(const cdsgd_attention *a)
     if (a->heads % a->kv_heads) return CDSGD_ERR_PARAM;
     if (!aligned(a->starts_q, 4) || !aligned(a->starts_k, 4)) return CDSGD_ERR_ALIGN;
     const size_t group = (size_t)(a->heads / a->kv_heads);
-    if ((groups_over(a->tokens_q, a->num_seqs, group, (size_t)a->kv_heads) * splits_of(*a)) >> 24 ||
-        groups_over(a->tokens_k, a->num_seqs, 1, (size_t)a->kv_heads) >> 24)
+    if ((groups_over(a->tokens_q, a->num_seqs, group, kTileRows, (size_t)a->kv_heads) * splits_of(*a)) >> 23 ||
+        groups_over(a->tokens_k, a->num_seqs, 1, kStreamKeys<64>, (size_t)a->kv_heads) >> 23)
         return CDSGD_ERR_SIZE;
     return CDSGD_OK;
 }
@@ -132,7 +132,7 @@ int cdsgd_attention_forward(const cdsgd_attention *batch, const void *q, size_t 
     if (any_overlap(outs, num_out, in, num_in)) return CDSGD_ERR_ALIAS;
     const AttentionSizes z = sizes_of(a);
     const unsigned splits = splits_of(a);
-    const unsigned groups = (unsigned)groups_over(a.tokens_q, a.num_seqs, z.group, z.kv_heads) * splits;
+    const unsigned groups = (unsigned)groups_over(a.tokens_q, a.num_seqs, z.group, kTileRows, z.kv_heads) * splits;
     hipStream_t stream = (hipStream_t)hip_stream;
     with_kernel(a, [&](auto dt, auto dim) {
         constexpr int DT = decltype(dt)::value, DP = decltype(dim)::value;
@@ -172,10 +172,10 @@ int cdsgd_attention_backward(const cdsgd_attention *batch, const void *dout, siz
     with_kernel(a, [&](auto dt, auto dim) {
         constexpr int DT = decltype(dt)::value, DP = decltype(dim)::value;
         float *const row_lse = static_cast<float *>(workspace), *const delta = row_lse + rows, *const size = delta + rows;
-        hipLaunchKernelGGL((k_attention_dq<DT, DP>), dim3((unsigned)groups_over(a.tokens_q, a.num_seqs, z.group, z.kv_heads)), dim3(256), 0, stream, z,
+        hipLaunchKernelGGL((k_attention_dq<DT, DP>), dim3((unsigned)groups_over(a.tokens_q, a.num_seqs, z.group, kTileRows, z.kv_heads)), dim3(256), 0, stream, z,
                            read_of<DT>(dout, ld_dout), read_of<DT>(q, ld_q), read_of<DT>(k, ld_k), read_of<DT>(v, ld_v), read_of<DT>(out, ld_out), lse,
                            write_of<DT>(dq, ld_dq), row_lse, delta, size);
-        hipLaunchKernelGGL((k_attention_dkv<DT, DP>), dim3((unsigned)groups_over(a.tokens_k, a.num_seqs, 1, z.kv_heads)), dim3(256), 0, stream, z,
+        hipLaunchKernelGGL((k_attention_dkv<DT, DP>), dim3((unsigned)groups_over(a.tokens_k, a.num_seqs, 1, kStreamKeys<DP>, z.kv_heads)), dim3(64 * kKeyWaves<DP> * kStreams<DP>), 0, stream, z,
                            read_of<DT>(dout, ld_dout), read_of<DT>(q, ld_q), read_of<DT>(k, ld_k), read_of<DT>(v, ld_v), (const float *)row_lse,
                            (const float *)delta, (const float *)size, write_of<DT>(dk, ld_dk), write_of<DT>(dv, ld_dv));
     });

@@ -185,6 +185,31 @@ __device__ __forceinline__ s8v columns_operand(Lds tile, unsigned row0, unsigned
     return s8v{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 }
 
+// Where a lane finds its operands in a tile: the places of its first ones, from which those of the others differ by a few bits.
+template <int DP>
+struct Operands {
+    unsigned row, column;
+
+    __device__ __forceinline__ Operands()
+    {
+        const unsigned l = threadIdx.x % 64u, at = 16u * (l / 16u % 2u) + 4u * (l % 4u);
+        row = lds_chunk<DP>(l % 32u, l / 32u);
+        column = lds_chunk<DP>(4u * (l / 32u) + l % 16u / 4u, at / 8u) + at % 8u * 2u;
+    }
+    // At the head of a loop: what the others are is worked out where they are read, one instruction each, and not kept in registers across it.
+    __device__ __forceinline__ void renew() { asm volatile("" : "+v"(row), "+v"(column)); }
+    // elements 16 k + 8 (l / 32) ... + 7 of row l % 32 of those that begin at `from`
+    __device__ __forceinline__ s8v rows(Lds from, unsigned k) const { return *(const CDSGD_LDS s8v *)(from + (row ^ k * 32u)); }
+    // column 32 d + l % 32 of rows 4 (l / 32) ... + 3 and 8 + 4 (l / 32) ... + 3 of those
+    __device__ __forceinline__ s8v columns(Lds from, unsigned d) const
+    {
+        typedef CDSGD_LDS s4v *Four;
+        const s4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(from + (column ^ d * 64u)));
+        const s4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(from + 16u * DP + (column ^ (d * 64u | 32u))));
+        return s8v{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    }
+};
+
 // A buffer's description, in scalar registers.
 __device__ __forceinline__ i4s same_in_all(i4s x)
 {
@@ -214,6 +239,18 @@ struct TileLoads {
         for (unsigned i = 0; i < kLoads; ++i) load_to_lds<16>(buffer, tile + (wave * kLoads + i) * 1024u, at[i]);
     }
 };
+
+// The order of what stands before in its block: AHEAD reads of LDS, then COUNT products, each followed by EACH more reads while there are any.
+template <int AHEAD, int COUNT, int EACH>
+__device__ __forceinline__ void reads_ahead()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+    }
+}
 
 // Of the 32 rows of a result, 16 from 16 t on, rounded: a second operand.
 template <int DT>
@@ -335,6 +372,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(AttentionSizes z, 
         for (unsigned i = 0; i < DP / 16; ++i)
 #pragma unroll
             for (unsigned b = 0; b < 2; ++b) x[b] = mfma<DT>(rows_operand<DP>(tile_k, 32u * b, i), bq[i], x[b]);
+        reads_ahead<6, DP / 8, 1>();
         if (j + kTileKeys > least) {
 #pragma unroll
             for (unsigned b = 0; b < 2; ++b)
@@ -449,8 +487,8 @@ __device__ __forceinline__ float to_one(float most)
     return e == 0u || e > 253u ? 1.0f : __builtin_bit_cast(float, (254u - e) << 23);
 }
 
-// dq.  For the next kernel row_lse receives lse of every row, times log2 e and less the lift, delta dout . out, and size (of fp16 tensors) the
-// largest magnitude in dout, all [kv head][token][head of the group].
+// dq.  For the next kernel row_lse receives what S begins with in every row, (lift - lse log2 e) / c, delta -dout . out, and size (of fp16 tensors)
+// the largest magnitude in dout, all [kv head][token][head of the group].
 template <int DT, int DP>
 __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
                                                       Heads<const Elem<DT>> v, Heads<const Elem<DT>> out, const float *__restrict__ lse,
@@ -499,10 +537,11 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
     const float up = DT == kGradF16 ? to_one(largest) : 1.0f;
     landed(bq);
     landed(bd);
+    const float c = z.scale * kLog2e;
     if (row < rows && half == 0u) {
         const size_t place = ((size_t)kv * z.tokens_q + s.q0 + query) * z.group + head - head0;
-        row_lse[place] = base - kLiftBack<DT>;
-        delta[place] = sum;
+        row_lse[place] = (kLiftBack<DT> - base) / c;
+        delta[place] = -sum;
         if (DT == kGradF16) size[place] = largest;
     }
 
@@ -513,29 +552,44 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
     };
     const unsigned mine = row < rows ? seen(row) : 0u, to = seen(rows - 1u), least = (unsigned)__builtin_amdgcn_readfirstlane((int)seen(wave * 32u));
     f16v acc[DP / 32] = {};
-    const float c = z.scale * kLog2e;
     const TileLoads<DP, kTileKeys, 4> loads_k(wave, 1u, k.ld, z.dim), loads_v(wave, 1u, v.ld, z.dim);
     const auto ask = [&](unsigned j, unsigned b) __attribute__((always_inline)) {
         const unsigned left = s.keys - j < kTileKeys ? s.keys - j : kTileKeys;
         loads_k.ask(lds + b * 2u * kTile, wave, k.p + (size_t)(s.k0 + j) * k.ld + kv * z.dim, ((left - 1u) * k.ld + z.dim) * 2u);
         loads_v.ask(lds + b * 2u * kTile + kTile, wave, v.p + (size_t)(s.k0 + j) * v.ld + kv * z.dim, ((left - 1u) * v.ld + z.dim) * 2u);
     };
+    Operands<DP> operand;
     unsigned buffer = 0;
     if (to) ask(0, 0);
     for (unsigned j = 0; j < to; j += kTileKeys) {
         wait_for_loads<0>();
         __syncthreads();
         if (j + kTileKeys < to) ask(j + kTileKeys, buffer ^ 1u);
-        const Lds tile_k = lds + buffer * 2u * kTile, tile_v = tile_k + kTile;
+        const unsigned at = buffer;
         buffer ^= 1u;
         if (wave * 32u >= rows) continue;
+        operand.renew();
 #pragma unroll
         for (unsigned b = 0; b < 2; ++b) {
+            const Lds at_k = lds + at * 2u * kTile + b * (32u * DP * 2u), at_v = at_k + kTile;
             f16v x = {}, y = {};
+            s8v ring_k[2], ring_v[2];
+            const auto fetch_rows = [&](unsigned i) __attribute__((always_inline)) {
+                ring_k[i % 2u] = operand.rows(at_k, i);
+                ring_v[i % 2u] = operand.rows(at_v, i);
+            };
+            fetch_rows(0);
 #pragma unroll
-            for (unsigned i = 0; i < DP / 16; ++i) x = mfma<DT>(rows_operand<DP>(tile_k, 32u * b, i), bq[i], x);
+            for (unsigned i = 0; i < DP / 16; ++i) {
+                if (i + 1u < DP / 16) fetch_rows(i + 1u);
+                __builtin_amdgcn_sched_barrier(0);
+                x = mfma<DT>(ring_k[i % 2u], bq[i], x);
+                y = mfma<DT>(ring_v[i % 2u], bd[i], y);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            s8v columns[DP / 16];
 #pragma unroll
-            for (unsigned i = 0; i < DP / 16; ++i) y = mfma<DT>(rows_operand<DP>(tile_v, 32u * b, i), bd[i], y);
+            for (unsigned i = 0; i < DP / 16; ++i) columns[i] = operand.columns(at_k + i / (DP / 32) * (16u * DP * 2u), i % (DP / 32));
             if (j + kTileKeys > least) {
 #pragma unroll
                 for (unsigned r = 0; r < 16; ++r)
@@ -543,40 +597,55 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
             }
 #pragma unroll
             for (unsigned r = 0; r < 16; ++r) {
-                y[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -base)) * ((y[r] - sum) * up);
+                y[r] -= sum;
+                y[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -base)) * (DT == kGradF16 ? y[r] * up : y[r]);
             }
 #pragma unroll
             for (unsigned h = 0; h < 2; ++h) {
                 const s8v ds = rounded<DT>(y, h);
 #pragma unroll
-                for (unsigned d = 0; d < DP / 32; ++d) acc[d] = mfma<DT>(columns_operand<DP>(tile_k, 32u * b + 16u * h, d), ds, acc[d]);
+                for (unsigned d = 0; d < DP / 32; ++d) acc[d] = mfma<DT>(columns[h * (DP / 32) + d], ds, acc[d]);
             }
         }
     }
     if (row < rows) store_row<DT, DP>(dq.p + (size_t)(s.q0 + query) * dq.ld + head * z.dim, acc, z.scale / up, z.dim);
 }
 
-// dk and dv: a group takes 128 keys of one key head, and runs over the rows that see them.
+// dk and dv.  A group takes the keys of kKeyWaves waves, 32 each, of one key head and runs over the rows that see them, in kStreams streams:
+// stream i takes every kStreams-th tile of rows, and the streams' sums meet at the end.  The first keys of a long causal sequence are seen by all
+// of its rows, and the launch is as long as the longest group.  us (8191 tokens in 8 sequences, 32 heads of 128 over 8 | 4096 tokens, not
+// causal, the same heads; fp16, 7999 tokens in 16 sequences, 12 heads of 64, not causal | 4096 tokens, 32 heads of 64 over 8):
+//   128 elements a head: 4 waves in 2 streams 264 | 526, 2 in 4 255 | 575, 4 in one stream 345;  64: 2 in 2 70 | 318, 4 in 1 71 | 410, 4 in 2 82 | 314, 2 in 4 97 | 324
+// Of 128 elements a head, a wave's registers hold its keys and both results, but not its values too, which are read from LDS.
+constexpr unsigned kStreamRows = 32;
+template <int DP>
+constexpr unsigned kKeyWaves = DP == 128 ? 4 : 2;
+template <int DP>
+constexpr unsigned kStreams = 2;
+template <int DP>
+constexpr unsigned kStreamKeys = 32 * kKeyWaves<DP>;
+
 template <int DT, int DP>
-__global__ __launch_bounds__(256, 2) void k_attention_dkv(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
+__global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attention_dkv(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
                                                        Heads<const Elem<DT>> v, const float *__restrict__ all_lse, const float *__restrict__ delta,
                                                        const float *__restrict__ size, Heads<Elem<DT>> dk, Heads<Elem<DT>> dv)
 {
-    // Two groups to a compute unit: of 128 elements a head, a wave's registers hold its keys and both results, but not its values too, which are
-    // read from LDS, where the rows of queries make room for them.
     constexpr bool kValuesInLds = DP == 128;
-    constexpr unsigned kRows = kValuesInLds ? 32 : 64;  // of queries at a time
-    constexpr unsigned kTile = kRows * DP * 2, kStage = 2 * kTile + 1024;
-    __shared__ __align__(1024) unsigned char smem[2 * kStage + (kValuesInLds ? kTileRows * DP * 2 : 0)];  // twice a tile of q, one of dout, and three numbers of each row
-    const Lds lds = (Lds)smem, values = lds + 2u * kStage;
+    constexpr unsigned KW = kKeyWaves<DP>, S = kStreams<DP>, kKeys = kStreamKeys<DP>;
+    // of a stream, twice: a tile of q, one of dout, and three numbers of each row
+    constexpr unsigned kRows = kStreamRows, kTile = kRows * DP * 2, kStage = 2 * kTile + 1024, kValues = S * 2 * kStage;
+    constexpr unsigned kSums = 32 * DP * 4;  // of a wave's results of one kind
+    static_assert((S - 1) * KW * kSums <= kValues, "the streams' sums fit where their tiles were");
+    __shared__ __align__(1024) unsigned char smem[kValues + (kValuesInLds ? kKeys * DP * 2 : 0)];
+    const Lds lds = (Lds)smem, values = lds + kValues;
     const unsigned kv = blockIdx.x % z.kv_heads;
     const int *starts = z.starts_k ? z.starts_k : z.starts_q;
-    const TileAt t = tile_of(starts, z.tokens_k, z.num_seqs, 1u, kTileRows, blockIdx.x / z.kv_heads);
+    const TileAt t = tile_of(starts, z.tokens_k, z.num_seqs, 1u, kKeys, blockIdx.x / z.kv_heads);
     const Sequence s = sequence_of(z, t.seq);
     if (t.at >= s.keys) return;
-    const unsigned key0 = (unsigned)t.at, keys = s.keys - key0 < kTileRows ? s.keys - key0 : kTileRows;
-    const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), l = threadIdx.x % 64u, half = l / 32u, key = wave * 32u + l % 32u;
-    const unsigned head0 = kv * z.group;
+    const unsigned key0 = (unsigned)t.at, keys = s.keys - key0 < kKeys ? s.keys - key0 : kKeys;
+    const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), stream = wave / KW, side = wave % KW;
+    const unsigned l = threadIdx.x % 64u, half = l / 32u, key = side * 32u + l % 32u, head0 = kv * z.group;
 
     const __amdgpu_buffer_rsrc_t from_k = buffer_at(k.p + (size_t)(s.k0 + key0) * k.ld + kv * z.dim);
     const __amdgpu_buffer_rsrc_t from_v = buffer_at(v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim);
@@ -587,13 +656,9 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttentionSizes z, Head
         if constexpr (!kValuesInLds) bv[i] = load16(from_v, row_offset(key, keys, 1u, v.ld, 16u * i + 8u * half, z.dim));
     }
     if constexpr (kValuesInLds) {
-        const TileLoads<DP, kTileRows, 4> loads_v(wave, 1u, v.ld, z.dim);
+        const TileLoads<DP, kKeys, KW * S> loads_v(wave, 1u, v.ld, z.dim);
         loads_v.ask(values, wave, v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim, ((keys - 1u) * v.ld + z.dim) * 2u);
     }
-    const auto value = [&](unsigned i) __attribute__((always_inline)) {
-        if constexpr (kValuesInLds) return rows_operand<DP>(values, wave * 32u, i);
-        else return bv[i];
-    };
     landed(bk);
     if constexpr (!kValuesInLds) landed(bv);
     // the first query that sees key j is j - (keys - queries)
@@ -606,38 +671,42 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttentionSizes z, Head
     const float c = z.scale * kLog2e;
     float up = 1.0f;
     bool begun = false;
-    // queries at a time: as many as have kRows rows at most, or a part of one query's heads
-    const unsigned group = z.group, at_once = group < kRows ? kRows / group : 1u;
-    const TileLoads<DP, kRows, 4> loads_q(wave, group, q.ld, z.dim), loads_d(wave, group, dout.ld, z.dim);
+    // A tile is as many queries as have kRows rows at most, or (`parts` of them) a part of one query's heads.
+    const unsigned group = z.group, at_once = group < kRows ? kRows / group : 1u, parts = (group + kRows - 1u) / kRows;
+    const unsigned from = first_of(key0), tiles = (s.queries - from + at_once - 1u) / at_once * parts;
+    const TileLoads<DP, kRows, KW> loads_q(side, group, q.ld, z.dim), loads_d(side, group, dout.ld, z.dim);
     // (values, not one of three variables: the compiler would keep those in memory)
-    const float *const numbers = wave == 0u ? +all_lse : wave == 1u ? +delta : +size;
-    const auto ask = [&](unsigned i, unsigned part, unsigned b) __attribute__((always_inline)) {
-        const unsigned queries = s.queries - i < at_once ? s.queries - i : at_once, heads = group - part < kRows ? group - part : kRows;
-        const Lds to = lds + b * kStage;
-        loads_q.ask(to, wave, q.p + (size_t)(s.q0 + i) * q.ld + (head0 + part) * z.dim, ((queries - 1u) * q.ld + heads * z.dim) * 2u);
-        loads_d.ask(to + kTile, wave, dout.p + (size_t)(s.q0 + i) * dout.ld + (head0 + part) * z.dim, ((queries - 1u) * dout.ld + heads * z.dim) * 2u);
-        if (wave < (DT == kGradF16 ? 3u : 2u)) {
-            load_to_lds<4>(same_in_all(buffer_of(numbers + ((size_t)kv * z.tokens_q + s.q0 + i) * group + part, queries * heads * 4u)), to + 2u * kTile + wave * 256u, l * 4u);
-        }
+    const float *const numbers = side == 0u ? +all_lse : +delta;
+    // tile `n` of all; past the last nothing is in range
+    const auto ask = [&](unsigned n, unsigned b) __attribute__((always_inline)) {
+        const unsigned i = from + n / parts * at_once, part = n % parts * kRows, there = n < tiles ? s.queries - i : 0u;
+        const unsigned queries = there < at_once ? there : at_once, heads = group - part < kRows ? group - part : kRows;
+        const Lds to = lds + (stream * 2u + b) * kStage;
+        const size_t token = s.q0 + (n < tiles ? i : 0u);
+        const unsigned far = queries ? queries - 1u : 0u;
+        loads_q.ask(to, side, q.p + token * q.ld + (head0 + part) * z.dim, queries ? (far * q.ld + heads * z.dim) * 2u : 0u);
+        loads_d.ask(to + kTile, side, dout.p + token * dout.ld + (head0 + part) * z.dim, queries ? (far * dout.ld + heads * z.dim) * 2u : 0u);
+        const size_t at = ((size_t)kv * z.tokens_q + token) * group + part;
+        if (KW == 2 || side < 2u) load_to_lds<4>(same_in_all(buffer_of(numbers + at, queries * heads * 4u)), to + 2u * kTile + side * 256u, l * 4u);
+        if (DT == kGradF16 && side == 0u) load_to_lds<4>(same_in_all(buffer_of(size + at, queries * heads * 4u)), to + 2u * kTile + 512u, l * 4u);
     };
-    unsigned i = first_of(key0), part = 0, buffer = 0;
-    if (i < s.queries) ask(i, part, 0);
-    while (i < s.queries) {
+    Operands<DP> operand;
+    unsigned buffer = 0;
+    if (tiles) ask(stream, 0);
+    for (unsigned first = 0; first < tiles; first += S) {
         wait_for_loads<0>();
         __syncthreads();
-        const unsigned now = i;
-        if (group < kRows || part + kRows >= group) i += at_once, part = 0;
-        else part += kRows;
-        if (i < s.queries) ask(i, part, buffer ^ 1u);
-        const Lds tile_q = lds + buffer * kStage, tile_d = tile_q + kTile;
-        const CDSGD_LDS float *row_lse = (const CDSGD_LDS float *)(tile_d + kTile), *row_delta = row_lse + 64, *row_size = row_lse + 128;
+        const unsigned n = first + stream, now = from + n / parts * at_once;
+        if (first + S < tiles) ask(n + S, buffer ^ 1u);
+        const unsigned at = buffer;
+        const CDSGD_LDS float *row_lse = (const CDSGD_LDS float *)(lds + (stream * 2u + at) * kStage + 2u * kTile), *row_delta = row_lse + 64, *row_size = row_lse + 128;
         buffer ^= 1u;
-        if (wave * 32u >= keys) continue;
+        if (side * 32u >= keys || n >= tiles) continue;
+        operand.renew();
         if constexpr (DT == kGradF16) {
-            static_assert(kRows <= 64, "a lane looks at a row");
             float largest = row_size[l % kRows];
 #pragma unroll
-            for (int m = 1; m < 64; m *= 2) largest = __builtin_fmaxf(largest, __shfl_xor(largest, m));
+            for (int m = 1; m < 32; m *= 2) largest = __builtin_fmaxf(largest, __shfl_xor(largest, m));
             largest = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, largest)));
             const float want = to_one(largest);
             if (largest > 0.0f && (!begun || want < up)) {
@@ -649,46 +718,99 @@ __global__ __launch_bounds__(256, 2) void k_attention_dkv(AttentionSizes z, Head
                 begun = true;
             }
         }
+        // S less lse, and dP less delta: both begin with what is taken from them.  The operands of a pair of products are read beside the pair before.
+        f16v x, y;
+#pragma unroll
+        for (unsigned r = 0; r < 16; r += 4) {
+            const f4 base = *(const CDSGD_LDS f4 *)(row_lse + row_of(r, half)), sum = *(const CDSGD_LDS f4 *)(row_delta + row_of(r, half));
+#pragma unroll
+            for (unsigned e = 0; e < 4; ++e) x[r + e] = base[e], y[r + e] = sum[e];
+        }
+        const Lds at_q = lds + (stream * 2u + at) * kStage, at_d = at_q + kTile;
+        s8v ring_q[2], ring_d[2], ring_v[2];
+        const auto fetch_rows = [&](unsigned e) __attribute__((always_inline)) {
+            ring_q[e % 2u] = operand.rows(at_q, e);
+            ring_d[e % 2u] = operand.rows(at_d, e);
+            if constexpr (kValuesInLds) ring_v[e % 2u] = operand.rows(values + side * (32u * DP * 2u), e);
+        };
+        fetch_rows(0);
+#pragma unroll
+        for (unsigned e = 0; e < DP / 16; ++e) {
+            if (e + 1u < DP / 16) fetch_rows(e + 1u);
+            __builtin_amdgcn_sched_barrier(0);
+            x = mfma<DT>(ring_q[e % 2u], bk[e], x);
+            y = mfma<DT>(ring_d[e % 2u], kValuesInLds ? ring_v[e % 2u] : bv[kValuesInLds ? 0 : e], y);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        constexpr unsigned kProducts = DP / 8, kAhead = 3;
+        s8v ring[kAhead + 1];
+        const auto fetch_columns = [&](unsigned i) __attribute__((always_inline)) {
+            ring[i % (kAhead + 1)] = operand.columns((i % 2u ? at_q : at_d) + i / (kProducts / 2u) * (16u * DP * 2u), i / 2u % (DP / 32));
+        };
+#pragma unroll
+        for (unsigned i = 0; i < kAhead; ++i) fetch_columns(i);
         // (every row of the tile sees every key of the wave, but for causal tiles on the border)
-        const bool border = z.causal && first_of(key0 + wave * 32u + 31u) > now;
-        const unsigned first = first_of(key0 + key), hidden = first <= now ? 0u : group < kRows ? (first - now) * group : kRows;  // rows of the tile
+        if (z.causal && first_of(key0 + side * 32u + 31u) > now) {
+            const unsigned first_row = first_of(key0 + key), hidden = first_row <= now ? 0u : group < kRows ? (first_row - now) * group : kRows;
 #pragma unroll
-        for (unsigned b = 0; b < kRows / 32; ++b) {
-            f16v x = {}, y = {};
+            for (unsigned r = 0; r < 16; ++r)
+                if (row_of(r, half) < hidden) x[r] = -kInfinity, y[r] = 0.0f;
+        }
+        const float down = up * (1.0f / kLifted<DT>);
 #pragma unroll
-            for (unsigned e = 0; e < DP / 16; ++e) x = mfma<DT>(rows_operand<DP>(tile_q, 32u * b, e), bk[e], x);
+        for (unsigned r = 0; r < 16; ++r) {
+            x[r] = __builtin_amdgcn_exp2f(x[r] * c);
+            y[r] = x[r] * (DT == kGradF16 ? y[r] * down : y[r]);
+        }
+        const s8v p[2] = {rounded<DT>(x, 0), rounded<DT>(x, 1)}, ds[2] = {rounded<DT>(y, 0), rounded<DT>(y, 1)};
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (unsigned e = 0; e < DP / 16; ++e) y = mfma<DT>(rows_operand<DP>(tile_d, 32u * b, e), value(e), y);
-            if (border) {
+        for (unsigned i = 0; i < kProducts; ++i) {
+            if (i + kAhead < kProducts) fetch_columns(i + kAhead);
+            const unsigned h = i / (kProducts / 2u), d = i / 2u % (DP / 32);
+            if (i % 2u) acc_k[d] = mfma<DT>(ring[i % (kAhead + 1)], ds[h], acc_k[d]);
+            else acc_v[d] = mfma<DT>(ring[i % (kAhead + 1)], p[h], acc_v[d]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    // the streams' sums, added in their order
+    wait_for_loads<0>();
+    __syncthreads();
+    const float f = z.scale / up;
+    CDSGD_LDS f4 *const sums = (CDSGD_LDS f4 *)lds;
 #pragma unroll
-                for (unsigned r = 0; r < 16; ++r)
-                    if (32u * b + row_of(r, half) < hidden) x[r] = -kInfinity, y[r] = 0.0f;
-            }
-            const float down = up * (1.0f / kLifted<DT>);
+    for (unsigned which = 0; which < 2; ++which) {
+        f16v(&acc)[DP / 32] = which ? acc_v : acc_k;
+        if constexpr (S > 1) __syncthreads();
+        if (stream) {
 #pragma unroll
-            for (unsigned r = 0; r < 16; r += 4) {
-                const f4 base = *(const CDSGD_LDS f4 *)(row_lse + 32u * b + row_of(r, half)), sum = *(const CDSGD_LDS f4 *)(row_delta + 32u * b + row_of(r, half));
+            for (unsigned d = 0; d < DP / 32; ++d)
 #pragma unroll
                 for (unsigned e = 0; e < 4; ++e) {
-                    x[r + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r + e], c, -base[e]));
-                    y[r + e] = x[r + e] * ((y[r + e] - sum[e]) * down);
+                    f4 w = {acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
+                    if (!which) w *= f;
+                    sums[(((stream - 1u) * KW + side) * (DP / 8u) + d * 4u + e) * 64u + l] = w;
                 }
-            }
+        }
+        if constexpr (S > 1) __syncthreads();
+        if (!stream) {
 #pragma unroll
-            for (unsigned h = 0; h < 2; ++h) {
-                const s8v p = rounded<DT>(x, h), ds = rounded<DT>(y, h);
+            for (unsigned d = 0; d < DP / 32; ++d)
 #pragma unroll
-                for (unsigned d = 0; d < DP / 32; ++d) {
-                    acc_v[d] = mfma<DT>(columns_operand<DP>(tile_d, 32u * b + 16u * h, d), p, acc_v[d]);
-                    acc_k[d] = mfma<DT>(columns_operand<DP>(tile_q, 32u * b + 16u * h, d), ds, acc_k[d]);
+                for (unsigned e = 0; e < 4; ++e) {
+                    f4 w = {acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
+                    if (!which) w *= f;
+#pragma unroll
+                    for (unsigned i = 0; i < S - 1; ++i) w += sums[((i * KW + side) * (DP / 8u) + d * 4u + e) * 64u + l];
+#pragma unroll
+                    for (unsigned i = 0; i < 4; ++i) acc[d][4 * e + i] = w[i];
                 }
+            if (key < keys) {
+                const Heads<Elem<DT>> &to = which ? dv : dk;
+                store_row<DT, DP>(to.p + (size_t)(s.k0 + key0 + key) * to.ld + kv * z.dim, acc, which ? 1.0f / kLifted<DT> : 1.0f, z.dim);
             }
         }
     }
-    if (key >= keys) return;
-    const size_t token = s.k0 + key0 + key;
-    store_row<DT, DP>(dk.p + token * dk.ld + kv * z.dim, acc_k, z.scale / up, z.dim);
-    store_row<DT, DP>(dv.p + token * dv.ld + kv * z.dim, acc_v, 1.0f / kLifted<DT>, z.dim);
 }
 
 }  // namespace
