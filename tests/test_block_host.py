@@ -51,7 +51,8 @@ def test_mxint8_refuses(L, want, over):
     a = dict(x=at(0), dtype=BF16, rows=10, cols=100, ld=100, codes=at(1), scales=at(2))
     a.update(over)
     assert L.cdsgd_mxint8_quantize(a["x"], a["dtype"], a["rows"], a["cols"], a["ld"], a["codes"], a["scales"], None) == want
-    assert L.cdsgd_mxint8_dequantize(a["codes"], a["scales"], a["rows"], a["cols"], a["x"], a["dtype"], a["ld"], None) == want or over.get("scales") == at(1) + 127
+    if over.get("scales") != at(1) + 127:       # (what dequantisation reads may overlap)
+        assert L.cdsgd_mxint8_dequantize(a["codes"], a["scales"], a["rows"], a["cols"], a["x"], a["dtype"], a["ld"], None) == want
 
 
 def _held(p=None, ld=0, codes=None, scales=None):
