@@ -8,9 +8,8 @@
 
 namespace {
 
-// Elements to a lane at a time: 16 bytes of the widest type, so that loads and stores of either type are to whole lines.
-template <int ST>
-constexpr int kNormEach = kEach<ST>;
+// Elements to a lane at a time: 16 bytes of fp32, so that its loads and stores are to whole lines.
+constexpr int kNormEach = 4;
 
 struct NormWeights {
     const float *weight, *block_weight, *gate;
@@ -40,72 +39,103 @@ __device__ __forceinline__ void load_weight(const float *w, unsigned cols, unsig
     if (w) widened<kGradF32, E>(load_few<kGradF32, E>(w, cols, c), v);
 }
 
+// Weights of a lane's elements: in registers throughout where there are few of them, or read again (from L2) for every row.
+constexpr int kKeptWeights = 16;
+
+// A group goes from row to row, and asks for the next one's elements before it sums this one's.  Bound by HBM and by the two sums that a row
+// waits for: 8192 x 4096 in bf16 on an fp32 stream 88 us, 4.6 TB/s (weights read again for every row, and nothing asked for ahead: 105).
 template <int ST, int DT, int WAVES, int V>
 __global__ __launch_bounds__(64 * WAVES) void k_block_norm_forward(NormWeights by, unsigned rows, unsigned cols, Rows<const Elem<ST>> h,
                                                                    Rows<const Elem<DT>> b, Rows<Elem<ST>> h_out, Rows<Elem<DT>> y,
                                                                    float *__restrict__ rstd, HeldOut h8, HeldOut b8)
 {
-    constexpr int E = kNormEach<ST>;
+    constexpr int E = kNormEach;
+    constexpr bool kKept = V * E <= kKeptWeights;
     __shared__ double room[2 * WAVES];
     unsigned turn = 0;
-    for (size_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        Few<ST, E> eh[V];
-        Few<DT, E> eb[V];
+    const auto place = [&](int k) __attribute__((always_inline)) { return (k * 64 * WAVES + threadIdx.x) * E; };
+    // scale gate block_weight
+    const auto load_into = [&](int k, double (&into)[E]) __attribute__((always_inline)) {
+        float w[E], g[E];
+        load_weight<E>(by.block_weight, cols, place(k), w);
+        load_weight<E>(by.gate, cols, place(k), g);
 #pragma unroll
-        for (int k = 0; k < V; ++k) eh[k] = load_few<ST, E>(h.p + r * h.ld, cols, (k * 64 * WAVES + threadIdx.x) * E);
-        if (b.p) {
+        for (int i = 0; i < E; ++i) into[i] = (double)g[i] * (double)w[i] * by.scale;
+    };
+    double into[V][E];
+    float weight[V][E];
+    if constexpr (kKept) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) eb[k] = load_few<DT, E>(b.p + r * b.ld, cols, (k * 64 * WAVES + threadIdx.x) * E);
+        for (int k = 0; k < V; ++k) {
+            load_weight<E>(by.weight, cols, place(k), weight[k]);
+            if (b.p) load_into(k, into[k]);
         }
-        double n = 1.0;
+    }
+    Few<ST, E> next_h[V];
+    Few<DT, E> next_b[V] = {};
+    const auto ask = [&](size_t r) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            next_h[k] = load_few<ST, E>(h.p + r * h.ld, cols, place(k));
+            if (b.p) next_b[k] = load_few<DT, E>(b.p + r * b.ld, cols, place(k));
+        }
+    };
+    const double mean = 1.0 / cols;
+    ask(blockIdx.x);
+    for (size_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        Few<DT, E> eb[V];
+        float v[V][E];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            widened<ST, E>(next_h[k], v[k]);
+            eb[k] = next_b[k];
+        }
+        if (r + gridDim.x < rows) ask(r + gridDim.x);
+        double n = 1.0, sum = 0;
         if (by.block_weight) {
-            double sum = 0;
 #pragma unroll
             for (int k = 0; k < V; ++k)
 #pragma unroll
                 for (int i = 0; i < E; ++i) sum = __builtin_fma((double)eb[k].v[i], (double)eb[k].v[i], sum);
-            n = 1.0 / __builtin_sqrt(group_sum<WAVES>(sum, room, turn++) / cols + by.eps);
+            n = 1.0 / __builtin_sqrt(group_sum<WAVES>(sum, room, turn++) * mean + by.eps);
+            sum = 0;
         }
-        float v[V][E];
-        double sum = 0;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const unsigned c = (k * 64 * WAVES + threadIdx.x) * E;
             if (b.p) {
-                float w[E], g[E];
-                load_weight<E>(by.block_weight, cols, c, w);
-                load_weight<E>(by.gate, cols, c, g);
+                if constexpr (!kKept) load_into(k, into[k]);
 #pragma unroll
-                for (int i = 0; i < E; ++i)
-                    v[k][i] = (float)__builtin_fma((double)g[i] * (double)w[i] * by.scale, (double)eb[k].v[i] * n, (double)eh[k].v[i]);
-                if (c < cols) store_few<ST, E>(h_out.p + r * h_out.ld, cols, c, v[k]);
+                for (int i = 0; i < E; ++i) {
+                    const double x = __builtin_fma(into[k][i], (double)eb[k].v[i] * n, (double)v[k][i]);
+                    v[k][i] = (float)x;
+                    sum = __builtin_fma(x, x, sum);
+                }
+                if (place(k) < cols) store_few<ST, E>(h_out.p + r * h_out.ld, cols, place(k), v[k]);
             } else {
-                widened<ST, E>(eh[k], v[k]);
-            }
 #pragma unroll
-            for (int i = 0; i < E; ++i) sum = __builtin_fma((double)v[k][i], (double)v[k][i], sum);
+                for (int i = 0; i < E; ++i) sum = __builtin_fma((double)v[k][i], (double)v[k][i], sum);
+            }
         }
-        const float rr = (float)(1.0 / __builtin_sqrt(group_sum<WAVES>(sum, room, turn++) / cols + by.eps));
+        const float rr = (float)(1.0 / __builtin_sqrt(group_sum<WAVES>(sum, room, turn++) * mean + by.eps));
         if (threadIdx.x == 0) {
             rstd[r] = rr;
             if (by.block_weight) rstd[(size_t)rows + r] = (float)n;
         }
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const unsigned c = (k * 64 * WAVES + threadIdx.x) * E;
-            float w[E], out[E];
-            load_weight<E>(by.weight, cols, c, w);
+            float out[E];
+            if constexpr (!kKept) load_weight<E>(by.weight, cols, place(k), weight[k]);
 #pragma unroll
-            for (int i = 0; i < E; ++i) out[i] = v[k][i] * rr * w[i];
-            if (c < cols) store_few<DT, E>(y.p + r * y.ld, cols, c, out);
+            for (int i = 0; i < E; ++i) out[i] = v[k][i] * rr * weight[k][i];
+            if (place(k) < cols) store_few<DT, E>(y.p + r * y.ld, cols, place(k), out);
             if (h8.codes) {
 #pragma unroll
                 for (int i = 0; i < E; ++i) v[k][i] = (float)(Elem<ST>)v[k][i];
-                save<E>(h8.codes, h8.scales, r, cols, c, v[k]);
+                save<E>(h8.codes, h8.scales, r, cols, place(k), v[k]);
             }
             if (b8.codes) {
-                widened<DT, E>(eb[k], v[k]);
-                save<E>(b8.codes, b8.scales, r, cols, c, v[k]);
+                widened<DT, E>(eb[k], out);
+                save<E>(b8.codes, b8.scales, r, cols, place(k), out);
             }
         }
     }
@@ -126,47 +156,70 @@ struct NormIn {
     }
 };
 
-// parts: [groups][2][cols], the sums over a group's rows of dy x and of t c.
+// parts: [groups][2][cols, to a whole four], the sums over a group's rows of dy x and of t c.  8192 x 4096 as above: 104 us, 5.8 TB/s.
 template <int ST, int DT, int WAVES, int V, bool HELD_H, bool HELD_B>
 __global__ __launch_bounds__(64 * WAVES) void k_block_norm_backward(NormWeights by, unsigned rows, unsigned cols, Rows<const Elem<DT>> dy,
                                                                     Rows<const Elem<ST>> dh_out, HeldIn h, HeldIn b,
                                                                     const float *__restrict__ rstd, Rows<Elem<ST>> dh, Rows<Elem<DT>> db,
                                                                     float *__restrict__ parts)
 {
-    constexpr int E = kNormEach<ST>;
+    constexpr int E = kNormEach;
+    constexpr bool kKept = V * E <= kKeptWeights;
     typedef NormIn<ST, E, HELD_H> H;
     typedef NormIn<DT, E, HELD_B> B;
     __shared__ float room[2 * WAVES];
     unsigned turn = 0;
-    float sum_x[V][E] = {}, sum_c[V][E] = {};
+    const auto place = [&](int k) __attribute__((always_inline)) { return (k * 64 * WAVES + threadIdx.x) * E; };
     const float mean = 1.0f / (float)cols, scale = (float)by.scale;
-    for (size_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        Few<DT, E> ed[V];
-        Few<ST, E> et[V] = {};
-        typename H::Type eh[V];
-        typename B::Type eb[V] = {};
+    // scale gate block_weight
+    const auto load_into = [&](int k, float (&into)[E]) __attribute__((always_inline)) {
+        float g[E];
+        load_weight<E>(by.block_weight, cols, place(k), into);
+        load_weight<E>(by.gate, cols, place(k), g);
+#pragma unroll
+        for (int i = 0; i < E; ++i) into[i] *= scale * g[i];
+    };
+    float into[V][E], weight[V][E], sum_x[V][E] = {}, sum_c[V][E] = {};
+    if constexpr (kKept) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const unsigned c = (k * 64 * WAVES + threadIdx.x) * E;
-            ed[k] = load_few<DT, E>(dy.p + r * dy.ld, cols, c);
-            eh[k] = H::load(h, r, cols, c);
-            if (dh_out.p) et[k] = load_few<ST, E>(dh_out.p + r * dh_out.ld, cols, c);
-            if (b.p) eb[k] = B::load(b, r, cols, c);
+            load_weight<E>(by.weight, cols, place(k), weight[k]);
+            if (b.p) load_into(k, into[k]);
         }
-        const float rr = rstd[r], n = by.block_weight ? rstd[(size_t)rows + r] : 1.0f;
+    }
+    struct {
+        Few<DT, E> d[V];
+        Few<ST, E> t[V] = {};
+        typename H::Type h[V];
+        typename B::Type b[V] = {};
+        float r, n = 1.0f;
+    } next;
+    const auto ask = [&](size_t r) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            next.d[k] = load_few<DT, E>(dy.p + r * dy.ld, cols, place(k));
+            next.h[k] = H::load(h, r, cols, place(k));
+            if (dh_out.p) next.t[k] = load_few<ST, E>(dh_out.p + r * dh_out.ld, cols, place(k));
+            if (b.p) next.b[k] = B::load(b, r, cols, place(k));
+        }
+        next.r = rstd[r];
+        if (by.block_weight) next.n = rstd[(size_t)rows + r];
+    };
+    ask(blockIdx.x);
+    for (size_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const auto now = next;
+        if (r + gridDim.x < rows) ask(r + gridDim.x);
         float x[V][E], t[V][E], part = 0.0f;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const unsigned c = (k * 64 * WAVES + threadIdx.x) * E;
-            float w[E];
-            load_weight<E>(by.weight, cols, c, w);
-            H::values(eh[k], x[k]);
-            widened<DT, E>(ed[k], t[k]);
+            if constexpr (!kKept) load_weight<E>(by.weight, cols, place(k), weight[k]);
+            H::values(now.h[k], x[k]);
+            widened<DT, E>(now.d[k], t[k]);
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                x[k][i] *= rr;
+                x[k][i] *= now.r;
                 sum_x[k][i] = __builtin_fmaf(t[k][i], x[k][i], sum_x[k][i]);
-                t[k][i] *= w[i];
+                t[k][i] *= weight[k][i];
                 part = __builtin_fmaf(t[k][i], x[k][i], part);
             }
         }
@@ -174,20 +227,17 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm_backward(NormWeights 
         part = 0.0f;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const unsigned c = (k * 64 * WAVES + threadIdx.x) * E;
 #pragma unroll
-            for (int i = 0; i < E; ++i) t[k][i] = __builtin_fmaf(rr, __builtin_fmaf(-c1, x[k][i], t[k][i]), (float)et[k].v[i]);
-            if (c < cols) store_few<ST, E>(dh.p + r * dh.ld, cols, c, t[k]);
+            for (int i = 0; i < E; ++i) t[k][i] = __builtin_fmaf(now.r, __builtin_fmaf(-c1, x[k][i], t[k][i]), (float)now.t[k].v[i]);
+            if (place(k) < cols) store_few<ST, E>(dh.p + r * dh.ld, cols, place(k), t[k]);
             if (b.p) {
-                float w[E], g[E];
-                load_weight<E>(by.block_weight, cols, c, w);
-                load_weight<E>(by.gate, cols, c, g);
-                B::values(eb[k], x[k]);
+                if constexpr (!kKept) load_into(k, into[k]);
+                B::values(now.b[k], x[k]);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    x[k][i] *= n;
+                    x[k][i] *= now.n;
                     sum_c[k][i] = __builtin_fmaf(t[k][i], x[k][i], sum_c[k][i]);
-                    t[k][i] *= scale * g[i] * w[i];
+                    t[k][i] *= into[k][i];
                     part = __builtin_fmaf(t[k][i], x[k][i], part);
                 }
             }
@@ -196,47 +246,53 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm_backward(NormWeights 
         const float c2 = by.block_weight ? group_sum<WAVES>(part, room, turn++) * mean : 0.0f;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const unsigned c = (k * 64 * WAVES + threadIdx.x) * E;
 #pragma unroll
-            for (int i = 0; i < E; ++i) t[k][i] = n * __builtin_fmaf(-c2, x[k][i], t[k][i]);
-            if (c < cols) store_few<DT, E>(db.p + r * db.ld, cols, c, t[k]);
+            for (int i = 0; i < E; ++i) t[k][i] = now.n * __builtin_fmaf(-c2, x[k][i], t[k][i]);
+            if (place(k) < cols) store_few<DT, E>(db.p + r * db.ld, cols, place(k), t[k]);
         }
     }
-    float *const mine = parts + (size_t)blockIdx.x * 2u * cols;
+    const unsigned pitch = (cols + 3u) / 4u * 4u;  // (whole fours: their sums are 0 behind the end)
+    float *const mine = parts + (size_t)blockIdx.x * 2u * pitch;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        const unsigned c = (k * 64 * WAVES + threadIdx.x) * E;
-        if (c < cols) {
-            store_few<kGradF32, E>(mine, cols, c, sum_x[k]);
-            store_few<kGradF32, E>(mine + cols, cols, c, sum_c[k]);
+        if (place(k) < pitch) {
+            store_few<kGradF32, E, false>(mine, pitch, place(k), sum_x[k]);
+            store_few<kGradF32, E, false>(mine + pitch, pitch, place(k), sum_c[k]);
         }
     }
 }
 
-// The groups' sums, joined in 64 bits in an order of their own number alone: 16 lanes take every sixteenth of them for a column.
+// The groups' sums, joined in 64 bits in an order of their own number alone: 8 lanes take 32 columns, and 32 times as many every 32nd of the
+// parts each.
 __global__ __launch_bounds__(256) void k_block_norm_join(const float *__restrict__ parts, unsigned groups, unsigned cols, NormWeights by,
                                                          float *__restrict__ dweight, float *__restrict__ dblock_weight,
                                                          float *__restrict__ dgate)
 {
-    __shared__ double room[16][17];
-    const unsigned col = threadIdx.x % 16u, slice = threadIdx.x / 16u, c = blockIdx.x * 16u + col;
+    __shared__ double room[32][33];
+    const unsigned slice = threadIdx.x / 8u, first = threadIdx.x % 8u * 4u, c0 = blockIdx.x * 32u, pitch = (cols + 3u) / 4u * 4u;
     const bool second = blockIdx.y != 0;
-    double sum = 0;
-    if (c < cols) {
-        const float *p = parts + (second ? cols : 0u) + c;
-        for (unsigned g = slice; g < groups; g += 16u) sum += (double)p[(size_t)g * 2u * cols];
-    }
-    room[slice][col] = sum;
-    __syncthreads();
-    if (slice != 0 || c >= cols) return;
+    double sum[4] = {};
+    const f4 *p = reinterpret_cast<const f4 *>(parts + (second ? pitch : 0u) + (c0 + first < pitch ? c0 + first : 0u));
+#pragma unroll 8
+    for (unsigned g = slice; g < groups; g += 32u) {
+        const f4 x = p[(size_t)g * (pitch / 2u)];
 #pragma unroll
-    for (unsigned k = 1; k < 16; ++k) sum += room[k][col];
+        for (int i = 0; i < 4; ++i) sum[i] += (double)x[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) room[slice][first + i] = sum[i];
+    __syncthreads();
+    const unsigned c = c0 + threadIdx.x;
+    if (threadIdx.x >= 32u || c >= cols) return;
+    double all = room[0][threadIdx.x];
+#pragma unroll
+    for (unsigned k = 1; k < 32; ++k) all += room[k][threadIdx.x];
     if (!second) {
-        dweight[c] = (float)sum;
+        dweight[c] = (float)all;
     } else {
-        sum *= by.scale;
-        if (dblock_weight) dblock_weight[c] = (float)(sum * (by.gate ? (double)by.gate[c] : 1.0));
-        if (dgate) dgate[c] = (float)(sum * (by.block_weight ? (double)by.block_weight[c] : 1.0));
+        all *= by.scale;
+        if (dblock_weight) dblock_weight[c] = (float)(all * (by.gate ? (double)by.gate[c] : 1.0));
+        if (dgate) dgate[c] = (float)(all * (by.block_weight ? (double)by.block_weight[c] : 1.0));
     }
 }
 
