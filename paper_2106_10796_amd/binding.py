@@ -9,6 +9,7 @@ declines (-1) whatever is not plainly good; ctypes and the checks below then con
 that module is not there, or was built for another library, torch or Python, ctypes serves every call.
 """
 import ctypes
+import math
 import os
 import sysconfig
 from typing import NamedTuple
@@ -94,7 +95,9 @@ _calls = _Declines()
 _CALLED = ("cdsgd_quantize_pack", "cdsgd_decode_sum", "cdsgd_decode_sum_sparse", "cdsgd_update", "cdsgd_sparse_encode",
            "cdsgd_sparse_words", "cdsgd_sparse_segments", "cdsgd_step_fused", "cdsgd_step_fused_range",
            "cdsgd_step_fused_static", "cdsgd_grad_norm_compute", "cdsgd_adamw_step", "cdsgd_adamw_grad_norm",
-           "cdsgd_adamw_read_states", "cdsgd_mxfp4_quantize", "cdsgd_mxfp4_dequantize", "cdsgd_mxfp4_matmul")
+           "cdsgd_adamw_read_states", "cdsgd_mxfp4_quantize", "cdsgd_mxfp4_dequantize", "cdsgd_mxfp4_matmul",
+           "cdsgd_mxint8_quantize", "cdsgd_mxint8_dequantize", "cdsgd_gated_forward", "cdsgd_gated_backward",
+           "cdsgd_block_norm_forward", "cdsgd_block_norm_backward", "cdsgd_attention_forward", "cdsgd_attention_backward")
 
 
 def _native():
@@ -936,18 +939,26 @@ def _on_this_device(*tensors):
 
 def cdsgd_mxint8_quantize(x, q):
     """x [rows, cols] into q."""
-    p, dtype, r, c, ld = _rows(x, "x")
-    codes, scales = _mx8(q, "q", r, c)
-    _on_this_device(x, q)
-    _check(lib().cdsgd_mxint8_quantize(p, dtype, r, c, ld, codes, scales, _stream()), "cdsgd_mxint8_quantize")
+    st = _native().mxint8_quantize(x, q, _stream)
+    if st < 0:
+        p, dtype, r, c, ld = _rows(x, "x")
+        codes, scales = _mx8(q, "q", r, c)
+        _on_this_device(x, q)
+        st = lib().cdsgd_mxint8_quantize(p, dtype, r, c, ld, codes, scales, _stream())
+    if st != OK:
+        _check(st, "cdsgd_mxint8_quantize")
 
 
 def cdsgd_mxint8_dequantize(q, out):
     """The values that q stands for, into out [rows, cols]."""
-    codes, scales = _mx8(q, "q")
-    p, dtype, r, c, ld = _rows(out, "out", q.rows, q.cols)
-    _on_this_device(out, q)
-    _check(lib().cdsgd_mxint8_dequantize(codes, scales, r, c, p, dtype, ld, _stream()), "cdsgd_mxint8_dequantize")
+    st = _native().mxint8_dequantize(q, out, _stream)
+    if st < 0:
+        codes, scales = _mx8(q, "q")
+        p, dtype, r, c, ld = _rows(out, "out", q.rows, q.cols)
+        _on_this_device(out, q)
+        st = lib().cdsgd_mxint8_dequantize(codes, scales, r, c, p, dtype, ld, _stream())
+    if st != OK:
+        _check(st, "cdsgd_mxint8_dequantize")
 
 
 def _act(act):
@@ -958,23 +969,30 @@ def _act(act):
 
 def cdsgd_gated_forward(a, u, y, a8=None, u8=None, act="silu"):
     """y = act(a) * u, matrices of one type.  a8, u8 (Mxint8, both or none): a and u in 8 bits, for the backward pass."""
-    pa, dtype, r, c, ld_a = _rows(a, "a")
-    pu, ld_u = _rows_of(u, dtype, "u", r, c)
-    py, ld_y = _rows_of(y, dtype, "y", r, c)
-    saved = (*_mx8(a8, "a8", r, c, optional=True), *_mx8(u8, "u8", r, c, optional=True))
-    _on_this_device(a, u, y, a8, u8)
-    _check(lib().cdsgd_gated_forward(_act(act), dtype, r, c, pa, ld_a, pu, ld_u, py, ld_y, *saved, _stream()), "cdsgd_gated_forward")
+    st = _native().gated_forward(a, u, y, a8, u8, ACTS.get(act), _stream)
+    if st < 0:
+        pa, dtype, r, c, ld_a = _rows(a, "a")
+        pu, ld_u = _rows_of(u, dtype, "u", r, c)
+        py, ld_y = _rows_of(y, dtype, "y", r, c)
+        saved = (*_mx8(a8, "a8", r, c, optional=True), *_mx8(u8, "u8", r, c, optional=True))
+        _on_this_device(a, u, y, a8, u8)
+        st = lib().cdsgd_gated_forward(_act(act), dtype, r, c, pa, ld_a, pu, ld_u, py, ld_y, *saved, _stream())
+    if st != OK:
+        _check(st, "cdsgd_gated_forward")
 
 
 def cdsgd_gated_backward(dy, a, u, da, du, act="silu"):
     """da and du from dy and from a and u: matrices, or Mxint8 as the forward pass saved them."""
-    p, dtype, r, c, ld = _rows(dy, "dy")
-    ha, hu = _held(a, dtype, "a", r, c), _held(u, dtype, "u", r, c)
-    pa, ld_a = _rows_of(da, dtype, "da", r, c)
-    pu, ld_u = _rows_of(du, dtype, "du", r, c)
-    _on_this_device(dy, a, u, da, du)
-    _check(lib().cdsgd_gated_backward(_act(act), dtype, r, c, p, ld, ctypes.byref(ha), ctypes.byref(hu), pa, ld_a, pu, ld_u, _stream()),
-           "cdsgd_gated_backward")
+    st = _native().gated_backward(dy, a, u, da, du, ACTS.get(act), _stream)
+    if st < 0:
+        p, dtype, r, c, ld = _rows(dy, "dy")
+        ha, hu = _held(a, dtype, "a", r, c), _held(u, dtype, "u", r, c)
+        pa, ld_a = _rows_of(da, dtype, "da", r, c)
+        pu, ld_u = _rows_of(du, dtype, "du", r, c)
+        _on_this_device(dy, a, u, da, du)
+        st = lib().cdsgd_gated_backward(_act(act), dtype, r, c, p, ld, ctypes.byref(ha), ctypes.byref(hu), pa, ld_a, pu, ld_u, _stream())
+    if st != OK:
+        _check(st, "cdsgd_gated_backward")
 
 
 def new_block_norm_workspace(rows: int, cols: int, device="cuda") -> torch.Tensor:
@@ -988,54 +1006,65 @@ class BlockNorm:
     block_weight there is no norm after the block, without gate no gate."""
 
     def __init__(self, weight, block_weight=None, gate=None, scale=1.0, eps=1e-6):
-        self.weight, self.block_weight, self.gate, self.scale, self.eps = weight, block_weight, gate, float(scale), float(eps)
+        self._weights = (weight, block_weight, gate)
         self._cols = weight.numel()
-        self._at = [_dev(t, torch.float32, self._cols, name) for t, name in ((weight, "weight"), (block_weight, "block_weight"), (gate, "gate"))]
+        at = [_dev(t, torch.float32, self._cols, name) for t, name in zip(self._weights, ("weight", "block_weight", "gate"))]
+        _on_this_device(*self._weights)
+        self._norm = cdsgd_block_norm(0, 0, 0, self._cols, *at, float(scale), float(eps))
+        self._at, self._device = ctypes.addressof(self._norm), weight.device.index
 
-    def _of(self, dtype, stream, rows, block):
-        weights = self._at if block else [self._at[0], None, None]
-        return cdsgd_block_norm(dtype, stream, rows, self._cols, *weights, self.scale, self.eps)
+    scale = property(lambda self: self._norm.scale)
+    eps = property(lambda self: self._norm.eps)
 
-    def _sizes(self, y, name, stream, stream_name):
-        """(address, type, rows, elements between two rows) of y, and the stream's type."""
+    def _of(self, y, name, stream, stream_name, block):
+        """The norm for y's type and rows and for the stream's type, and (address, elements between two rows) of y."""
         p, dtype, r, c, ld = _rows(y, name)
         if c != self._cols:
             raise ValueError("%s has %d columns, expected %d" % (name, c, self._cols))
         if not isinstance(stream, torch.Tensor) or stream.dtype not in GRAD_DTYPES:
             raise TypeError("%s must be a CUDA matrix of float32, bfloat16 or float16" % stream_name)
-        return p, dtype, r, ld, GRAD_DTYPES[stream.dtype]
+        n = self._norm
+        weights = (n.block_weight, n.gate) if block else (None, None)
+        return cdsgd_block_norm(dtype, GRAD_DTYPES[stream.dtype], r, c, n.weight, *weights, n.scale, n.eps), p, ld
 
     def forward(self, h, y, rstd, block=None, h_out=None, h8=None, block8=None):
         """y (and, with a block's output, h_out) from h; rstd (float32 [2, rows]) receives the factors of both norms.  h8, block8 (Mxint8, optional):
         h_out and block in 8 bits, for the backward pass.  Without a block y is the norm of h, and h8 is h in 8 bits."""
-        p, dtype, r, ld, stream = self._sizes(y, "y", h, "h")
-        c = self._cols
-        ph, ld_h = _rows_of(h, stream, "h", r, c)
-        pb, ld_b = _rows_of(block, dtype, "block", r, c, optional=True)
-        po, ld_o = _rows_of(h_out, stream, "h_out", r, c, optional=True)
-        saved = (*_mx8(h8, "h8", r, c, optional=True), *_mx8(block8, "block8", r, c, optional=True))
-        _on_this_device(h, y, rstd, block, h_out, h8, block8, self.weight, self.block_weight, self.gate)
-        of = self._of(dtype, stream, r, block is not None)
-        _check(lib().cdsgd_block_norm_forward(ctypes.byref(of), ph, ld_h, pb, ld_b, po, ld_o, p, ld, _dev(rstd, torch.float32, 2 * r, "rstd"),
-                                              *saved, _stream()), "cdsgd_block_norm_forward")
+        st = _native().block_norm_forward(self._at, self._device, h, y, rstd, block, h_out, h8, block8, _stream)
+        if st < 0:
+            of, p, ld = self._of(y, "y", h, "h", block is not None)
+            r, c = of.rows, of.cols
+            ph, ld_h = _rows_of(h, of.stream_dtype, "h", r, c)
+            pb, ld_b = _rows_of(block, of.dtype, "block", r, c, optional=True)
+            po, ld_o = _rows_of(h_out, of.stream_dtype, "h_out", r, c, optional=True)
+            saved = (*_mx8(h8, "h8", r, c, optional=True), *_mx8(block8, "block8", r, c, optional=True))
+            _on_this_device(h, y, rstd, block, h_out, h8, block8, *self._weights)
+            st = lib().cdsgd_block_norm_forward(ctypes.byref(of), ph, ld_h, pb, ld_b, po, ld_o, p, ld, _dev(rstd, torch.float32, 2 * r, "rstd"),
+                                                *saved, _stream())
+        if st != OK:
+            _check(st, "cdsgd_block_norm_forward")
 
     def backward(self, dy, h, rstd, dh, dweight, workspace, dh_out=None, block=None, dblock=None, dblock_weight=None, dgate=None):
         """The gradients of h (dh), of the block's output (dblock) and of the weights, from those of y (dy) and of h_out (dh_out; None: 0), the
         forward pass's rstd, and its h_out and block as they are or as Mxint8.  workspace: new_block_norm_workspace."""
-        p, dtype, r, ld, stream = self._sizes(dy, "dy", dh, "dh")
-        c = self._cols
-        pt, ld_t = _rows_of(dh_out, stream, "dh_out", r, c, optional=True)
-        ph, ld_h = _rows_of(dh, stream, "dh", r, c)
-        pb, ld_b = _rows_of(dblock, dtype, "dblock", r, c, optional=True)
-        held_h = _held(h, stream, "h", r, c)
-        held_b = cdsgd_held() if block is None else _held(block, dtype, "block", r, c)
-        _on_this_device(dy, h, rstd, dh, dweight, workspace, dh_out, block, dblock, dblock_weight, dgate, self.weight, self.block_weight, self.gate)
-        of = self._of(dtype, stream, r, block is not None)
-        _check(lib().cdsgd_block_norm_backward(
-            ctypes.byref(of), p, ld, pt, ld_t, ctypes.byref(held_h), ctypes.byref(held_b), _dev(rstd, torch.float32, 2 * r, "rstd"), ph, ld_h, pb, ld_b,
-            _dev(dweight, torch.float32, c, "dweight"), _dev(dblock_weight, torch.float32, c, "dblock_weight"),
-            _dev(dgate, torch.float32, c, "dgate"), _dev(workspace, torch.uint8, None, "workspace"),
-            workspace.numel() if workspace is not None else 0, _stream()), "cdsgd_block_norm_backward")
+        st = _native().block_norm_backward(self._at, self._device, dy, h, rstd, dh, dweight, workspace, dh_out, block, dblock, dblock_weight, dgate,
+                                           _stream)
+        if st < 0:
+            of, p, ld = self._of(dy, "dy", dh, "dh", block is not None)
+            r, c = of.rows, of.cols
+            pt, ld_t = _rows_of(dh_out, of.stream_dtype, "dh_out", r, c, optional=True)
+            ph, ld_h = _rows_of(dh, of.stream_dtype, "dh", r, c)
+            pb, ld_b = _rows_of(dblock, of.dtype, "dblock", r, c, optional=True)
+            held_h = _held(h, of.stream_dtype, "h", r, c)
+            held_b = cdsgd_held() if block is None else _held(block, of.dtype, "block", r, c)
+            _on_this_device(dy, h, rstd, dh, dweight, workspace, dh_out, block, dblock, dblock_weight, dgate, *self._weights)
+            st = lib().cdsgd_block_norm_backward(
+                ctypes.byref(of), p, ld, pt, ld_t, ctypes.byref(held_h), ctypes.byref(held_b), _dev(rstd, torch.float32, 2 * r, "rstd"), ph, ld_h, pb,
+                ld_b, _dev(dweight, torch.float32, c, "dweight"), _dev(dblock_weight, torch.float32, c, "dblock_weight"),
+                _dev(dgate, torch.float32, c, "dgate"), _dev(workspace, torch.uint8, None, "workspace"),
+                workspace.numel() if workspace is not None else 0, _stream())
+        if st != OK:
+            _check(st, "cdsgd_block_norm_backward")
 
 
 ATTENTION_DTYPES = {torch.bfloat16: 1, torch.float16: 2}
@@ -1071,7 +1100,7 @@ def _batch(q, k, starts, starts_k, causal, scale):
     seqs = 1 if starts is None else starts.numel() - 1
     return cdsgd_attention(ATTENTION_DTYPES[q.dtype], int(bool(causal)), q.shape[0], k.shape[0], seqs,
                            None if starts is None else _starts(starts, "starts"), None if starts_k is None else _starts(starts_k, "starts_k", seqs),
-                           q.shape[1], k.shape[1], q.shape[2], float(q.shape[2]) ** -0.5 if scale is None else float(scale))
+                           q.shape[1], k.shape[1], q.shape[2], 1.0 / math.sqrt(q.shape[2]) if scale is None else float(scale))
 
 
 def new_attention_workspace(q, k, seqs=1, train=False):
@@ -1091,28 +1120,36 @@ def cdsgd_attention_forward(q, k, v, out, lse=None, starts=None, starts_k=None, 
     """out = softmax(scale q k^T) v over a packed batch: q, out [tokens, heads, dim], k, v [tokens, kv_heads, dim], bfloat16 or float16.
     starts, starts_k (int32 [sequences + 1] on the GPU): where the sequences' queries and keys begin and end; None: one sequence, or the same for both.
     lse (float32 [heads, tokens], optional): for the backward pass.  scale: None is dim ** -0.5.  workspace: new_attention_workspace."""
-    pq, ld_q = _heads(q, "q")
-    pk, ld_k = _heads(k, "k", q.dtype)
-    pv, ld_v = _heads(v, "v", q.dtype, k.shape)
-    po, ld_o = _heads(out, "out", q.dtype, q.shape)
-    b = _batch(q, k, starts, starts_k, causal, scale)
-    _on_this_device(q, k, v, out, lse, starts, starts_k, workspace)
-    _check(lib().cdsgd_attention_forward(ctypes.byref(b), pq, ld_q, pk, ld_k, pv, ld_v, po, ld_o,
-                                         _dev(lse, torch.float32, q.shape[0] * q.shape[1], "lse"), _dev(workspace, torch.uint8, None, "workspace"),
-                                         workspace.numel() if workspace is not None else 0, _stream()), "cdsgd_attention_forward")
+    st = _native().attention_forward(q, k, v, out, lse, starts, starts_k, causal, scale, workspace, _stream)
+    if st < 0:
+        pq, ld_q = _heads(q, "q")
+        pk, ld_k = _heads(k, "k", q.dtype)
+        pv, ld_v = _heads(v, "v", q.dtype, k.shape)
+        po, ld_o = _heads(out, "out", q.dtype, q.shape)
+        b = _batch(q, k, starts, starts_k, causal, scale)
+        _on_this_device(q, k, v, out, lse, starts, starts_k, workspace)
+        st = lib().cdsgd_attention_forward(ctypes.byref(b), pq, ld_q, pk, ld_k, pv, ld_v, po, ld_o,
+                                             _dev(lse, torch.float32, q.shape[0] * q.shape[1], "lse"), _dev(workspace, torch.uint8, None, "workspace"),
+                                             workspace.numel() if workspace is not None else 0, _stream())
+    if st != OK:
+        _check(st, "cdsgd_attention_forward")
 
 
 def cdsgd_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, starts=None, starts_k=None, causal=True, scale=None, workspace=None):
     """dq, dk and dv from dout, the inputs, and the forward pass's out and lse.  workspace: new_attention_workspace with train."""
-    pq, ld_q = _heads(q, "q")
-    pk, ld_k = _heads(k, "k", q.dtype)
-    at = []
-    for t, name, like in ((v, "v", k), (out, "out", q), (dout, "dout", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k)):
-        at.append(_heads(t, name, q.dtype, like.shape))
-    (pv, ld_v), (po, ld_o), (pd, ld_d), (pdq, ld_dq), (pdk, ld_dk), (pdv, ld_dv) = at
-    b = _batch(q, k, starts, starts_k, causal, scale)
-    _on_this_device(q, k, v, out, lse, dout, dq, dk, dv, starts, starts_k, workspace)
-    _check(lib().cdsgd_attention_backward(ctypes.byref(b), pd, ld_d, pq, ld_q, pk, ld_k, pv, ld_v, po, ld_o,
-                                          _dev(lse, torch.float32, q.shape[0] * q.shape[1], "lse"), pdq, ld_dq, pdk, ld_dk, pdv, ld_dv,
-                                          _dev(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0,
-                                          _stream()), "cdsgd_attention_backward")
+    st = _native().attention_backward(dout, q, k, v, out, lse, dq, dk, dv, starts, starts_k, causal, scale, workspace, _stream)
+    if st < 0:
+        pq, ld_q = _heads(q, "q")
+        pk, ld_k = _heads(k, "k", q.dtype)
+        at = []
+        for t, name, like in ((v, "v", k), (out, "out", q), (dout, "dout", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k)):
+            at.append(_heads(t, name, q.dtype, like.shape))
+        (pv, ld_v), (po, ld_o), (pd, ld_d), (pdq, ld_dq), (pdk, ld_dk), (pdv, ld_dv) = at
+        b = _batch(q, k, starts, starts_k, causal, scale)
+        _on_this_device(q, k, v, out, lse, dout, dq, dk, dv, starts, starts_k, workspace)
+        st = lib().cdsgd_attention_backward(ctypes.byref(b), pd, ld_d, pq, ld_q, pk, ld_k, pv, ld_v, po, ld_o,
+                                              _dev(lse, torch.float32, q.shape[0] * q.shape[1], "lse"), pdq, ld_dq, pdk, ld_dk, pdv, ld_dv,
+                                              _dev(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0,
+                                              _stream())
+    if st != OK:
+        _check(st, "cdsgd_attention_backward")

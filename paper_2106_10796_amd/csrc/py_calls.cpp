@@ -9,12 +9,15 @@
 #include <Python.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/detail/CUDAHooksInterface.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
+#include <cmath>
 #include <cstring>
 
 #include "cdsgd.h"
+#include "cdsgd_block.h"
 #include "cdsgd_ops.h"
 
 namespace {
@@ -37,6 +40,14 @@ struct Library {
     decltype(&cdsgd_mxfp4_quantize) mxfp4_quantize;
     decltype(&cdsgd_mxfp4_dequantize) mxfp4_dequantize;
     decltype(&cdsgd_mxfp4_matmul) mxfp4_matmul;
+    decltype(&cdsgd_mxint8_quantize) mxint8_quantize;
+    decltype(&cdsgd_mxint8_dequantize) mxint8_dequantize;
+    decltype(&cdsgd_gated_forward) gated_forward;
+    decltype(&cdsgd_gated_backward) gated_backward;
+    decltype(&cdsgd_block_norm_forward) block_norm_forward;
+    decltype(&cdsgd_block_norm_backward) block_norm_backward;
+    decltype(&cdsgd_attention_forward) attention_forward;
+    decltype(&cdsgd_attention_backward) attention_backward;
 } lib;
 
 struct NotPlain {};  // leave it to the binding
@@ -380,6 +391,270 @@ PyObject *mxfp4_matmul(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- include/cdsgd_block.h: as above, and every tensor is on the current device ----------------------------------------------------
+
+void on_this_device(PyObject *o)
+{
+    if (o == Py_None) return;
+    if (PyTuple_Check(o)) o = PyTuple_GET_ITEM(o, 0);  // (a matrix in 8 bits: its codes, which mx8 has looked at)
+    if (THPVariable_Unpack(o).get_device() != at::detail::getCUDAHooks().getCurrentDevice()) throw NotPlain();
+}
+
+Matrix matrix_here(PyObject *o)
+{
+    const Matrix m = matrix(o);
+    on_this_device(o);
+    return m;
+}
+
+// A matrix like another, of its type or of `dtype`; None where that is allowed.
+Matrix like(PyObject *o, const Matrix &x, int dtype, bool or_none = false)
+{
+    if (or_none && o == Py_None) return {nullptr, dtype, x.rows, x.cols, 0};
+    const Matrix m = matrix_here(o);
+    if (m.dtype != dtype || m.rows != x.rows || m.cols != x.cols) throw NotPlain();
+    return m;
+}
+
+void *buffer_here(PyObject *o, at::ScalarType type, size_t n, size_t *numel = nullptr)
+{
+    if (o == Py_None) {
+        if (numel) *numel = 0;
+        return nullptr;
+    }
+    void *p = buffer(o, type, n, numel);
+    on_this_device(o);
+    return p;
+}
+float *floats_here(PyObject *o, size_t n) { return static_cast<float *>(buffer_here(o, at::kFloat, n)); }
+
+// A matrix in 8 bits, as the binding's class of that name holds it.
+struct Mx8 {
+    int8_t *codes = nullptr;
+    uint8_t *scales = nullptr;
+    size_t rows = 0, cols = 0;
+};
+
+bool is_mx8(PyObject *o) { return PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 4 && std::strcmp(Py_TYPE(o)->tp_name, "Mxint8") == 0; }
+
+Mx8 mx8(PyObject *o)
+{
+    if (!is_mx8(o)) throw NotPlain();
+    const long rows = whole(PyTuple_GET_ITEM(o, 2)), cols = whole(PyTuple_GET_ITEM(o, 3));
+    if (rows < 1 || cols < 1 || rows > INT_MAX || cols > INT_MAX) throw NotPlain();
+    const size_t groups = ((size_t)cols + 31) / 32;
+    Mx8 q;
+    q.rows = (size_t)rows;
+    q.cols = (size_t)cols;
+    q.codes = static_cast<int8_t *>(buffer(PyTuple_GET_ITEM(o, 0), at::kChar, q.rows * 32 * groups));
+    q.scales = static_cast<uint8_t *>(buffer(PyTuple_GET_ITEM(o, 1), at::kByte, q.rows * groups));
+    on_this_device(o);
+    return q;
+}
+
+Mx8 mx8_like(PyObject *o, const Matrix &x)
+{
+    if (o == Py_None) return Mx8();
+    const Mx8 q = mx8(o);
+    if (q.rows != x.rows || q.cols != x.cols) throw NotPlain();
+    return q;
+}
+
+cdsgd_held held(PyObject *o, const Matrix &x, int dtype)
+{
+    if (is_mx8(o)) {
+        const Mx8 q = mx8_like(o, x);
+        return {nullptr, 0, q.codes, q.scales};
+    }
+    const Matrix m = like(o, x, dtype);
+    return {m.p, m.ld, nullptr, nullptr};
+}
+
+PyObject *mxint8_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 3, [&] {
+        const Matrix x = matrix_here(a[0]);
+        const Mx8 q = mx8(a[1]);
+        if (q.rows != x.rows || q.cols != x.cols) throw NotPlain();
+        void *s = stream_of(a[2]);
+        return unlocked([&] { return lib.mxint8_quantize(x.p, x.dtype, x.rows, x.cols, x.ld, q.codes, q.scales, s); });
+    });
+}
+
+PyObject *mxint8_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 3, [&] {
+        const Mx8 q = mx8(a[0]);
+        const Matrix out = matrix_here(a[1]);
+        if (out.rows != q.rows || out.cols != q.cols) throw NotPlain();
+        void *s = stream_of(a[2]);
+        return unlocked([&] { return lib.mxint8_dequantize(q.codes, q.scales, q.rows, q.cols, out.p, out.dtype, out.ld, s); });
+    });
+}
+
+PyObject *gated_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 7, [&] {
+        const Matrix x = matrix_here(a[0]), u = like(a[1], x, x.dtype), y = like(a[2], x, x.dtype);
+        const Mx8 a8 = mx8_like(a[3], x), u8 = mx8_like(a[4], x);
+        const int act = small(a[5]);
+        void *s = stream_of(a[6]);
+        return unlocked([&] {
+            return lib.gated_forward(act, x.dtype, x.rows, x.cols, x.p, x.ld, u.p, u.ld, y.p, y.ld, a8.codes, a8.scales, u8.codes, u8.scales, s);
+        });
+    });
+}
+
+PyObject *gated_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 7, [&] {
+        const Matrix dy = matrix_here(a[0]);
+        const cdsgd_held x = held(a[1], dy, dy.dtype), u = held(a[2], dy, dy.dtype);
+        const Matrix da = like(a[3], dy, dy.dtype), du = like(a[4], dy, dy.dtype);
+        const int act = small(a[5]);
+        void *s = stream_of(a[6]);
+        return unlocked([&] { return lib.gated_backward(act, dy.dtype, dy.rows, dy.cols, dy.p, dy.ld, &x, &u, da.p, da.ld, du.p, du.ld, s); });
+    });
+}
+
+// The norm at that address, for that matrix and stream type; `device` is that of its weights.
+cdsgd_block_norm norm_of_rows(PyObject *at, PyObject *device, const Matrix &y, int stream, bool block)
+{
+    cdsgd_block_norm n = *handle<const cdsgd_block_norm>(at);
+    if (n.cols != y.cols || small(device) != at::detail::getCUDAHooks().getCurrentDevice()) throw NotPlain();
+    n.dtype = y.dtype;
+    n.stream_dtype = stream;
+    n.rows = y.rows;
+    if (!block) n.block_weight = n.gate = nullptr;
+    return n;
+}
+
+PyObject *block_norm_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&] {
+        const Matrix y = matrix_here(a[3]), h = matrix_here(a[2]);
+        if (h.rows != y.rows || h.cols != y.cols) throw NotPlain();
+        const cdsgd_block_norm norm = norm_of_rows(a[0], a[1], y, h.dtype, a[5] != Py_None);
+        float *rstd = floats_here(a[4], 2 * y.rows);
+        const Matrix b = like(a[5], y, y.dtype, true), out = like(a[6], y, h.dtype, true);
+        const Mx8 h8 = mx8_like(a[7], y), b8 = mx8_like(a[8], y);
+        void *s = stream_of(a[9]);
+        return unlocked([&] {
+            return lib.block_norm_forward(&norm, h.p, h.ld, b.p, b.ld, out.p, out.ld, y.p, y.ld, rstd, h8.codes, h8.scales, b8.codes, b8.scales, s);
+        });
+    });
+}
+
+PyObject *block_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 14, [&] {
+        const Matrix dy = matrix_here(a[2]), dh = matrix_here(a[5]);
+        if (dh.rows != dy.rows || dh.cols != dy.cols) throw NotPlain();
+        const bool block = a[9] != Py_None;
+        const cdsgd_block_norm norm = norm_of_rows(a[0], a[1], dy, dh.dtype, block);
+        const cdsgd_held h = held(a[3], dy, dh.dtype), none = {nullptr, 0, nullptr, nullptr}, b = block ? held(a[9], dy, dy.dtype) : none;
+        const float *rstd = floats_here(a[4], 2 * dy.rows);
+        float *dw = floats_here(a[6], dy.cols);
+        size_t room = 0;
+        void *workspace = buffer_here(a[7], at::kByte, kAny, &room);
+        const Matrix dt = like(a[8], dy, dh.dtype, true), db = like(a[10], dy, dy.dtype, true);
+        float *dw_b = floats_here(a[11], dy.cols), *dgate = floats_here(a[12], dy.cols);
+        void *s = stream_of(a[13]);
+        return unlocked([&] {
+            return lib.block_norm_backward(&norm, dy.p, dy.ld, dt.p, dt.ld, &h, &b, rstd, dh.p, dh.ld, db.p, db.ld, dw, dw_b, dgate, workspace, room, s);
+        });
+    });
+}
+
+// [tokens, heads, dim] with a token's heads in a row.
+struct Heads {
+    void *p;
+    int dtype;
+    size_t tokens, heads, dim, ld;
+};
+
+Heads heads(PyObject *o)
+{
+    if (!THPVariable_CheckExact(o)) throw NotPlain();
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.dim() != 3) throw NotPlain();
+    Heads x;
+    if (t.scalar_type() == at::kBFloat16) x.dtype = CDSGD_GRAD_BF16;
+    else if (t.scalar_type() == at::kHalf) x.dtype = CDSGD_GRAD_F16;
+    else throw NotPlain();
+    const int64_t n = t.size(0), h = t.size(1), d = t.size(2), ld = n > 1 ? t.stride(0) : h * d;
+    if (n < 1 || h < 1 || d < 1 || h > INT_MAX || d > INT_MAX || (d > 1 && t.stride(2) != 1) || (h > 1 && t.stride(1) != d) || ld < h * d) throw NotPlain();
+    on_this_device(o);
+    x.p = t.data_ptr();
+    x.tokens = (size_t)n;
+    x.heads = (size_t)h;
+    x.dim = (size_t)d;
+    x.ld = (size_t)ld;
+    return x;
+}
+
+Heads heads_like(PyObject *o, const Heads &x)
+{
+    const Heads y = heads(o);
+    if (y.dtype != x.dtype || y.tokens != x.tokens || y.heads != x.heads || y.dim != x.dim) throw NotPlain();
+    return y;
+}
+
+cdsgd_attention batch_of(const Heads &q, const Heads &k, PyObject *starts, PyObject *starts_k, PyObject *causal, PyObject *scale)
+{
+    if (q.dtype != k.dtype || q.dim != k.dim || (causal != Py_True && causal != Py_False)) throw NotPlain();
+    cdsgd_attention b = {};
+    b.dtype = q.dtype;
+    b.causal = causal == Py_True;
+    b.tokens_q = q.tokens;
+    b.tokens_k = k.tokens;
+    b.num_seqs = 1;
+    b.heads = (int)q.heads;
+    b.kv_heads = (int)k.heads;
+    b.dim = (int)q.dim;
+    b.scale = scale == Py_None ? 1.0 / std::sqrt((double)q.dim) : real(scale);
+    if (starts == Py_None) {
+        if (starts_k != Py_None) throw NotPlain();
+        return b;
+    }
+    size_t count = 0;
+    b.starts_q = static_cast<const int32_t *>(buffer_here(starts, at::kInt, kAny, &count));
+    if (count < 2 || THPVariable_Unpack(starts).dim() != 1) throw NotPlain();
+    b.num_seqs = count - 1;
+    b.starts_k = static_cast<const int32_t *>(buffer_here(starts_k, at::kInt, count));
+    return b;
+}
+
+PyObject *attention_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 11, [&] {
+        const Heads q = heads(a[0]), k = heads(a[1]), v = heads_like(a[2], k), out = heads_like(a[3], q);
+        float *lse = floats_here(a[4], q.tokens * q.heads);
+        const cdsgd_attention b = batch_of(q, k, a[5], a[6], a[7], a[8]);
+        size_t room = 0;
+        void *workspace = buffer_here(a[9], at::kByte, kAny, &room);
+        void *s = stream_of(a[10]);
+        return unlocked([&] { return lib.attention_forward(&b, q.p, q.ld, k.p, k.ld, v.p, v.ld, out.p, out.ld, lse, workspace, room, s); });
+    });
+}
+
+PyObject *attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 15, [&] {
+        const Heads q = heads(a[1]), k = heads(a[2]), v = heads_like(a[3], k), dout = heads_like(a[0], q), out = heads_like(a[4], q);
+        const float *lse = floats_here(a[5], q.tokens * q.heads);
+        const Heads dq = heads_like(a[6], q), dk = heads_like(a[7], k), dv = heads_like(a[8], k);
+        const cdsgd_attention b = batch_of(q, k, a[9], a[10], a[11], a[12]);
+        size_t room = 0;
+        void *workspace = buffer_here(a[13], at::kByte, kAny, &room);
+        void *s = stream_of(a[14]);
+        return unlocked([&] {
+            return lib.attention_backward(&b, dout.p, dout.ld, q.p, q.ld, k.p, k.ld, v.p, v.ld, out.p, out.ld, lse, dq.p, dq.ld, dk.p, dk.ld, dv.p, dv.ld,
+                                          workspace, room, s);
+        });
+    });
+}
+
 // bind(addresses of the library's functions, in the order of `Library`)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -413,7 +688,11 @@ PyMethodDef methods[] = {method("bind", bind), method("quantize_pack", quantize_
                          method("grad_norm_compute", grad_norm_compute), method("adamw_step", adamw_step),
                          method("adamw_grad_norm", adamw_grad_norm), method("adamw_read_states", adamw_read_states),
                          method("mxfp4_quantize", mxfp4_quantize), method("mxfp4_dequantize", mxfp4_dequantize),
-                         method("mxfp4_matmul", mxfp4_matmul), {nullptr, nullptr, 0, nullptr}};
+                         method("mxfp4_matmul", mxfp4_matmul), method("mxint8_quantize", mxint8_quantize),
+                         method("mxint8_dequantize", mxint8_dequantize), method("gated_forward", gated_forward),
+                         method("gated_backward", gated_backward), method("block_norm_forward", block_norm_forward),
+                         method("block_norm_backward", block_norm_backward), method("attention_forward", attention_forward),
+                         method("attention_backward", attention_backward), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
