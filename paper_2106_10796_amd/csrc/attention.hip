@@ -23,14 +23,15 @@ inline unsigned long long groups_over(size_t tokens, size_t num_seqs, size_t eac
     return ((unsigned long long)tokens * each / tile + num_seqs) * kv_heads;
 }
 
-// Over how many groups the keys of a row are split: where the rows alone do not fill the card, as many as fill it twice, none of them
-// with fewer keys (of a sequence of ordinary length) than four tiles.
+// Over how many groups the keys of a row are split: where the rows alone do not fill the card, as many as fill it, none of them with fewer keys
+// (of a sequence of ordinary length) than four tiles.  One token of 32 heads over 8, 32768 keys, us, pass and join: 256 groups 24.1 + 6.0,
+// 512 24.7 + 8.5, 1024 25.8 + 14.1.
 inline unsigned splits_of(const cdsgd_attention &b)
 {
     const unsigned long long groups = groups_over(b.tokens_q, b.num_seqs, (size_t)(b.heads / b.kv_heads), kTileRows, (size_t)b.kv_heads);
     if (groups >= 256) return 1;
-    const unsigned long long want = (511 + groups) / groups, most = b.tokens_k / b.num_seqs / (4 * kTileKeys);
-    static_assert(kMostSplits >= 512, "of 512 groups all may share one row's keys");
+    const unsigned long long want = (255 + groups) / groups, most = b.tokens_k / b.num_seqs / (4 * kTileKeys);
+    static_assert(kMostSplits >= 256, "of 256 groups all may share one row's keys");
     return (unsigned)(want < most ? want : most < 1 ? 1 : most);
 }
 

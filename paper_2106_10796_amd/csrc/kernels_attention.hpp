@@ -37,7 +37,7 @@ template <int DT>
 constexpr float kLifted = DT == kGradF16 ? 32768.0f : 1.0f;
 
 constexpr unsigned kTileRows = 128;  // rows of a group of the forward pass and of dq, and keys of a group of dk and dv
-constexpr unsigned kMostSplits = 512;
+constexpr unsigned kMostSplits = 256;
 constexpr unsigned kTileKeys = 64;   // what a group takes at a time of the other side
 
 template <int DT>
