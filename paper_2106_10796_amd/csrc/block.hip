@@ -27,7 +27,8 @@ struct Layout {
     unsigned long long groups;
 };
 
-// Rows to a lane: `many` on large matrices, 1 where that leaves compute units idle.
+// Rows to a lane: `many` on large matrices, 1 where that leaves compute units idle.  (8192 x 4096 in bf16, us: quantisation with 4 rows to a
+// lane 24.0, 2 18.7; values 18.8, 16.5.)
 inline Layout layout_of(size_t rows, size_t cols, unsigned each, unsigned many)
 {
     Layout y = {each == 4 ? 3u : 2u, many, 0};
@@ -135,13 +136,13 @@ int cdsgd_mxint8_quantize(const void *x, int dtype, size_t rows, size_t cols, si
     if (any_overlap(out, 2, in, 1)) return CDSGD_ERR_ALIAS;
     with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        const Layout y = layout_of(rows, cols, kEach<DT>, 4);
+        const Layout y = layout_of(rows, cols, kEach<DT>, 2);
         status = in_launches(y.groups, 256, [&](dim3 grid, unsigned first) {
             const auto launch = [&](auto kernel) {
                 hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)hip_stream, static_cast<const Elem<DT> *>(x), ld, (unsigned)rows,
                                    (unsigned)cols, codes, scales, y.lanes_log2, first);
             };
-            if (y.rows == 4) launch(k_held8_quantize<DT, 4>);
+            if (y.rows == 2) launch(k_held8_quantize<DT, 2>);
             else launch(k_held8_quantize<DT, 1>);
         });
     });
@@ -161,13 +162,13 @@ int cdsgd_mxint8_dequantize(const int8_t *codes, const uint8_t *scales, size_t r
     if (any_overlap(to, 1, in, 2)) return CDSGD_ERR_ALIAS;
     with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        const Layout y = layout_of(rows, cols, kEach<DT>, 4);
+        const Layout y = layout_of(rows, cols, kEach<DT>, 2);
         status = in_launches(y.groups, 256, [&](dim3 grid, unsigned first) {
             const auto launch = [&](auto kernel) {
                 hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)hip_stream, codes, scales, (unsigned)rows, (unsigned)cols,
                                    static_cast<Elem<DT> *>(out), ld, y.lanes_log2, first);
             };
-            if (y.rows == 4) launch(k_held8_values<DT, 4>);
+            if (y.rows == 2) launch(k_held8_values<DT, 2>);
             else launch(k_held8_values<DT, 1>);
         });
     });
