@@ -27,7 +27,8 @@ extern "C" {
  * An element is code * 2^(s - 133) with its block's s; s = 255 is NaN throughout the block.
  * cdsgd_mxint8_quantize    s is the exponent field of the block's largest magnitude as an fp32 number, the code x * 2^(133 - s) rounded to
  *                          nearest, ties to even, and to 127 at most.  A NaN or an infinity in a block makes its s 255 and its codes 0.
- * cdsgd_mxint8_dequantize  the values, rounded once if the type has not enough bits (bf16 and fp32 have: fp16 not below 2^-18 of s - 133)
+ * cdsgd_mxint8_dequantize  the values, rounded once where the type has no such number (fp16 has none above 65504, and small ones with fewer bits).
+ *                          A code of -128, which nothing here writes, is read as -128.
  */
 size_t cdsgd_mxint8_code_bytes(size_t rows, size_t cols);
 size_t cdsgd_mxint8_scale_bytes(size_t rows, size_t cols);
@@ -116,7 +117,7 @@ int cdsgd_block_norm_backward(const cdsgd_block_norm *norm, const void *dy, size
  *   workspace     cdsgd_attention_workspace bytes for either pass, 16-byte aligned, NULL where that is 0.  Calls that share one must be ordered;
  *                 its content means nothing between calls.
  *   errors        CDSGD_ERR_PARAM: dtype, causal not 0 or 1, heads not a multiple of kv_heads, starts_k without starts_q, no starts and
- *                 num_seqs not 1, scale not finite or not above 0.  CDSGD_ERR_SIZE: dim, a count of 0, tokens 2^31 and more, num_seqs 2^24 and more,
+ *                 num_seqs not 1, scale below 1e-30 or above 1e30.  CDSGD_ERR_SIZE: dim, a count of 0, tokens 2^31 and more, num_seqs 2^24 and more,
  *                 heads above 65535, more work than a launch holds, too small a workspace.
  */
 typedef struct {
@@ -124,7 +125,7 @@ typedef struct {
     size_t tokens_q, tokens_k, num_seqs;
     const int32_t *starts_q, *starts_k;
     int heads, kv_heads, dim;
-    double scale;
+    double scale; /* from 1e-30 to 1e30 */
 } cdsgd_attention;
 
 size_t cdsgd_attention_workspace(const cdsgd_attention *batch, int backward);

@@ -931,10 +931,9 @@ def _on_this_device(*tensors):
     """Calls work on the current device: that is where their tensors are."""
     here = torch.cuda.current_device()
     for t in tensors:
-        if isinstance(t, Mxint8):
-            t = t.codes
-        if t is not None and t.device.index != here:
-            raise ValueError("a tensor is not on the current device")
+        for x in t[:2] if isinstance(t, Mxint8) else (t,):
+            if x is not None and x.device.index != here:
+                raise ValueError("a tensor is not on the current device")
 
 
 def cdsgd_mxint8_quantize(x, q):

@@ -2,7 +2,6 @@
 
 #include <hip/hip_runtime.h>
 
-#include <cmath>
 #include <cstdint>
 
 #include "cdsgd_block.h"
@@ -41,7 +40,7 @@ int check_batch(const cdsgd_attention *a)
 {
     if (!a) return CDSGD_ERR_NULL;
     if ((a->dtype != CDSGD_GRAD_BF16 && a->dtype != CDSGD_GRAD_F16) || (a->causal != 0 && a->causal != 1) || (a->starts_k && !a->starts_q) ||
-        (!a->starts_q && a->num_seqs != 1) || !std::isfinite((float)a->scale) || !((float)a->scale > 0))
+        (!a->starts_q && a->num_seqs != 1) || !(a->scale >= 1e-30 && a->scale <= 1e30))
         return CDSGD_ERR_PARAM;
     if (!good_extent(a->tokens_q) || !good_extent(a->tokens_k) || a->num_seqs < 1 || a->num_seqs >= (size_t)1 << 24 || a->heads < 1 ||
         a->heads > 65535 || a->kv_heads < 1 || a->dim < 8 || a->dim > 128 || a->dim % 8)

@@ -40,7 +40,7 @@ __device__ __forceinline__ void load_weight(const float *w, unsigned cols, unsig
 }
 
 // Weights of a lane's elements: in registers throughout where there are few of them, or read again (from L2) for every row.
-constexpr int kKeptWeights = 16;
+constexpr int kKeptWeights = 8;
 
 // A group goes from row to row, and asks for the next one's elements before it sums this one's.  Bound by HBM and by the two sums that a row
 // waits for: 8192 x 4096 in bf16 on an fp32 stream 88 us, 4.6 TB/s (weights read again for every row, and nothing asked for ahead: 105).

@@ -396,7 +396,6 @@ PyObject *mxfp4_matmul(PyObject *, PyObject *const *a, Py_ssize_t n)
 void on_this_device(PyObject *o)
 {
     if (o == Py_None) return;
-    if (PyTuple_Check(o)) o = PyTuple_GET_ITEM(o, 0);  // (a matrix in 8 bits: its codes, which mx8 has looked at)
     if (THPVariable_Unpack(o).get_device() != at::detail::getCUDAHooks().getCurrentDevice()) throw NotPlain();
 }
 
@@ -448,7 +447,8 @@ Mx8 mx8(PyObject *o)
     q.cols = (size_t)cols;
     q.codes = static_cast<int8_t *>(buffer(PyTuple_GET_ITEM(o, 0), at::kChar, q.rows * 32 * groups));
     q.scales = static_cast<uint8_t *>(buffer(PyTuple_GET_ITEM(o, 1), at::kByte, q.rows * groups));
-    on_this_device(o);
+    on_this_device(PyTuple_GET_ITEM(o, 0));
+    on_this_device(PyTuple_GET_ITEM(o, 1));
     return q;
 }
 
