@@ -351,7 +351,7 @@ int cdsgd_block_norm_backward(const cdsgd_block_norm *norm, const void *dy, size
             else launch(k_block_norm_backward<ST, DT, W, V, false, false>);
         });
     });
-    hipLaunchKernelGGL(k_block_norm_join, dim3((unsigned)((n.cols + 31) / 32), dblock_weight || dgate ? 2 : 1), dim3(256), 0, (hipStream_t)hip_stream,
+    hipLaunchKernelGGL(k_block_norm_join, dim3((unsigned)((n.cols + 31) / 32), dblock_weight || dgate ? 2 : 1), dim3(1024), 0, (hipStream_t)hip_stream,
                        (const float *)parts, groups, (unsigned)n.cols, by, dweight, dblock_weight, dgate);
     return launch_status();
 }

@@ -42,6 +42,13 @@ __device__ __forceinline__ void load_weight(const float *w, unsigned cols, unsig
 // Weights of a lane's elements: in registers throughout where there are few of them, or read again (from L2) for every row.
 constexpr int kKeptWeights = 8;
 
+// The next row's elements are asked for ahead where there is room for them (forward and backward, us, 4096 x 8192 in bf16 on an fp32 stream, 8 waves
+// of four fours: ahead 126, 147, not 103, 163;  2048 x 12288, 16 waves: 158, 368, not 106, 236).
+template <int WAVES, int V>
+constexpr bool kForwardAhead = V <= 2;
+template <int WAVES, int V>
+constexpr bool kBackwardAhead = V <= 2 || WAVES <= 8;
+
 // A group goes from row to row, and asks for the next one's elements before it sums this one's.  Bound by HBM and by the two sums that a row
 // waits for: 8192 x 4096 in bf16 on an fp32 stream 88 us, 4.6 TB/s (weights read again for every row, and nothing asked for ahead: 105).
 template <int ST, int DT, int WAVES, int V>
@@ -81,8 +88,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm_forward(NormWeights b
         }
     };
     const double mean = 1.0 / cols;
-    ask(blockIdx.x);
+    if constexpr (kForwardAhead<WAVES, V>) ask(blockIdx.x);
     for (size_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        if constexpr (!kForwardAhead<WAVES, V>) ask(r);
         Few<DT, E> eb[V];
         float v[V][E];
 #pragma unroll
@@ -90,7 +98,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm_forward(NormWeights b
             widened<ST, E>(next_h[k], v[k]);
             eb[k] = next_b[k];
         }
-        if (r + gridDim.x < rows) ask(r + gridDim.x);
+        if (kForwardAhead<WAVES, V> && r + gridDim.x < rows) ask(r + gridDim.x);
         double n = 1.0, sum = 0;
         if (by.block_weight) {
 #pragma unroll
@@ -205,10 +213,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm_backward(NormWeights 
         next.r = rstd[r];
         if (by.block_weight) next.n = rstd[(size_t)rows + r];
     };
-    ask(blockIdx.x);
+    if constexpr (kBackwardAhead<WAVES, V>) ask(blockIdx.x);
     for (size_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        if constexpr (!kBackwardAhead<WAVES, V>) ask(r);
         const auto now = next;
-        if (r + gridDim.x < rows) ask(r + gridDim.x);
+        if (kBackwardAhead<WAVES, V> && r + gridDim.x < rows) ask(r + gridDim.x);
         float x[V][E], t[V][E], part = 0.0f;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
@@ -262,19 +271,20 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm_backward(NormWeights 
     }
 }
 
-// The groups' sums, joined in 64 bits in an order of their own number alone: 8 lanes take 32 columns, and 32 times as many every 32nd of the
-// parts each.
-__global__ __launch_bounds__(256) void k_block_norm_join(const float *__restrict__ parts, unsigned groups, unsigned cols, NormWeights by,
+// The groups' sums, joined in 64 bits in an order of their own number alone: 8 lanes take 32 columns, and 128 times as many every 128th of the
+// parts each (2048 parts of 1024 columns 21 us with 32 of them).
+__global__ __launch_bounds__(1024) void k_block_norm_join(const float *__restrict__ parts, unsigned groups, unsigned cols, NormWeights by,
                                                          float *__restrict__ dweight, float *__restrict__ dblock_weight,
                                                          float *__restrict__ dgate)
 {
-    __shared__ double room[32][33];
+    constexpr unsigned kJoined = 128;
+    __shared__ double room[kJoined][33];
     const unsigned slice = threadIdx.x / 8u, first = threadIdx.x % 8u * 4u, c0 = blockIdx.x * 32u, pitch = (cols + 3u) / 4u * 4u;
     const bool second = blockIdx.y != 0;
     double sum[4] = {};
     const f4 *p = reinterpret_cast<const f4 *>(parts + (second ? pitch : 0u) + (c0 + first < pitch ? c0 + first : 0u));
 #pragma unroll 8
-    for (unsigned g = slice; g < groups; g += 32u) {
+    for (unsigned g = slice; g < groups; g += kJoined) {
         const f4 x = p[(size_t)g * (pitch / 2u)];
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[i] += (double)x[i];
@@ -285,8 +295,8 @@ __global__ __launch_bounds__(256) void k_block_norm_join(const float *__restrict
     const unsigned c = c0 + threadIdx.x;
     if (threadIdx.x >= 32u || c >= cols) return;
     double all = room[0][threadIdx.x];
-#pragma unroll
-    for (unsigned k = 1; k < 32; ++k) all += room[k][threadIdx.x];
+#pragma unroll 16
+    for (unsigned k = 1; k < kJoined; ++k) all += room[k][threadIdx.x];
     if (!second) {
         dweight[c] = (float)all;
     } else {
