@@ -332,13 +332,6 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(AttentionSizes z, 
     const long long hidden_from = (long long)s.keys - s.queries + 1;  // query i sees keys below i + this
 
     const unsigned head0 = kv * z.group;
-    const __amdgpu_buffer_rsrc_t from_q = buffer_at(q.p + (size_t)(s.q0 + first_query) * q.ld + head0 * z.dim);
-    s8v bq[DP / 16];
-#pragma unroll
-    for (unsigned i = 0; i < DP / 16; ++i) bq[i] = load16(from_q, row_offset(skip + row, skip + rows, z.group, q.ld, 16u * i + 8u * half, z.dim));
-
-    landed(bq);
-
     // keys that a row sees, that all of the tile's together see, and that each of the wave's sees
     const auto seen = [&](unsigned r) __attribute__((always_inline)) -> unsigned {
         if (!z.causal) return s.keys;
@@ -366,6 +359,12 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(AttentionSizes z, 
     };
     unsigned buffer = 0;
     if (from < to) ask(from, 0);
+    // asked for behind the first tile, which is on its way meanwhile (one token over 32768 keys 24.3 -> 23.4 us)
+    const __amdgpu_buffer_rsrc_t from_q = buffer_at(q.p + (size_t)(s.q0 + first_query) * q.ld + head0 * z.dim);
+    s8v bq[DP / 16];
+#pragma unroll
+    for (unsigned i = 0; i < DP / 16; ++i) bq[i] = load16(from_q, row_offset(skip + row, skip + rows, z.group, q.ld, 16u * i + 8u * half, z.dim));
+    landed(bq);
     for (unsigned j = from; j < to; j += kTileKeys) {
         wait_for_loads<0>();
         __syncthreads();
@@ -655,20 +654,10 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
     const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), stream = wave / KW, side = wave % KW;
     const unsigned l = threadIdx.x % 64u, half = l / 32u, key = side * 32u + l % 32u, head0 = kv * z.group;
 
-    const __amdgpu_buffer_rsrc_t from_k = buffer_at(k.p + (size_t)(s.k0 + key0) * k.ld + kv * z.dim);
-    const __amdgpu_buffer_rsrc_t from_v = buffer_at(v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim);
-    s8v bk[DP / 16], bv[kValuesInLds ? 1 : DP / 16];
-#pragma unroll
-    for (unsigned i = 0; i < DP / 16; ++i) {
-        bk[i] = load16(from_k, row_offset(key, keys, 1u, k.ld, 16u * i + 8u * half, z.dim));
-        if constexpr (!kValuesInLds) bv[i] = load16(from_v, row_offset(key, keys, 1u, v.ld, 16u * i + 8u * half, z.dim));
-    }
     if constexpr (kValuesInLds) {
         const TileLoads<DP, kKeys, KW * S> loads_v(wave, 1u, v.ld, z.dim);
         loads_v.ask(values, wave, v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim, ((keys - 1u) * v.ld + z.dim) * 2u);
     }
-    landed(bk);
-    if constexpr (!kValuesInLds) landed(bv);
     // the first query that sees key j is j - (keys - queries)
     const long long later = (long long)s.queries - s.keys;
     const auto first_of = [&](unsigned j) __attribute__((always_inline)) -> unsigned {
@@ -701,6 +690,16 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
     Operands<DP> operand;
     unsigned buffer = 0;
     if (tiles) ask(stream, 0);
+    const __amdgpu_buffer_rsrc_t from_k = buffer_at(k.p + (size_t)(s.k0 + key0) * k.ld + kv * z.dim);
+    const __amdgpu_buffer_rsrc_t from_v = buffer_at(v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim);
+    s8v bk[DP / 16], bv[kValuesInLds ? 1 : DP / 16];
+#pragma unroll
+    for (unsigned i = 0; i < DP / 16; ++i) {
+        bk[i] = load16(from_k, row_offset(key, keys, 1u, k.ld, 16u * i + 8u * half, z.dim));
+        if constexpr (!kValuesInLds) bv[i] = load16(from_v, row_offset(key, keys, 1u, v.ld, 16u * i + 8u * half, z.dim));
+    }
+    landed(bk);
+    if constexpr (!kValuesInLds) landed(bv);
     for (unsigned first = 0; first < tiles; first += S) {
         wait_for_loads<0>();
         __syncthreads();
