@@ -23,7 +23,7 @@ inline unsigned long long groups_over(size_t tokens, size_t num_seqs, size_t eac
 }
 
 // Over how many groups the keys of a row are split: where the rows alone do not fill the card, as many as fill it, none of them with fewer keys
-// (of a sequence of ordinary length) than four tiles.  One token of 32 heads over 8, 32768 keys, us, pass and join: 256 groups 24.1 + 6.0,
+// (of a sequence of ordinary length) than four tiles.  One token of 32 heads over 8, 32768 keys, us, pass and join: 256 groups 23.4 + 5.7,
 // 512 24.7 + 8.5, 1024 25.8 + 14.1.
 inline unsigned splits_of(const cdsgd_attention &b)
 {

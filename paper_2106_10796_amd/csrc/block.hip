@@ -63,7 +63,7 @@ inline int check_held(const cdsgd_held *x, size_t rows, size_t cols, int dtype, 
 constexpr size_t kMostCols = 16384;
 
 // Groups of the norm's backward pass, which leave their sums over rows: enough to fill the card, few enough that joining them
-// costs little beside the pass (us, pass and join, 8192 x 4096: 1024 groups 130 + 24, 512 104 + 7; 1003 x 2049: 1003 15 + 20, 256 15 + 4).
+// costs little beside the pass (us, pass and join, 8192 x 4096: 1024 groups 113 + 8.7, 512 107 + 6.2; 1003 x 2049: 1003 16 + 9.5, 256 15 + 4.2).
 inline unsigned norm_groups(size_t rows, size_t cols)
 {
     const size_t most = ((size_t)1 << 21) / cols, want = most < 128 ? 128 : most > 2048 ? 2048 : most;
