@@ -485,22 +485,42 @@ __global__ __launch_bounds__(256) void k_attention_join(AttentionSizes z, Heads<
 // ---------------------------------------------------------------------------
 // backward
 // ---------------------------------------------------------------------------
-// A power of two that brings numbers up to `most` to about 1 (1 where most is 0 or not finite).
-__device__ __forceinline__ float to_one(float most)
-{
-    const unsigned e = __builtin_bit_cast(unsigned, most) >> 23 & 0xFFu;
-    return e == 0u || e > 253u ? 1.0f : __builtin_bit_cast(float, (254u - e) << 23);
-}
+// dS of fp16 tensors is an operand times a power of two of its own, a row's in dq and a key's in dk (either is a lane's): fp16 ends at 65504, which
+// |dS| passes where values are large, and loses bits below 2^-14, where a flat row of many keys has all of it.  `fit` is given numbers that are
+// multiplied by `by` already.  The first that are not 0 bring the largest to 2^7 ... 2^8, later ones above 2^15 bring it there again, and what is summed up
+// is multiplied with them: nothing is lost of a number but below 2^-32 of the largest.  (7999 tokens in 16 sequences, 12 heads of 64, not causal, us: dq
+// 42 -> 45 and dk, dv 69 -> 62 with it in place of one power of two of dout's largest magnitude, which dk and dv's rows had to be searched for.)
+struct Lift {
+    float by = 1.0f;
+    bool begun = false;
+
+    template <int N>
+    __device__ __forceinline__ void fit(f16v &y, f16v (&acc)[N])
+    {
+        float most = 0.0f;
+#pragma unroll
+        for (unsigned r = 0; r < 16; ++r) most = __builtin_fmaxf(most, __builtin_fabsf(y[r]));
+        most = larger_half(most);
+        const bool change = most > 32768.0f || (!begun && most > 0.0f);
+        if (__builtin_amdgcn_ballot_w64(change) == 0) return;
+        const unsigned e = __builtin_bit_cast(unsigned, most) >> 23, to = 261u - e;  // (of most's exponent field e, that of 2^7 over its power of two)
+        const float f = !change || e == 255u ? 1.0f : __builtin_bit_cast(float, (to < 227u ? to : 227u) << 23);
+        begun = begun || change;
+        by *= f;
+        y *= f;
+#pragma unroll
+        for (int d = 0; d < N; ++d) acc[d] *= f;
+    }
+};
 
 // dq, and with it the first kernel of the backward pass: tiles as in the forward pass, three products for its two.  4096 tokens, 32 heads of 128 over 8,
 // not causal: 370 us, 1.1 PFLOP/s, bound as the forward pass is; 8191 tokens in 8 sequences, causal: 163.
-// For the next kernel row_lse receives what S begins with in every row, (lift - lse log2 e) / c, delta -dout . out, and size (of fp16 tensors)
-// the largest magnitude in dout, all [kv head][token][head of the group].
+// For the next kernel row_lse receives what S begins with in every row, (lift - lse log2 e) / c, and delta -dout . out, both
+// [kv head][token][head of the group].
 template <int DT, int DP>
 __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
                                                       Heads<const Elem<DT>> v, Heads<const Elem<DT>> out, const float *__restrict__ lse,
-                                                      Heads<Elem<DT>> dq, float *__restrict__ row_lse, float *__restrict__ delta,
-                                                      float *__restrict__ size)
+                                                      Heads<Elem<DT>> dq, float *__restrict__ row_lse, float *__restrict__ delta)
 {
     constexpr unsigned kTile = kTileKeys * DP * 2;
     __shared__ __align__(1024) unsigned char smem[4 * kTile];  // two tiles of keys and of values
@@ -522,7 +542,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
     const __amdgpu_buffer_rsrc_t from_d = buffer_at(dout.p + token * dout.ld + head0 * z.dim);
     const __amdgpu_buffer_rsrc_t from_o = buffer_at(out.p + token * out.ld + head0 * z.dim);
     s8v bq[DP / 16], bd[DP / 16];
-    float sum = 0.0f, largest = 0.0f;
+    float sum = 0.0f;
 #pragma unroll
     for (unsigned i = 0; i < DP / 16; ++i) {
         typedef Elem<DT> e8 __attribute__((ext_vector_type(8)));
@@ -532,16 +552,11 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
         const e8 o = __builtin_bit_cast(e8, load16(from_o, row_offset(skip + row, skip + rows, z.group, out.ld, d, z.dim)));
         const e8 g = __builtin_bit_cast(e8, bd[i]);
 #pragma unroll
-        for (unsigned e = 0; e < 8; ++e) {
-            sum = __builtin_fmaf((float)g[e], (float)o[e], sum);
-            largest = __builtin_fmaxf(largest, __builtin_fabsf((float)g[e]));
-        }
+        for (unsigned e = 0; e < 8; ++e) sum = __builtin_fmaf((float)g[e], (float)o[e], sum);
     }
     sum = sum_of_halves(sum);
-    largest = larger_half(largest);
     // (a row that sees nothing, and one that is not there, has no share in anything)
     const float log_sum = row < rows ? lse[at] : kInfinity, base = log_sum == -kInfinity ? kInfinity : log_sum * kLog2e;
-    const float up = DT == kGradF16 ? to_one(largest) : 1.0f;
     landed(bq);
     landed(bd);
     const float c = z.scale * kLog2e;
@@ -549,7 +564,6 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
         const size_t place = ((size_t)kv * z.tokens_q + s.q0 + query) * z.group + head - head0;
         row_lse[place] = (kLiftBack<DT> - base) / c;
         delta[place] = -sum;
-        if (DT == kGradF16) size[place] = largest;
     }
 
     const auto seen = [&](unsigned r) __attribute__((always_inline)) -> unsigned {
@@ -566,6 +580,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
         loads_v.ask(lds + b * 2u * kTile + kTile, wave, v.p + (size_t)(s.k0 + j) * v.ld + kv * z.dim, ((left - 1u) * v.ld + z.dim) * 2u);
     };
     Operands<DP> operand;
+    Lift lift;
     unsigned buffer = 0;
     if (to) ask(0, 0);
     for (unsigned j = 0; j < to; j += kTileKeys) {
@@ -605,8 +620,9 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
 #pragma unroll
             for (unsigned r = 0; r < 16; ++r) {
                 y[r] -= sum;
-                y[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -base)) * (DT == kGradF16 ? y[r] * up : y[r]);
+                y[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -base)) * (DT == kGradF16 ? y[r] * lift.by : y[r]);
             }
+            if constexpr (DT == kGradF16) lift.fit(y, acc);
 #pragma unroll
             for (unsigned h = 0; h < 2; ++h) {
                 const s8v ds = rounded<DT>(y, h);
@@ -615,7 +631,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
             }
         }
     }
-    if (row < rows) store_row<DT, DP>(dq.p + (size_t)(s.q0 + query) * dq.ld + head * z.dim, acc, z.scale / up, z.dim);
+    if (row < rows) store_row<DT, DP>(dq.p + (size_t)(s.q0 + query) * dq.ld + head * z.dim, acc, z.scale / lift.by, z.dim);
 }
 
 // dk and dv.  A group takes the keys of kKeyWaves waves, 32 each, of one key head and runs over the rows that see them, in kStreams streams:
@@ -635,11 +651,11 @@ constexpr unsigned kStreamKeys = 32 * kKeyWaves<DP>;
 template <int DT, int DP>
 __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attention_dkv(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
                                                        Heads<const Elem<DT>> v, const float *__restrict__ all_lse, const float *__restrict__ delta,
-                                                       const float *__restrict__ size, Heads<Elem<DT>> dk, Heads<Elem<DT>> dv)
+                                                       Heads<Elem<DT>> dk, Heads<Elem<DT>> dv)
 {
     constexpr bool kValuesInLds = DP == 128;
     constexpr unsigned KW = kKeyWaves<DP>, S = kStreams<DP>, kKeys = kStreamKeys<DP>;
-    // of a stream, twice: a tile of q, one of dout, and three numbers of each row
+    // of a stream, twice: a tile of q, one of dout, and two numbers of each row
     constexpr unsigned kRows = kStreamRows, kTile = kRows * DP * 2, kStage = 2 * kTile + 1024, kValues = S * 2 * kStage;
     constexpr unsigned kSums = 32 * DP * 4;  // of a wave's results of one kind
     static_assert((S - 1) * KW * kSums <= kValues, "the streams' sums fit where their tiles were");
@@ -666,8 +682,7 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
     };
     f16v acc_k[DP / 32] = {}, acc_v[DP / 32] = {};
     const float c = z.scale * kLog2e;
-    float up = 1.0f;
-    bool begun = false;
+    Lift lift;
     // A tile is as many queries as have kRows rows at most, or (`parts` of them) a part of one query's heads.
     const unsigned group = z.group, at_once = group < kRows ? kRows / group : 1u, parts = (group + kRows - 1u) / kRows;
     const unsigned from = first_of(key0), tiles = (s.queries - from + at_once - 1u) / at_once * parts;
@@ -685,7 +700,6 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
         loads_d.ask(to + kTile, side, dout.p + token * dout.ld + (head0 + part) * z.dim, queries ? (far * dout.ld + heads * z.dim) * 2u : 0u);
         const size_t at = ((size_t)kv * z.tokens_q + token) * group + part;
         if (KW == 2 || side < 2u) load_to_lds<4>(same_in_all(buffer_of(numbers + at, queries * heads * 4u)), to + 2u * kTile + side * 256u, l * 4u);
-        if (DT == kGradF16 && side == 0u) load_to_lds<4>(same_in_all(buffer_of(size + at, queries * heads * 4u)), to + 2u * kTile + 512u, l * 4u);
     };
     Operands<DP> operand;
     unsigned buffer = 0;
@@ -706,25 +720,10 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
         const unsigned n = first + stream, now = from + n / parts * at_once;
         if (first + S < tiles) ask(n + S, buffer ^ 1u);
         const unsigned at = buffer;
-        const CDSGD_LDS float *row_lse = (const CDSGD_LDS float *)(lds + (stream * 2u + at) * kStage + 2u * kTile), *row_delta = row_lse + 64, *row_size = row_lse + 128;
+        const CDSGD_LDS float *row_lse = (const CDSGD_LDS float *)(lds + (stream * 2u + at) * kStage + 2u * kTile), *row_delta = row_lse + 64;
         buffer ^= 1u;
         if (side * 32u >= keys || n >= tiles) continue;
         operand.renew();
-        if constexpr (DT == kGradF16) {
-            float largest = row_size[l % kRows];
-#pragma unroll
-            for (int m = 1; m < 32; m *= 2) largest = __builtin_fmaxf(largest, __shfl_xor(largest, m));
-            largest = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, largest)));
-            const float want = to_one(largest);
-            if (largest > 0.0f && (!begun || want < up)) {
-                if (begun) {
-#pragma unroll
-                    for (unsigned d = 0; d < DP / 32; ++d) acc_k[d] *= want / up;
-                }
-                up = want;
-                begun = true;
-            }
-        }
         // S less lse, and dP less delta: both begin with what is taken from them.  The operands of a pair of products are read beside the pair before.
         f16v x, y;
 #pragma unroll
@@ -763,12 +762,13 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
             for (unsigned r = 0; r < 16; ++r)
                 if (row_of(r, half) < hidden) x[r] = -kInfinity, y[r] = 0.0f;
         }
-        const float down = up * (1.0f / kLifted<DT>);
+        const float down = lift.by * (1.0f / kLifted<DT>);
 #pragma unroll
         for (unsigned r = 0; r < 16; ++r) {
             x[r] = __builtin_amdgcn_exp2f(x[r] * c);
             y[r] = x[r] * (DT == kGradF16 ? y[r] * down : y[r]);
         }
+        if constexpr (DT == kGradF16) lift.fit(y, acc_k);
         const s8v p[2] = {rounded<DT>(x, 0), rounded<DT>(x, 1)}, ds[2] = {rounded<DT>(y, 0), rounded<DT>(y, 1)};
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -783,7 +783,7 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
     // the streams' sums, added in their order
     wait_for_loads<0>();
     __syncthreads();
-    const float f = z.scale / up;
+    const float f = z.scale / lift.by;
     CDSGD_LDS f4 *const sums = (CDSGD_LDS f4 *)lds;
 #pragma unroll
     for (unsigned which = 0; which < 2; ++which) {

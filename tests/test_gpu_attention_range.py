@@ -1,0 +1,103 @@
+"""Attention's gradients where values, gradients or logits are far from 1, against plain implementations in 64 bits.
+
+Tolerances count roundings as those of test_gpu_attention.py do, but that dS of fp16 tensors is off by at most 2^-32 of the largest |dS| that it is summed
+up with, a row's for dq and a key's for dk: its power of two brings the largest so far to 2^7 at least, and half a step of fp16's smallest numbers is 2^-25."""
+import pytest
+import torch
+
+from paper_2106_10796_amd import binding as B
+from test_gpu_attention import SMALL, U, close, half_step, inputs, logit_error, probabilities, reference, starts_of, tiny, tiny_p
+
+pytestmark = pytest.mark.gpu
+
+
+def run(dout, q, k, v, lens_q, lens_k, causal, scale):
+    room = B.new_attention_workspace(q, k, seqs=len(lens_q), train=True)
+    out, lse, grads = torch.empty_like(q), torch.empty(q.shape[1], q.shape[0], device="cuda"), [torch.empty_like(t) for t in (q, k, v)]
+    starts = starts_of(lens_q), starts_of(lens_k)
+    B.cdsgd_attention_forward(q, k, v, out, lse, *starts, causal, scale, room)
+    B.cdsgd_attention_backward(dout, q, k, v, out, lse, *grads, *starts, causal, scale, room)
+    return out, lse, grads
+
+
+def check_gradients(dout, q, k, v, out, lse, grads, lens_q, lens_k, causal, scale, exact_logits=False):
+    """exact_logits: the products q . k are exact in fp32, whatever their order, so that what is left of a logit's error is that of differences."""
+    u, dim, f16 = half_step(q), q.shape[2], q.dtype == torch.float16
+    dq, dk, dv = grads
+    for rows, cols, h, mine, s, size, x, y, z in reference(q, k, v, lens_q, lens_k, causal, scale):
+        nq, nk = s.shape[1], s.shape[2]
+        do, o = (t[rows, mine].double().transpose(0, 1).contiguous() for t in (dout, out))
+        at = torch.logsumexp(s, 2) if exact_logits else lse[mine, rows].double()
+        p = probabilities(s, at)
+        e_p = 2 * U * (8 * torch.where(torch.isinf(s), 0.0, s - at[..., None]).abs() + 16 + nk) if exact_logits else 2 * logit_error(s, size, at, dim)
+        dp, delta = torch.matmul(do, z.t().contiguous()), (do * o).sum(2, keepdim=True)
+        ds = p * (dp - delta)
+        e_ds = ds.abs() * (u + e_p) + 2 * U * dim * p * (torch.matmul(do.abs(), z.abs().t().contiguous()) + (do * o).abs().sum(2, keepdim=True))
+        e_ds = e_ds + 2 * SMALL * (1 + (dp - delta).abs())
+        least = 2.0 ** -32 * (ds.abs() + e_ds) * (p > 0) if f16 else torch.zeros_like(ds)
+        of_row, of_key = least.amax(2, keepdim=True) * (p > 0), least.amax((0, 1), keepdim=True) * (p > 0)
+        want = scale * torch.matmul(ds, y)
+        close(dq[rows, mine].transpose(0, 1), want, scale * torch.matmul(e_ds + of_row + 2 * U * nk * ds.abs(), y.abs()) + u * want.abs() + tiny(q), "dq")
+        n = nq * s.shape[0]
+        e_v = p * (u + e_p) + 2 * SMALL + tiny_p(q, 15)
+        for got, w, e_w, other, what, f in ((dk, ds, e_ds + of_key, x, "dk", scale), (dv, p, e_v, do, "dv", 1.0)):
+            flat = lambda t: t.reshape(n, t.shape[2])  # noqa: E731
+            want = f * torch.matmul(flat(w).t().contiguous(), flat(other))
+            error = f * torch.matmul((flat(e_w) + 2 * U * n * flat(w).abs()).t().contiguous(), flat(other).abs()) + u * want.abs() + tiny(q)
+            close(got[cols, h], want, error, what)
+
+
+def go(dout, q, k, v, lens_q, lens_k, causal, scale=None):
+    scale = q.shape[2] ** -0.5 if scale is None else scale
+    out, lse, grads = run(dout, q, k, v, lens_q, lens_k, causal, scale)
+    check_gradients(dout, q, k, v, out, lse, grads, lens_q, lens_k, causal, scale)
+    return grads
+
+
+def test_dS_above_the_largest_number_of_fp16():
+    """Two keys with values of 1100 and -1100: dS is 70400 and -70400, the gradients ordinary numbers."""
+    full = lambda n, x: torch.full((n, 1, 128), x, dtype=torch.float16, device="cuda")  # noqa: E731
+    sign = torch.tensor([1.0, -1.0], device="cuda").half()[:, None, None]
+    dq, dk, dv = go(full(1, 1.0), full(1, 0.0), full(2, 0.01) * sign, full(2, 1100.0) * sign, [1], [2], False)
+    assert bool(torch.isfinite(dq).all()) and float(dq[0, 0, 0]) == pytest.approx(2 * 70400 * float(torch.tensor(0.01).half()) / 128 ** 0.5, rel=2.0 ** -9)
+    assert bool((dk == 0).all()) and bool((dv == 0.5).all())
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("v_size,dout_size", [(0.02, 1.0), (0.005, 1e-3), (4e3, 1.0), (4e3, 1e-4), (1.0, 30.0), (1e-4, 1e-4), (2e4, 1.0)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_values_and_gradients_of_any_size(v_size, dout_size, causal, dim):
+    lens = [40, 300]
+    q, k, v, dout = inputs(lens, lens, 4, 2, dim, "f16", seed=11)
+    go((dout.float() * dout_size).half(), q, k, (v.float() * v_size).clamp(-65504, 65504).half(), lens, lens, causal)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("v_size", [1.0, 0.02, 0.005])
+@pytest.mark.parametrize("keys", [16384, 40000])
+def test_flat_rows_of_many_keys(keys, v_size, dtype):
+    """Probabilities of 1 over the number of keys: dS of a row is small throughout."""
+    q, k, v, dout = inputs([3], [keys], 2, 1, 128, dtype, seed=12)
+    go(dout, q * 0.1, k, (v.float() * v_size).to(v.dtype), [3], [keys], False)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("large", [slice(0, 2), slice(150, 152), slice(298, 300)], ids=["first", "middle", "last"])
+def test_rows_with_gradients_of_very_different_size(large, dim):
+    """A few rows' gradients are 10^6 times the others': a row's results, and those of keys that the large ones do not see, are as if they were alone."""
+    lens = [300]
+    q, k, v, dout = inputs(lens, lens, 4, 2, dim, "f16", seed=13)
+    size = torch.full((300, 1, 1), 1e-4, device="cuda")
+    size[large] = 1e2
+    go((dout.float() * size).half(), q, k, v, lens, lens, True)
+
+
+def test_rows_without_gradients():
+    """Rows of zeros first, last and between: the first dS that is not 0 sets the power of two."""
+    lens = [260]
+    q, k, v, dout = inputs(lens, lens, 4, 1, 64, "f16", seed=14)
+    for rows in (slice(0, 130), slice(70, 260), slice(0, 260)):
+        some = dout.clone()
+        some[rows] = 0
+        dq, dk, dv = go(some, q, k, v, lens, lens, False)
+        assert bool((dq[rows] == 0).all())
