@@ -111,7 +111,8 @@ int cdsgd_block_norm_backward(const cdsgd_block_norm *norm, const void *dy, size
  *   dim           elements of a head: a multiple of 8, at most 128
  *   q, out, dout, dq  [tokens_q][heads][dim];  k, v, dk, dv  [tokens_k][kv_heads][dim]: the heads of a token in a row, tokens ld elements
  *                 apart, 16-byte aligned, ld a multiple of 8 and at most 2^20 (CDSGD_ERR_ALIGN, CDSGD_ERR_SIZE)
- *   lse           fp32[heads][tokens_q], natural logarithms; the forward pass takes NULL for none
+ *   lse           fp32[heads][tokens_q], natural logarithms; the forward pass takes NULL for none.  The backward pass is given the forward pass's;
+ *                 where it is beyond 2800 or so, of which fp32 leaves too few bits, a row's sum is formed from its logits again
  *   starts_q, starts_k  int32[num_seqs + 1], not falling, from 0 or more to tokens_q (tokens_k) or less.  They are not looked at on the host:
  *                 what is out of range is cut to it, and starts that fall give rows of no meaning, but nothing outside the tensors is
  *                 touched.  starts_k NULL: starts_q.  Both NULL: one sequence, all rows (num_seqs 1).

@@ -171,13 +171,13 @@ int cdsgd_attention_backward(const cdsgd_attention *batch, const void *dout, siz
     hipStream_t stream = (hipStream_t)hip_stream;
     with_kernel(a, [&](auto dt, auto dim) {
         constexpr int DT = decltype(dt)::value, DP = decltype(dim)::value;
-        float *const row_lse = static_cast<float *>(workspace), *const delta = row_lse + rows;
+        float *const row_lse = static_cast<float *>(workspace), *const delta = row_lse + rows, *const far = delta + rows;
         hipLaunchKernelGGL((k_attention_dq<DT, DP>), dim3((unsigned)groups_over(a.tokens_q, a.num_seqs, z.group, kTileRows, z.kv_heads)), dim3(256), 0, stream, z,
                            read_of<DT>(dout, ld_dout), read_of<DT>(q, ld_q), read_of<DT>(k, ld_k), read_of<DT>(v, ld_v), read_of<DT>(out, ld_out), lse,
-                           write_of<DT>(dq, ld_dq), row_lse, delta);
+                           write_of<DT>(dq, ld_dq), row_lse, delta, far);
         hipLaunchKernelGGL((k_attention_dkv<DT, DP>), dim3((unsigned)groups_over(a.tokens_k, a.num_seqs, 1, kStreamKeys<DP>, z.kv_heads)), dim3(64 * kKeyWaves<DP> * kStreams<DP>), 0, stream, z,
                            read_of<DT>(dout, ld_dout), read_of<DT>(q, ld_q), read_of<DT>(k, ld_k), read_of<DT>(v, ld_v), (const float *)row_lse,
-                           (const float *)delta, write_of<DT>(dk, ld_dk), write_of<DT>(dv, ld_dv));
+                           (const float *)delta, (const float *)far, write_of<DT>(dk, ld_dk), write_of<DT>(dv, ld_dv));
     });
     return launch_status();
 }

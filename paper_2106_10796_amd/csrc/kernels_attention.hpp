@@ -36,6 +36,10 @@ constexpr float kLiftBack = DT == kGradF16 ? 15.0f : 0.0f;
 template <int DT>
 constexpr float kLifted = DT == kGradF16 ? 32768.0f : 1.0f;
 
+// The backward pass takes a row's logits less lse log2 e, in fp32.  Of 2^12 that leaves P a share of 2^-12 off, half a step of fp16; rows beyond it have their
+// largest logit and their sum formed again, and take the largest off first.
+constexpr float kFarBack = 4096.0f;
+
 constexpr unsigned kTileRows = 128;  // rows of a group of the forward pass and of dq, and keys of a group of dk and dv
 constexpr unsigned kMostSplits = 256;
 constexpr unsigned kTileKeys = 64;   // what a group takes at a time of the other side
@@ -51,6 +55,9 @@ __device__ __forceinline__ f16v mfma(s8v a, s8v b, f16v c)
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
     }
 }
+
+// The lane's number, worked out where it is used: behind a loop that has no register left to keep it in.
+__device__ __forceinline__ unsigned lane_now() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
 
 // The row of a result's element r.
 __device__ __forceinline__ constexpr unsigned row_of(unsigned r, unsigned half) { return 8u * (r / 4u) + 4u * half + r % 4u; }
@@ -288,7 +295,7 @@ template <int DT, int DP>
 __device__ __forceinline__ void store_row(Elem<DT> *row, const f16v (&acc)[DP / 32], float f, unsigned dim)
 {
     typedef Elem<DT> e4 __attribute__((ext_vector_type(4)));
-    const unsigned half = threadIdx.x % 64u / 32u;
+    const unsigned half = lane_now() / 32u;
 #pragma unroll
     for (unsigned d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -515,15 +522,18 @@ struct Lift {
 
 // dq, and with it the first kernel of the backward pass: tiles as in the forward pass, three products for its two.  4096 tokens, 32 heads of 128 over 8,
 // not causal: 370 us, 1.1 PFLOP/s, bound as the forward pass is; 8191 tokens in 8 sequences, causal: 163.
-// For the next kernel row_lse receives what S begins with in every row, (lift - lse log2 e) / c, and delta -dout . out, both
-// [kv head][token][head of the group].
+// For the next kernel row_lse receives what S begins with in every row, (lift - lse log2 e) / c, far 0, and delta -dout . out, all
+// [kv head][token][head of the group].  A row whose lse is far from 0 leaves its largest S, and in far 2^lift over the sum of exp(scale (S - largest));
+// where a tile has such rows its first one's far is not 0 (-1 if it is not far itself).
 template <int DT, int DP>
 __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
                                                       Heads<const Elem<DT>> v, Heads<const Elem<DT>> out, const float *__restrict__ lse,
-                                                      Heads<Elem<DT>> dq, float *__restrict__ row_lse, float *__restrict__ delta)
+                                                      Heads<Elem<DT>> dq, float *__restrict__ row_lse, float *__restrict__ delta,
+                                                      float *__restrict__ far)
 {
     constexpr unsigned kTile = kTileKeys * DP * 2;
     __shared__ __align__(1024) unsigned char smem[4 * kTile];  // two tiles of keys and of values
+    __shared__ unsigned far_waves[4];
     const Lds lds = (Lds)smem;
     const unsigned kv = blockIdx.x % z.kv_heads;
     const TileAt t = tile_of(z.starts_q, z.tokens_q, z.num_seqs, z.group, kTileRows,
@@ -556,15 +566,11 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
     }
     sum = sum_of_halves(sum);
     // (a row that sees nothing, and one that is not there, has no share in anything)
-    const float log_sum = row < rows ? lse[at] : kInfinity, base = log_sum == -kInfinity ? kInfinity : log_sum * kLog2e;
+    const float log_sum = row < rows ? lse[at] : kInfinity;
+    float base = log_sum == -kInfinity ? kInfinity : log_sum * kLog2e, top = 0.0f;
     landed(bq);
     landed(bd);
     const float c = z.scale * kLog2e;
-    if (row < rows && half == 0u) {
-        const size_t place = ((size_t)kv * z.tokens_q + s.q0 + query) * z.group + head - head0;
-        row_lse[place] = (kLiftBack<DT> - base) / c;
-        delta[place] = -sum;
-    }
 
     const auto seen = [&](unsigned r) __attribute__((always_inline)) -> unsigned {
         if (!z.causal) return s.keys;
@@ -574,12 +580,64 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
     const unsigned mine = row < rows ? seen(row) : 0u, to = seen(rows - 1u), least = (unsigned)__builtin_amdgcn_readfirstlane((int)seen(wave * 32u));
     f16v acc[DP / 32] = {};
     const TileLoads<DP, kTileKeys, 4> loads_k(wave, 1u, k.ld, z.dim), loads_v(wave, 1u, v.ld, z.dim);
-    const auto ask = [&](unsigned j, unsigned b) __attribute__((always_inline)) {
+    const auto ask_keys = [&](unsigned j, unsigned b) __attribute__((always_inline)) {
         const unsigned left = s.keys - j < kTileKeys ? s.keys - j : kTileKeys;
         loads_k.ask(lds + b * 2u * kTile, wave, k.p + (size_t)(s.k0 + j) * k.ld + kv * z.dim, ((left - 1u) * k.ld + z.dim) * 2u);
+    };
+    const auto ask = [&](unsigned j, unsigned b) __attribute__((always_inline)) {
+        const unsigned left = s.keys - j < kTileKeys ? s.keys - j : kTileKeys;
+        ask_keys(j, b);
         loads_v.ask(lds + b * 2u * kTile + kTile, wave, v.p + (size_t)(s.k0 + j) * v.ld + kv * z.dim, ((left - 1u) * v.ld + z.dim) * 2u);
     };
     Operands<DP> operand;
+    const auto hide = [&](f16v &x, unsigned first) __attribute__((always_inline)) {
+#pragma unroll
+        for (unsigned r = 0; r < 16; ++r)
+            if (first + row_of(r, half) >= mine) x[r] = -kInfinity;
+    };
+    const bool is_far = mine > 0u && __builtin_fabsf(base) > kFarBack;
+    const bool far_wave = __builtin_amdgcn_ballot_w64(is_far) != 0;
+    if (l == 0u) far_waves[wave] = far_wave;
+    __syncthreads();
+    const bool far_tile = far_waves[0] || far_waves[1] || far_waves[2] || far_waves[3];
+    if (far_tile) {
+        float most = -kInfinity, total = 0.0f;
+        unsigned buffer = 0;
+        if (to) ask_keys(0, 0);
+        for (unsigned j = 0; j < to; j += kTileKeys) {
+            wait_for_loads<0>();
+            __syncthreads();
+            if (j + kTileKeys < to) ask_keys(j + kTileKeys, buffer ^ 1u);
+            const unsigned at = buffer;
+            buffer ^= 1u;
+            if (!far_wave) continue;
+#pragma unroll 1
+            for (unsigned b = 0; b < 2; ++b) {
+                f16v x = {};
+#pragma unroll
+                for (unsigned i = 0; i < DP / 16; ++i) x = mfma<DT>(operand.rows(lds + at * 2u * kTile + b * (32u * DP * 2u), i), bq[i], x);
+                if (j + kTileKeys > least) hide(x, j + 32u * b);
+                const float before = most;
+#pragma unroll
+                for (unsigned r = 0; r < 16; ++r) most = __builtin_fmaxf(most, x[r]);
+                most = larger_half(most);
+                if (most != -kInfinity) {
+                    total *= __builtin_amdgcn_exp2f((before - most) * c);
+#pragma unroll
+                    for (unsigned r = 0; r < 16; ++r) total += __builtin_amdgcn_exp2f((x[r] - most) * c);
+                }
+            }
+        }
+        __syncthreads();  // (the tiles' places are written again)
+        total = sum_of_halves(total);
+        if (is_far && most != -kInfinity) top = most, base = __builtin_log2f(total);
+    }
+    if (row < rows && half == 0u) {
+        const size_t place = ((size_t)kv * z.tokens_q + s.q0 + query) * z.group + head - head0;
+        row_lse[place] = top != 0.0f ? top : (kLiftBack<DT> - base) / c;
+        delta[place] = -sum;
+        far[place] = top != 0.0f ? __builtin_amdgcn_exp2f(kLiftBack<DT> - base) : row == 0u && far_tile ? -1.0f : 0.0f;
+    }
     Lift lift;
     unsigned buffer = 0;
     if (to) ask(0, 0);
@@ -617,6 +675,10 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
                 for (unsigned r = 0; r < 16; ++r)
                     if (j + 32u * b + row_of(r, half) >= mine) x[r] = -kInfinity, y[r] = 0.0f;
             }
+            if (far_wave) {
+#pragma unroll
+                for (unsigned r = 0; r < 16; ++r) x[r] -= top;
+            }
 #pragma unroll
             for (unsigned r = 0; r < 16; ++r) {
                 y[r] -= sum;
@@ -639,7 +701,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
 // of its rows, and the launch is as long as the longest group.  us (8191 tokens in 8 sequences, 32 heads of 128 over 8 | 4096 tokens, not
 // causal, the same heads; fp16, 7999 tokens in 16 sequences, 12 heads of 64, not causal | 4096 tokens, 32 heads of 64 over 8):
 //   128 elements a head: 4 waves in 2 streams 264 | 526, 2 in 4 255 | 575, 4 in one stream 345;  64: 2 in 2 70 | 318, 4 in 1 71 | 410, 4 in 2 82 | 314, 2 in 4 97 | 324
-// Of 128 elements a head, a wave's registers hold its keys and both results, but not its values too, which are read from LDS.
+// Of 128 elements a head, a wave's registers hold its keys and both results, but not its values too, which are read from LDS; of 64 there are three waves to
+// a SIMD (the fp16 batch 62 with two, 54 with three).
 constexpr unsigned kStreamRows = 32;
 template <int DP>
 constexpr unsigned kKeyWaves = DP == 128 ? 4 : 2;
@@ -649,13 +712,13 @@ template <int DP>
 constexpr unsigned kStreamKeys = 32 * kKeyWaves<DP>;
 
 template <int DT, int DP>
-__global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attention_dkv(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
+__global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, DP == 64 ? 3 : 2) void k_attention_dkv(AttentionSizes z, Heads<const Elem<DT>> dout, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k,
                                                        Heads<const Elem<DT>> v, const float *__restrict__ all_lse, const float *__restrict__ delta,
-                                                       Heads<Elem<DT>> dk, Heads<Elem<DT>> dv)
+                                                       const float *__restrict__ far, Heads<Elem<DT>> dk, Heads<Elem<DT>> dv)
 {
     constexpr bool kValuesInLds = DP == 128;
     constexpr unsigned KW = kKeyWaves<DP>, S = kStreams<DP>, kKeys = kStreamKeys<DP>;
-    // of a stream, twice: a tile of q, one of dout, and two numbers of each row
+    // of a stream, twice: a tile of q, one of dout, and three numbers of each row
     constexpr unsigned kRows = kStreamRows, kTile = kRows * DP * 2, kStage = 2 * kTile + 1024, kValues = S * 2 * kStage;
     constexpr unsigned kSums = 32 * DP * 4;  // of a wave's results of one kind
     static_assert((S - 1) * KW * kSums <= kValues, "the streams' sums fit where their tiles were");
@@ -689,17 +752,22 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
     const TileLoads<DP, kRows, KW> loads_q(side, group, q.ld, z.dim), loads_d(side, group, dout.ld, z.dim);
     // (values, not one of three variables: the compiler would keep those in memory)
     const float *const numbers = side == 0u ? +all_lse : +delta;
+    bool any_far = false;
+    for (unsigned long long i = l * (unsigned long long)kTileRows; i < (unsigned long long)s.queries * group; i += 64u * kTileRows)
+        any_far = any_far || far[((size_t)kv * z.tokens_q + s.q0) * group + i] != 0.0f;
+    any_far = __builtin_amdgcn_ballot_w64(any_far) != 0;
     // tile `n` of all; past the last nothing is in range
     const auto ask = [&](unsigned n, unsigned b) __attribute__((always_inline)) {
         const unsigned i = from + n / parts * at_once, part = n % parts * kRows, there = n < tiles ? s.queries - i : 0u;
         const unsigned queries = there < at_once ? there : at_once, heads = group - part < kRows ? group - part : kRows;
         const Lds to = lds + (stream * 2u + b) * kStage;
         const size_t token = s.q0 + (n < tiles ? i : 0u);
-        const unsigned far = queries ? queries - 1u : 0u;
-        loads_q.ask(to, side, q.p + token * q.ld + (head0 + part) * z.dim, queries ? (far * q.ld + heads * z.dim) * 2u : 0u);
-        loads_d.ask(to + kTile, side, dout.p + token * dout.ld + (head0 + part) * z.dim, queries ? (far * dout.ld + heads * z.dim) * 2u : 0u);
+        const unsigned last = queries ? queries - 1u : 0u;
+        loads_q.ask(to, side, q.p + token * q.ld + (head0 + part) * z.dim, queries ? (last * q.ld + heads * z.dim) * 2u : 0u);
+        loads_d.ask(to + kTile, side, dout.p + token * dout.ld + (head0 + part) * z.dim, queries ? (last * dout.ld + heads * z.dim) * 2u : 0u);
         const size_t at = ((size_t)kv * z.tokens_q + token) * group + part;
         if (KW == 2 || side < 2u) load_to_lds<4>(same_in_all(buffer_of(numbers + at, queries * heads * 4u)), to + 2u * kTile + side * 256u, l * 4u);
+        if (any_far && side == 0u) load_to_lds<4>(same_in_all(buffer_of(far + at, queries * heads * 4u)), to + 2u * kTile + 512u, l * 4u);
     };
     Operands<DP> operand;
     unsigned buffer = 0;
@@ -714,73 +782,89 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
     }
     landed(bk);
     if constexpr (!kValuesInLds) landed(bv);
-    for (unsigned first = 0; first < tiles; first += S) {
-        wait_for_loads<0>();
-        __syncthreads();
-        const unsigned n = first + stream, now = from + n / parts * at_once;
-        if (first + S < tiles) ask(n + S, buffer ^ 1u);
-        const unsigned at = buffer;
-        const CDSGD_LDS float *row_lse = (const CDSGD_LDS float *)(lds + (stream * 2u + at) * kStage + 2u * kTile), *row_delta = row_lse + 64;
-        buffer ^= 1u;
-        if (side * 32u >= keys || n >= tiles) continue;
-        operand.renew();
-        // S less lse, and dP less delta: both begin with what is taken from them.  The operands of a pair of products are read beside the pair before.
-        f16v x, y;
+    const auto run = [&](auto with_far) __attribute__((always_inline)) {
+        constexpr bool FAR = decltype(with_far)::value;
+        for (unsigned first = 0; first < tiles; first += S) {
+            wait_for_loads<0>();
+            __syncthreads();
+            const unsigned n = first + stream, now = from + n / parts * at_once;
+            if (first + S < tiles) ask(n + S, buffer ^ 1u);
+            const unsigned at = buffer;
+            const CDSGD_LDS float *row_lse = (const CDSGD_LDS float *)(lds + (stream * 2u + at) * kStage + 2u * kTile), *row_delta = row_lse + 64, *row_far = row_lse + 128;
+            buffer ^= 1u;
+            if (side * 32u >= keys || n >= tiles) continue;
+            operand.renew();
+            // S less lse, and dP less delta: both begin with what is taken from them (S, where there are far rows, with 0, as it did when their
+            // largest one was looked for).  The operands of a pair of products are read beside the pair before.
+            f16v x, y;
 #pragma unroll
-        for (unsigned r = 0; r < 16; r += 4) {
-            const f4 base = *(const CDSGD_LDS f4 *)(row_lse + row_of(r, half)), sum = *(const CDSGD_LDS f4 *)(row_delta + row_of(r, half));
+            for (unsigned r = 0; r < 16; r += 4) {
+                const f4 base = *(const CDSGD_LDS f4 *)(row_lse + row_of(r, half)), sum = *(const CDSGD_LDS f4 *)(row_delta + row_of(r, half));
 #pragma unroll
-            for (unsigned e = 0; e < 4; ++e) x[r + e] = base[e], y[r + e] = sum[e];
-        }
-        const Lds at_q = lds + (stream * 2u + at) * kStage, at_d = at_q + kTile;
-        s8v ring_q[2], ring_d[2], ring_v[2];
-        const auto fetch_rows = [&](unsigned e) __attribute__((always_inline)) {
-            ring_q[e % 2u] = operand.rows(at_q, e);
-            ring_d[e % 2u] = operand.rows(at_d, e);
-            if constexpr (kValuesInLds) ring_v[e % 2u] = operand.rows(values + side * (32u * DP * 2u), e);
-        };
-        fetch_rows(0);
+                for (unsigned e = 0; e < 4; ++e) x[r + e] = FAR ? 0.0f : base[e], y[r + e] = sum[e];
+            }
+            const Lds at_q = lds + (stream * 2u + at) * kStage, at_d = at_q + kTile;
+            s8v ring_q[2], ring_d[2], ring_v[2];
+            const auto fetch_rows = [&](unsigned e) __attribute__((always_inline)) {
+                ring_q[e % 2u] = operand.rows(at_q, e);
+                ring_d[e % 2u] = operand.rows(at_d, e);
+                if constexpr (kValuesInLds) ring_v[e % 2u] = operand.rows(values + side * (32u * DP * 2u), e);
+            };
+            fetch_rows(0);
 #pragma unroll
-        for (unsigned e = 0; e < DP / 16; ++e) {
-            if (e + 1u < DP / 16) fetch_rows(e + 1u);
+            for (unsigned e = 0; e < DP / 16; ++e) {
+                if (e + 1u < DP / 16) fetch_rows(e + 1u);
+                __builtin_amdgcn_sched_barrier(0);
+                x = mfma<DT>(ring_q[e % 2u], bk[e], x);
+                y = mfma<DT>(ring_d[e % 2u], kValuesInLds ? ring_v[e % 2u] : bv[kValuesInLds ? 0 : e], y);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (FAR) {
+#pragma unroll
+                for (unsigned r = 0; r < 16; ++r) {
+                    const float over = row_far[row_of(r, half)], first = row_lse[row_of(r, half)], less = x[r] - first;
+                    x[r] = over <= 0.0f ? x[r] + first : (less > 0.0f ? 0.0f : less) + __builtin_amdgcn_logf(over) / c;
+                    if (r % 2u == 1u) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            constexpr unsigned kProducts = DP / 8, kAhead = 3;
+            s8v ring[kAhead + 1];
+            const auto fetch_columns = [&](unsigned i) __attribute__((always_inline)) {
+                ring[i % (kAhead + 1)] = operand.columns((i % 2u ? at_q : at_d) + i / (kProducts / 2u) * (16u * DP * 2u), i / 2u % (DP / 32));
+            };
+#pragma unroll
+            for (unsigned i = 0; i < kAhead; ++i) fetch_columns(i);
+            // (every row of the tile sees every key of the wave, but for causal tiles on the border)
+            if (z.causal && first_of(key0 + side * 32u + 31u) > now) {
+                const unsigned first_row = first_of(key0 + key), hidden = first_row <= now ? 0u : group < kRows ? (first_row - now) * group : kRows;
+#pragma unroll
+                for (unsigned r = 0; r < 16; ++r)
+                    if (row_of(r, half) < hidden) x[r] = -kInfinity, y[r] = 0.0f;
+            }
+            const float down = lift.by * (1.0f / kLifted<DT>);
+#pragma unroll
+            for (unsigned r = 0; r < 16; ++r) {
+                x[r] = __builtin_amdgcn_exp2f(x[r] * c);
+                y[r] = x[r] * (DT == kGradF16 ? y[r] * down : y[r]);
+            }
+            if constexpr (DT == kGradF16) lift.fit(y, acc_k);
+            const s8v p[2] = {rounded<DT>(x, 0), rounded<DT>(x, 1)}, ds[2] = {rounded<DT>(y, 0), rounded<DT>(y, 1)};
             __builtin_amdgcn_sched_barrier(0);
-            x = mfma<DT>(ring_q[e % 2u], bk[e], x);
-            y = mfma<DT>(ring_d[e % 2u], kValuesInLds ? ring_v[e % 2u] : bv[kValuesInLds ? 0 : e], y);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        constexpr unsigned kProducts = DP / 8, kAhead = 3;
-        s8v ring[kAhead + 1];
-        const auto fetch_columns = [&](unsigned i) __attribute__((always_inline)) {
-            ring[i % (kAhead + 1)] = operand.columns((i % 2u ? at_q : at_d) + i / (kProducts / 2u) * (16u * DP * 2u), i / 2u % (DP / 32));
-        };
 #pragma unroll
-        for (unsigned i = 0; i < kAhead; ++i) fetch_columns(i);
-        // (every row of the tile sees every key of the wave, but for causal tiles on the border)
-        if (z.causal && first_of(key0 + side * 32u + 31u) > now) {
-            const unsigned first_row = first_of(key0 + key), hidden = first_row <= now ? 0u : group < kRows ? (first_row - now) * group : kRows;
-#pragma unroll
-            for (unsigned r = 0; r < 16; ++r)
-                if (row_of(r, half) < hidden) x[r] = -kInfinity, y[r] = 0.0f;
+            for (unsigned i = 0; i < kProducts; ++i) {
+                if (i + kAhead < kProducts) fetch_columns(i + kAhead);
+                const unsigned h = i / (kProducts / 2u), d = i / 2u % (DP / 32);
+                if (i % 2u) acc_k[d] = mfma<DT>(ring[i % (kAhead + 1)], ds[h], acc_k[d]);
+                else acc_v[d] = mfma<DT>(ring[i % (kAhead + 1)], p[h], acc_v[d]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        const float down = lift.by * (1.0f / kLifted<DT>);
-#pragma unroll
-        for (unsigned r = 0; r < 16; ++r) {
-            x[r] = __builtin_amdgcn_exp2f(x[r] * c);
-            y[r] = x[r] * (DT == kGradF16 ? y[r] * down : y[r]);
-        }
-        if constexpr (DT == kGradF16) lift.fit(y, acc_k);
-        const s8v p[2] = {rounded<DT>(x, 0), rounded<DT>(x, 1)}, ds[2] = {rounded<DT>(y, 0), rounded<DT>(y, 1)};
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (unsigned i = 0; i < kProducts; ++i) {
-            if (i + kAhead < kProducts) fetch_columns(i + kAhead);
-            const unsigned h = i / (kProducts / 2u), d = i / 2u % (DP / 32);
-            if (i % 2u) acc_k[d] = mfma<DT>(ring[i % (kAhead + 1)], ds[h], acc_k[d]);
-            else acc_v[d] = mfma<DT>(ring[i % (kAhead + 1)], p[h], acc_v[d]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    }
+    };
+    // (a branch for far rows within the loop costs 3 % of it, taken or not)
+    if (any_far) run(std::true_type());
+    else run(std::false_type());
     // the streams' sums, added in their order
+    const unsigned lane = lane_now(), own_key = side * 32u + lane % 32u;
     wait_for_loads<0>();
     __syncthreads();
     const float f = z.scale / lift.by;
@@ -796,7 +880,7 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
                 for (unsigned e = 0; e < 4; ++e) {
                     f4 w = {acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
                     if (!which) w *= f;
-                    sums[(((stream - 1u) * KW + side) * (DP / 8u) + d * 4u + e) * 64u + l] = w;
+                    sums[(((stream - 1u) * KW + side) * (DP / 8u) + d * 4u + e) * 64u + lane] = w;
                 }
         }
         if constexpr (S > 1) __syncthreads();
@@ -808,13 +892,13 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, 2) void k_attent
                     f4 w = {acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
                     if (!which) w *= f;
 #pragma unroll
-                    for (unsigned i = 0; i < S - 1; ++i) w += sums[((i * KW + side) * (DP / 8u) + d * 4u + e) * 64u + l];
+                    for (unsigned i = 0; i < S - 1; ++i) w += sums[((i * KW + side) * (DP / 8u) + d * 4u + e) * 64u + lane];
 #pragma unroll
                     for (unsigned i = 0; i < 4; ++i) acc[d][4 * e + i] = w[i];
                 }
-            if (key < keys) {
+            if (own_key < keys) {
                 const Heads<Elem<DT>> &to = which ? dv : dk;
-                store_row<DT, DP>(to.p + (size_t)(s.k0 + key0 + key) * to.ld + kv * z.dim, acc, which ? 1.0f / kLifted<DT> : 1.0f, z.dim);
+                store_row<DT, DP>(to.p + (size_t)(s.k0 + key0 + own_key) * to.ld + kv * z.dim, acc, which ? 1.0f / kLifted<DT> : 1.0f, z.dim);
             }
         }
     }

@@ -6,9 +6,17 @@ import pytest
 import torch
 
 from paper_2106_10796_amd import binding as B
-from test_gpu_attention import SMALL, U, close, half_step, inputs, logit_error, probabilities, reference, starts_of, tiny, tiny_p
+from test_gpu_attention import SMALL, U, close as close_finite, half_step, inputs, logit_error, probabilities, reference, starts_of, tiny, tiny_p
 
 pytestmark = pytest.mark.gpu
+
+
+def close(got, want, error, what):
+    """fp16 rounds 65520 and more to infinity: an infinity is near where the tolerance reaches a number of its sign that large."""
+    if got.dtype == torch.float16:
+        past = torch.isinf(got) & (torch.where(got > 0, want, -want) + error >= 65520)
+        got = torch.where(past, want, got.double()) if bool(past.any()) else got
+    close_finite(got, want, error, what)
 
 
 def run(dout, q, k, v, lens_q, lens_k, causal, scale):
@@ -101,3 +109,53 @@ def test_rows_without_gradients():
         some[rows] = 0
         dq, dk, dv = go(some, q, k, v, lens, lens, False)
         assert bool((dq[rows] == 0).all())
+
+
+def far_case(dtype, dim, scale, sign, lens_q, lens_k, seed, near_rows=()):
+    """Logits of scale * 2^10 and a few times scale * 2^-10 beside: products q . k are multiples of 2^-10 below 2^14, so that fp32 holds every partial sum."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    T, K, heads, kv = sum(lens_q), sum(lens_k), 4, 2
+    t = {"bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+    ints = lambda n, h: torch.randint(-3, 4, (n, h, dim), device="cuda", generator=gen).float() / 32  # noqa: E731
+    q, k = ints(T, heads), ints(K, kv)
+    q[:, :, 4:], k[:, :, 4:] = 0, 0
+    q[:, :, 0], k[:, :, 0] = 32 * sign, 32
+    for rows in near_rows:
+        q[rows, :, 0] = 0
+    _, _, v, dout = inputs(lens_q, lens_k, heads, kv, dim, dtype, seed=seed)
+    return q.to(t), k.to(t), v, dout
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 40])
+@pytest.mark.parametrize("scale", [2.0 ** 2, 2.0 ** 3, 2.0 ** 10, 2.0 ** 20, 2.0 ** 30])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("causal", [True, False])
+def test_gradients_of_far_logits(causal, sign, scale, dim, dtype):
+    """Logits from 2^12 to 2^40, where fp32 has no bits of lse left for what the probabilities are made of, beside rows of ordinary ones."""
+    lens = [150, 1, 77]
+    q, k, v, dout = far_case(dtype, dim, scale, sign, lens, lens, 21, near_rows=(slice(40, 47), slice(90, 128), slice(160, 190)))
+    out, lse, grads = run(dout, q, k, v, lens, lens, causal, scale)
+    check_gradients(dout, q, k, v, out, lse, grads, lens, lens, causal, scale, exact_logits=True)
+
+
+@pytest.mark.parametrize("lens_q,lens_k", [([200, 3], [60, 500]), ([1, 1], [3000, 70])], ids=str)
+def test_far_logits_of_rows_that_see_few_keys(lens_q, lens_k):
+    """Rows that see nothing among them."""
+    q, k, v, dout = far_case("bf16", 64, 2.0 ** 12, 1, lens_q, lens_k, 22)
+    out, lse, grads = run(dout, q, k, v, lens_q, lens_k, True, 2.0 ** 12)
+    check_gradients(dout, q, k, v, out, lse, grads, lens_q, lens_k, True, 2.0 ** 12, exact_logits=True)
+
+
+def test_far_logits_of_ordinary_numbers_keep_their_sums():
+    """Logits of about 10^6 and 10^9 that fp32 does not hold: probabilities are those of the forward pass, whose sum over keys is 1, so that a dout of one
+    number throughout gives dv its sum over queries, and v of one number throughout no dq (but for what `out` was rounded by)."""
+    lens = [300]
+    for size in (1e3, 3e4):
+        q, k, v, _ = inputs(lens, lens, 4, 2, 128, "bf16", seed=23)
+        q, k, v, dout = (q.float() * size).bfloat16(), (k.float() * size).bfloat16(), torch.ones_like(v), torch.ones_like(q)
+        out, _, (dq, dk, dv) = run(dout, q, k, v, lens, lens, True, 1.0)
+        assert bool((out == 1).all())
+        total = dv.double().sum(0)[:, 0]                          # of 300 queries of two heads, each a sum of probabilities: half a step each way
+        assert bool(((total - 600).abs() <= 600 * 3 * 2.0 ** -8).all()), total
+        assert all(bool(torch.isfinite(t).all()) for t in (dq, dk, dv))
