@@ -620,6 +620,7 @@ cdsgd_attention batch_of(const Heads &q, const Heads &k, PyObject *starts, PyObj
     size_t count = 0;
     b.starts_q = static_cast<const int32_t *>(buffer_here(starts, at::kInt, kAny, &count));
     if (count < 2 || THPVariable_Unpack(starts).dim() != 1) throw NotPlain();
+    if (starts_k != Py_None && THPVariable_CheckExact(starts_k) && THPVariable_Unpack(starts_k).dim() != 1) throw NotPlain();
     b.num_seqs = count - 1;
     b.starts_k = static_cast<const int32_t *>(buffer_here(starts_k, at::kInt, count));
     return b;
