@@ -105,10 +105,12 @@ int cdsgd_block_norm_backward(const cdsgd_block_norm *norm, const void *dy, size
  * A query that sees no key has out = 0 and lse = -infinity, and passes no gradient on.  The backward pass gives
  *   P = exp(S - lse);  dP = dout . v;  dS = P (dP - dout . out)
  *   dq = scale sum over j of dS k;  dk = scale sum over i, heads of dS q;  dv = sum over i, heads of P dout
- * Rows that belong to no sequence are neither read nor written.  A NaN or an infinity of a token reaches no other sequence and no other group of
- * heads; in its own sequence it may reach tokens from which `causal` hides it, up to 192 before it (in the backward pass also behind it).  Products are summed in fp32; P and dS are rounded to the tensors' type as
- * operands of the second products (dS of fp16 tensors times a power of two of its row for dq, of its key for dk, which is divided out again: nothing
- * overflows on the way, and what is lost of a number is below 2^-32 of the largest |dS| that it is summed up with).
+ * Rows that belong to no sequence are neither read nor written.  A NaN or an infinity of a token reaches no other sequence, no other group of heads,
+ * and, with `causal`, of its own sequence only what the formulas lead it to: a key's the queries that see it, a query's its own row and the keys
+ * that it sees (and from a row that one key has made NaN all keys that the row sees).  What it does not reach is the same to the bit without it.
+ * Products are summed in fp32; P and dS are rounded to the tensors' type as operands of the second products (dS of fp16 tensors times a power of two
+ * of its row for dq, of its key for dk, which is divided out again: nothing overflows on the way, and what is lost of a number is below 2^-32 of the
+ * largest |dS| that it is summed up with).
  *   dtype         CDSGD_GRAD_BF16 or CDSGD_GRAD_F16
  *   dim           elements of a head: a multiple of 8, at most 128
  *   q, out, dout, dq  [tokens_q][heads][dim];  k, v, dk, dv  [tokens_k][kv_heads][dim]: the heads of a token in a row, tokens ld elements

@@ -56,8 +56,13 @@ __device__ __forceinline__ f16v mfma(s8v a, s8v b, f16v c)
     }
 }
 
-// The lane's number, worked out where it is used: behind a loop that has no register left to keep it in.
-__device__ __forceinline__ unsigned lane_now() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
+// The lane's number, worked out where it is used, and what follows from it too: in and behind loops that have no registers left to keep that in.
+__device__ __forceinline__ unsigned lane_now()
+{
+    unsigned lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
 
 // The row of a result's element r.
 __device__ __forceinline__ constexpr unsigned row_of(unsigned r, unsigned half) { return 8u * (r / 4u) + 4u * half + r % 4u; }
@@ -172,27 +177,7 @@ __device__ __forceinline__ unsigned lds_chunk(unsigned row, unsigned chunk) { re
 
 typedef CDSGD_LDS unsigned char *Lds;
 
-// Row l % 32 (from `row0` on), elements 16 k + 8 (l / 32) ... + 7: a first operand.
-template <int DP>
-__device__ __forceinline__ s8v rows_operand(Lds tile, unsigned row0, unsigned k)
-{
-    const unsigned l = threadIdx.x % 64u;
-    return *(const CDSGD_LDS s8v *)(tile + row0 * (DP * 2u) + lds_chunk<DP>(l % 32u, 2u * k + l / 32u));
-}
-
-// Column 32 d + l % 32 of rows row0 + 4 (l / 32) ... + 3 and row0 + 8 + 4 (l / 32) ... + 3: a first operand, transposed.
-template <int DP>
-__device__ __forceinline__ s8v columns_operand(Lds tile, unsigned row0, unsigned d)
-{
-    const unsigned l = threadIdx.x % 64u, row = 4u * (l / 32u) + l % 16u / 4u, at = 32u * d + 16u * (l / 16u % 2u) + 4u * (l % 4u);
-    const unsigned in = at % 8u * 2u;
-    typedef CDSGD_LDS s4v *Four;
-    const s4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(tile + row0 * (DP * 2u) + lds_chunk<DP>(row, at / 8u) + in));
-    const s4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(tile + row0 * (DP * 2u) + lds_chunk<DP>(row + 8u, at / 8u) + in));
-    return s8v{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-}
-
-// Where a lane finds its operands in a tile: the places of its first ones, from which those of the others differ by a few bits.
+// Where a lane finds its (first) operands in a tile: the places of its first ones, from which those of the others differ by a few bits.
 template <int DP>
 struct Operands {
     unsigned row, column;
@@ -203,7 +188,7 @@ struct Operands {
         row = lds_chunk<DP>(l % 32u, l / 32u);
         column = lds_chunk<DP>(4u * (l / 32u) + l % 16u / 4u, at / 8u) + at % 8u * 2u;
     }
-    // At the head of a loop: what the others are is worked out where they are read, one instruction each, and not kept in registers across it.
+    // At the head of a loop with no registers left: what the others are is worked out where they are read, one instruction each, and not kept in registers across it.
     __device__ __forceinline__ void renew() { asm volatile("" : "+v"(row), "+v"(column)); }
     // elements 16 k + 8 (l / 32) ... + 7 of row l % 32 of those that begin at `from`
     __device__ __forceinline__ s8v rows(Lds from, unsigned k) const { return *(const CDSGD_LDS s8v *)(from + (row ^ k * 32u)); }
@@ -290,6 +275,72 @@ __device__ __forceinline__ float larger_half(float x)
     return __builtin_fmaxf(h.low, h.high);
 }
 
+// acc += first * second where the second operand has zeros in what a lane does not see of the 16 that are summed over: it sees number n if
+// from <= n < to.  A matrix instruction makes 0 times an infinity or NaN a NaN, so that these are taken out of the first operand, and what of them a lane
+// sees is added for itself.  Without any the result is that of the one product, to the bit.
+template <int DT>
+__device__ __forceinline__ void add_seen(f16v &acc, s8v first, s8v second, int from, int to)
+{
+    __builtin_amdgcn_sched_barrier(0);
+    typedef unsigned u4v __attribute__((ext_vector_type(4)));
+    constexpr unsigned kTop = DT == kGradBF16 ? 0x7F80u : 0x7C00u;
+    u4v w = __builtin_bit_cast(u4v, first), fine;
+    unsigned any = 0;
+#pragma unroll
+    for (unsigned i = 0; i < 4; ++i) {
+        const unsigned mask = ((w[i] & kTop) == kTop ? 0xFFFFu : 0u) | ((w[i] >> 16 & kTop) == kTop ? 0xFFFF0000u : 0u);
+        any |= mask;
+        fine[i] = w[i] & ~mask;
+        w[i] &= mask;
+    }
+    acc = mfma<DT>(__builtin_bit_cast(s8v, fine), second, acc);
+    if (__builtin_amdgcn_ballot_w64(any != 0u) == 0) return;
+    const u4v p = __builtin_bit_cast(u4v, second);
+    const unsigned half = lane_now() / 32u;
+    const auto widen = [](unsigned bits) __attribute__((always_inline)) { return (float)__builtin_bit_cast(Elem<DT>, (unsigned short)bits); };
+#pragma unroll 1
+    for (int n = 0; n < 16; ++n) {
+        const unsigned at = (unsigned)n / 4u % 2u, e = (unsigned)n / 8u * 4u + (unsigned)n % 4u;  // lanes of half `at` hold it, in slot e
+        const auto slot = [&](const u4v &x) __attribute__((always_inline)) { return (e < 2u ? x[0] : e < 4u ? x[1] : e < 6u ? x[2] : x[3]) >> e % 2u * 16u & 0xFFFFu; };
+        const unsigned mine = half == at ? slot(w) : 0u;
+        if (__builtin_amdgcn_ballot_w64(mine != 0u) == 0) continue;
+        const Halves both = halves(widen(slot(p)));
+        const float factor = at ? both.high : both.low;
+        const bool sees = n >= from && n < to;
+#pragma unroll
+        for (unsigned r = 0; r < 16; ++r) {
+            const unsigned bits = (unsigned)__builtin_amdgcn_ds_bpermute((int)(32u * at + row_of(r, half)) * 4, (int)mine);
+            if (sees && bits != 0u) acc[r] = __builtin_fmaf(widen(bits), factor, acc[r]);
+            if (r % 4u == 3u) __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
+// Is any of a wave's results an infinity or NaN?
+template <int N>
+__device__ __forceinline__ bool any_not_finite(const f16v (&acc)[N])
+{
+    float zero = 0.0f;
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (unsigned r = 0; r < 16; ++r) zero = __builtin_fmaf(acc[d][r], 0.0f, zero);
+    return __builtin_amdgcn_ballot_w64(zero != 0.0f) != 0;
+}
+
+// Does any of a group's waves say so?  room: a word for each of them.
+template <int WAVES>
+__device__ __forceinline__ bool any_of_group(bool mine, unsigned *room)
+{
+    __syncthreads();
+    if (threadIdx.x % 64u == 0u) room[threadIdx.x / 64u] = mine;
+    __syncthreads();
+    unsigned any = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) any |= room[i];
+    return __builtin_amdgcn_readfirstlane((int)any) != 0;
+}
+
 // A row's results, which lie in two lanes four elements at a time, times f and rounded.
 template <int DT, int DP>
 __device__ __forceinline__ void store_row(Elem<DT> *row, const f16v (&acc)[DP / 32], float f, unsigned dim)
@@ -319,12 +370,13 @@ __device__ __forceinline__ void store_row(Elem<DT> *row, const f16v (&acc)[DP / 
 // parts, part_lse: where several groups share a row's keys (`splits`), each leaves its own result, [splits][row of all][DP] in fp32 and
 // [splits][row of all]; rows of all are numbered [kv head][query][head of the group].
 template <int DT, int DP>
-__global__ __launch_bounds__(256, 2) void k_attention_forward(AttentionSizes z, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k, Heads<const Elem<DT>> v,
+__global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void k_attention_forward(AttentionSizes z, Heads<const Elem<DT>> q, Heads<const Elem<DT>> k, Heads<const Elem<DT>> v,
                                                            Heads<Elem<DT>> out, float *__restrict__ lse, unsigned splits, float *__restrict__ parts,
                                                            float *__restrict__ part_lse)
 {
     constexpr unsigned kTile = kTileKeys * DP * 2;
     __shared__ __align__(1024) unsigned char smem[4 * kTile];  // two tiles of keys and of values
+    __shared__ unsigned said[4];
     const Lds lds = (Lds)smem;
     const unsigned kv = blockIdx.x % z.kv_heads, split = blockIdx.x / z.kv_heads % splits;
     // (the last tiles of a sequence see the most keys: they go first)
@@ -372,59 +424,80 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(AttentionSizes z, 
 #pragma unroll
     for (unsigned i = 0; i < DP / 16; ++i) bq[i] = load16(from_q, row_offset(skip + row, skip + rows, z.group, q.ld, 16u * i + 8u * half, z.dim));
     landed(bq);
-    for (unsigned j = from; j < to; j += kTileKeys) {
-        wait_for_loads<0>();
-        __syncthreads();
-        if (j + kTileKeys < to) ask(j + kTileKeys, buffer ^ 1u);
-        const Lds tile_k = lds + buffer * 2u * kTile, tile_v = tile_k + kTile;
-        buffer ^= 1u;
-        if (wave * 32u >= rows) continue;
-        f16v x[2] = {};
+    const auto run = [&](auto careful) __attribute__((always_inline)) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        for (unsigned j = from; j < to; j += kTileKeys) {
+            wait_for_loads<0>();
+            __syncthreads();
+            if (j + kTileKeys < to) ask(j + kTileKeys, buffer ^ 1u);
+            const Lds tile_k = lds + buffer * 2u * kTile, tile_v = tile_k + kTile;
+            buffer ^= 1u;
+            if (wave * 32u >= rows) continue;
+            Operands<DP> operand;
+            if constexpr (CAREFUL) operand.renew();
+            f16v x[2] = {};
 #pragma unroll
-        for (unsigned i = 0; i < DP / 16; ++i)
+            for (unsigned i = 0; i < DP / 16; ++i)
 #pragma unroll
-            for (unsigned b = 0; b < 2; ++b) x[b] = mfma<DT>(rows_operand<DP>(tile_k, 32u * b, i), bq[i], x[b]);
-        reads_ahead<6, DP / 8, 1>();
-        if (j + kTileKeys > least) {
+                for (unsigned b = 0; b < 2; ++b) x[b] = mfma<DT>(operand.rows(tile_k + b * (32u * DP * 2u), i), bq[i], x[b]);
+            reads_ahead<6, DP / 8, 1>();
+            if (j + kTileKeys > least) {
+#pragma unroll
+                for (unsigned b = 0; b < 2; ++b)
+#pragma unroll
+                    for (unsigned r = 0; r < 16; ++r)
+                        if (j + 32u * b + row_of(r, half) >= mine) x[b][r] = -kInfinity;
+            }
+            float most = x[0][0];
+#pragma unroll
+            for (unsigned r = 1; r < 32; ++r) most = __builtin_fmaxf(most, x[r / 16][r % 16]);
+            most = larger_half(most);
+            // (what happens to a row is its own: others in the wave do not change its bits)
+            const bool rises = !(most <= top + slack);
+            if (__builtin_amdgcn_ballot_w64(rises) != 0) {
+                const float now = rises ? __builtin_fmaxf(most, top) : top, next = !rises ? shift : now == -kInfinity ? 0.0f : kLift<DT> - now * c;
+                // (of logits far from 0 the product with c loses more than what is left: differences first)
+                const float keep = !rises ? 1.0f : top == -kInfinity ? 0.0f : __builtin_fabsf(next) > kFar ? __builtin_amdgcn_exp2f((top - now) * c) : __builtin_amdgcn_exp2f(next - shift);
+                top = now, shift = next;
+                total *= keep;
+#pragma unroll
+                for (unsigned d = 0; d < DP / 32; ++d) acc[d] *= keep;
+            }
+            float add = shift;
+            const bool is_far = __builtin_fabsf(shift) > kFar;
+            if (__builtin_amdgcn_ballot_w64(is_far) != 0) {
+                const float base = is_far ? top : 0.0f;
+                add = is_far ? kLift<DT> : shift;
+#pragma unroll
+                for (unsigned r = 0; r < 32; ++r) x[r / 16][r % 16] -= base;
+            }
 #pragma unroll
             for (unsigned b = 0; b < 2; ++b)
 #pragma unroll
-                for (unsigned r = 0; r < 16; ++r)
-                    if (j + 32u * b + row_of(r, half) >= mine) x[b][r] = -kInfinity;
-        }
-        float most = x[0][0];
+                for (unsigned h = 0; h < 2; ++h) {
 #pragma unroll
-        for (unsigned r = 1; r < 32; ++r) most = __builtin_fmaxf(most, x[r / 16][r % 16]);
-        most = larger_half(most);
-        if (__builtin_amdgcn_ballot_w64(!(most <= top + slack)) != 0) {
-            const float now = __builtin_fmaxf(most, top), next = now == -kInfinity ? 0.0f : kLift<DT> - now * c;
-            // (of logits far from 0 the product with c loses more than what is left: differences first)
-            const float keep = top == -kInfinity ? 0.0f : __builtin_fabsf(next) > kFar ? __builtin_amdgcn_exp2f((top - now) * c) : __builtin_amdgcn_exp2f(next - shift);
-            top = now, shift = next;
-            total *= keep;
+                    for (unsigned r = 8 * h; r < 8 * h + 8; ++r) {
+                        x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r], c, add));
+                        total += x[b][r];
+                    }
+                    const s8v p = rounded<DT>(x[b], h);
 #pragma unroll
-            for (unsigned d = 0; d < DP / 32; ++d) acc[d] *= keep;
-        }
-        float add = shift;
-        if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(shift) > kFar) != 0) {
-            const float base = top == -kInfinity ? 0.0f : top;
-            add = kLift<DT>;
-#pragma unroll
-            for (unsigned r = 0; r < 32; ++r) x[r / 16][r % 16] -= base;
-        }
-#pragma unroll
-        for (unsigned b = 0; b < 2; ++b)
-#pragma unroll
-            for (unsigned h = 0; h < 2; ++h) {
-#pragma unroll
-                for (unsigned r = 8 * h; r < 8 * h + 8; ++r) {
-                    x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r], c, add));
-                    total += x[b][r];
+                    for (unsigned d = 0; d < DP / 32; ++d) {
+                        const s8v columns = operand.columns(tile_v + (2u * b + h) * (16u * DP * 2u), d);
+                        if constexpr (CAREFUL) add_seen<DT>(acc[d], columns, p, 0, (int)(mine - j - 32u * b - 16u * h));
+                        else acc[d] = mfma<DT>(columns, p, acc[d]);
+                    }
                 }
-                const s8v p = rounded<DT>(x[b], h);
+        }
+    };
+    run(std::false_type());
+    // Results that are not finite are formed again, so that no row has them from keys that are hidden from it.
+    if (z.causal && any_of_group<4>(any_not_finite(acc), said)) {
+        top = -kInfinity, shift = 0.0f, total = 0.0f, buffer = 0;
 #pragma unroll
-                for (unsigned d = 0; d < DP / 32; ++d) acc[d] = mfma<DT>(columns_operand<DP>(tile_v, 32u * b + 16u * h, d), p, acc[d]);
-            }
+        for (unsigned d = 0; d < DP / 32; ++d) acc[d] = f16v{};
+        if (from < to) ask(from, 0);
+        run(std::true_type());
     }
     total = sum_of_halves(total);
     if (row >= rows) return;
@@ -533,7 +606,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
 {
     constexpr unsigned kTile = kTileKeys * DP * 2;
     __shared__ __align__(1024) unsigned char smem[4 * kTile];  // two tiles of keys and of values
-    __shared__ unsigned far_waves[4];
+    __shared__ unsigned said[4];
     const Lds lds = (Lds)smem;
     const unsigned kv = blockIdx.x % z.kv_heads;
     const TileAt t = tile_of(z.starts_q, z.tokens_q, z.num_seqs, z.group, kTileRows,
@@ -597,9 +670,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
     };
     const bool is_far = mine > 0u && __builtin_fabsf(base) > kFarBack;
     const bool far_wave = __builtin_amdgcn_ballot_w64(is_far) != 0;
-    if (l == 0u) far_waves[wave] = far_wave;
-    __syncthreads();
-    const bool far_tile = far_waves[0] || far_waves[1] || far_waves[2] || far_waves[3];
+    bool far_tile = any_of_group<4>(far_wave, said);
     if (far_tile) {
         float most = -kInfinity, total = 0.0f;
         unsigned buffer = 0;
@@ -628,9 +699,9 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
                 }
             }
         }
-        __syncthreads();  // (the tiles' places are written again)
         total = sum_of_halves(total);
-        if (is_far && most != -kInfinity) top = most, base = __builtin_log2f(total);
+        if (is_far && __builtin_fabsf(most) < kInfinity) top = most, base = __builtin_log2f(total);
+        far_tile = any_of_group<4>(__builtin_amdgcn_ballot_w64(top != 0.0f) != 0, said);
     }
     if (row < rows && half == 0u) {
         const size_t place = ((size_t)kv * z.tokens_q + s.q0 + query) * z.group + head - head0;
@@ -641,57 +712,73 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
     Lift lift;
     unsigned buffer = 0;
     if (to) ask(0, 0);
-    for (unsigned j = 0; j < to; j += kTileKeys) {
-        wait_for_loads<0>();
-        __syncthreads();
-        if (j + kTileKeys < to) ask(j + kTileKeys, buffer ^ 1u);
-        const unsigned at = buffer;
-        buffer ^= 1u;
-        if (wave * 32u >= rows) continue;
-        operand.renew();
+    const auto run = [&](auto careful) __attribute__((always_inline)) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        for (unsigned j = 0; j < to; j += kTileKeys) {
+            wait_for_loads<0>();
+            __syncthreads();
+            if (j + kTileKeys < to) ask(j + kTileKeys, buffer ^ 1u);
+            const unsigned at = buffer;
+            buffer ^= 1u;
+            if (wave * 32u >= rows) continue;
+            operand.renew();
 #pragma unroll
-        for (unsigned b = 0; b < 2; ++b) {
-            const Lds at_k = lds + at * 2u * kTile + b * (32u * DP * 2u), at_v = at_k + kTile;
-            f16v x = {}, y = {};
-            s8v ring_k[2], ring_v[2];
-            const auto fetch_rows = [&](unsigned i) __attribute__((always_inline)) {
-                ring_k[i % 2u] = operand.rows(at_k, i);
-                ring_v[i % 2u] = operand.rows(at_v, i);
-            };
-            fetch_rows(0);
+            for (unsigned b = 0; b < 2; ++b) {
+                const Lds at_k = lds + at * 2u * kTile + b * (32u * DP * 2u), at_v = at_k + kTile;
+                f16v x = {}, y = {};
+                s8v ring_k[2], ring_v[2];
+                const auto fetch_rows = [&](unsigned i) __attribute__((always_inline)) {
+                    ring_k[i % 2u] = operand.rows(at_k, i);
+                    ring_v[i % 2u] = operand.rows(at_v, i);
+                };
+                fetch_rows(0);
 #pragma unroll
-            for (unsigned i = 0; i < DP / 16; ++i) {
-                if (i + 1u < DP / 16) fetch_rows(i + 1u);
-                __builtin_amdgcn_sched_barrier(0);
-                x = mfma<DT>(ring_k[i % 2u], bq[i], x);
-                y = mfma<DT>(ring_v[i % 2u], bd[i], y);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            s8v columns[DP / 16];
+                for (unsigned i = 0; i < DP / 16; ++i) {
+                    if (i + 1u < DP / 16) fetch_rows(i + 1u);
+                    __builtin_amdgcn_sched_barrier(0);
+                    x = mfma<DT>(ring_k[i % 2u], bq[i], x);
+                    y = mfma<DT>(ring_v[i % 2u], bd[i], y);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                s8v columns[DP / 16];
 #pragma unroll
-            for (unsigned i = 0; i < DP / 16; ++i) columns[i] = operand.columns(at_k + i / (DP / 32) * (16u * DP * 2u), i % (DP / 32));
-            if (j + kTileKeys > least) {
+                for (unsigned i = 0; i < (CAREFUL ? 0 : DP / 16); ++i) columns[i] = operand.columns(at_k + i / (DP / 32) * (16u * DP * 2u), i % (DP / 32));
+                if (j + kTileKeys > least) {
 #pragma unroll
-                for (unsigned r = 0; r < 16; ++r)
-                    if (j + 32u * b + row_of(r, half) >= mine) x[r] = -kInfinity, y[r] = 0.0f;
-            }
-            if (far_wave) {
+                    for (unsigned r = 0; r < 16; ++r)
+                        if (j + 32u * b + row_of(r, half) >= mine) x[r] = -kInfinity, y[r] = 0.0f;
+                }
+                if (far_wave) {
 #pragma unroll
-                for (unsigned r = 0; r < 16; ++r) x[r] -= top;
-            }
+                    for (unsigned r = 0; r < 16; ++r) x[r] -= top;
+                }
 #pragma unroll
-            for (unsigned r = 0; r < 16; ++r) {
-                y[r] -= sum;
-                y[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -base)) * (DT == kGradF16 ? y[r] * lift.by : y[r]);
-            }
-            if constexpr (DT == kGradF16) lift.fit(y, acc);
+                for (unsigned r = 0; r < 16; ++r) {
+                    y[r] -= sum;
+                    y[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -base)) * (DT == kGradF16 ? y[r] * lift.by : y[r]);
+                }
+                if constexpr (DT == kGradF16) lift.fit(y, acc);
 #pragma unroll
-            for (unsigned h = 0; h < 2; ++h) {
-                const s8v ds = rounded<DT>(y, h);
+                for (unsigned h = 0; h < 2; ++h) {
+                    const s8v ds = rounded<DT>(y, h);
 #pragma unroll
-                for (unsigned d = 0; d < DP / 32; ++d) acc[d] = mfma<DT>(columns[h * (DP / 32) + d], ds, acc[d]);
+                    for (unsigned d = 0; d < DP / 32; ++d) {
+                        if constexpr (CAREFUL)
+                            add_seen<DT>(acc[d], operand.columns(at_k + h * (16u * DP * 2u), d), ds, 0, (int)(mine - j - 32u * b - 16u * h));
+                        else acc[d] = mfma<DT>(columns[h * (DP / 32) + d], ds, acc[d]);
+                    }
+                }
             }
         }
+    };
+    run(std::false_type());
+    if (z.causal && any_of_group<4>(any_not_finite(acc), said)) {  // as in the forward pass
+        lift = Lift();
+        buffer = 0;
+#pragma unroll
+        for (unsigned d = 0; d < DP / 32; ++d) acc[d] = f16v{};
+        if (to) ask(0, 0);
+        run(std::true_type());
     }
     if (row < rows) store_row<DT, DP>(dq.p + (size_t)(s.q0 + query) * dq.ld + head * z.dim, acc, z.scale / lift.by, z.dim);
 }
@@ -701,8 +788,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_dq(AttentionSizes z, Heads
 // of its rows, and the launch is as long as the longest group.  us (8191 tokens in 8 sequences, 32 heads of 128 over 8 | 4096 tokens, not
 // causal, the same heads; fp16, 7999 tokens in 16 sequences, 12 heads of 64, not causal | 4096 tokens, 32 heads of 64 over 8):
 //   128 elements a head: 4 waves in 2 streams 264 | 526, 2 in 4 255 | 575, 4 in one stream 345;  64: 2 in 2 70 | 318, 4 in 1 71 | 410, 4 in 2 82 | 314, 2 in 4 97 | 324
-// Of 128 elements a head, a wave's registers hold its keys and both results, but not its values too, which are read from LDS; of 64 there are three waves to
-// a SIMD (the fp16 batch 62 with two, 54 with three).
+// A wave's registers hold its keys and both results, but not its values too, which are read from LDS: of 128 elements a head there is no room for
+// them, and of 64 without them there are three waves to a SIMD (the fp16 batch 62 with two, 54 with three).
 constexpr unsigned kStreamRows = 32;
 template <int DP>
 constexpr unsigned kKeyWaves = DP == 128 ? 4 : 2;
@@ -716,13 +803,13 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, DP == 64 ? 3 : 2
                                                        Heads<const Elem<DT>> v, const float *__restrict__ all_lse, const float *__restrict__ delta,
                                                        const float *__restrict__ far, Heads<Elem<DT>> dk, Heads<Elem<DT>> dv)
 {
-    constexpr bool kValuesInLds = DP == 128;
     constexpr unsigned KW = kKeyWaves<DP>, S = kStreams<DP>, kKeys = kStreamKeys<DP>;
     // of a stream, twice: a tile of q, one of dout, and three numbers of each row
     constexpr unsigned kRows = kStreamRows, kTile = kRows * DP * 2, kStage = 2 * kTile + 1024, kValues = S * 2 * kStage;
     constexpr unsigned kSums = 32 * DP * 4;  // of a wave's results of one kind
     static_assert((S - 1) * KW * kSums <= kValues, "the streams' sums fit where their tiles were");
-    __shared__ __align__(1024) unsigned char smem[kValues + (kValuesInLds ? kKeys * DP * 2 : 0)];
+    __shared__ __align__(1024) unsigned char smem[kValues + kKeys * DP * 2];
+    __shared__ unsigned said[KW * S];
     const Lds lds = (Lds)smem, values = lds + kValues;
     const unsigned kv = blockIdx.x % z.kv_heads;
     const int *starts = z.starts_k ? z.starts_k : z.starts_q;
@@ -733,10 +820,8 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, DP == 64 ? 3 : 2
     const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), stream = wave / KW, side = wave % KW;
     const unsigned l = threadIdx.x % 64u, half = l / 32u, key = side * 32u + l % 32u, head0 = kv * z.group;
 
-    if constexpr (kValuesInLds) {
-        const TileLoads<DP, kKeys, KW * S> loads_v(wave, 1u, v.ld, z.dim);
-        loads_v.ask(values, wave, v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim, ((keys - 1u) * v.ld + z.dim) * 2u);
-    }
+    const TileLoads<DP, kKeys, KW * S> loads_v(wave, 1u, v.ld, z.dim);
+    loads_v.ask(values, wave, v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim, ((keys - 1u) * v.ld + z.dim) * 2u);
     // the first query that sees key j is j - (keys - queries)
     const long long later = (long long)s.queries - s.keys;
     const auto first_of = [&](unsigned j) __attribute__((always_inline)) -> unsigned {
@@ -773,17 +858,13 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, DP == 64 ? 3 : 2
     unsigned buffer = 0;
     if (tiles) ask(stream, 0);
     const __amdgpu_buffer_rsrc_t from_k = buffer_at(k.p + (size_t)(s.k0 + key0) * k.ld + kv * z.dim);
-    const __amdgpu_buffer_rsrc_t from_v = buffer_at(v.p + (size_t)(s.k0 + key0) * v.ld + kv * z.dim);
-    s8v bk[DP / 16], bv[kValuesInLds ? 1 : DP / 16];
+    s8v bk[DP / 16];
 #pragma unroll
-    for (unsigned i = 0; i < DP / 16; ++i) {
-        bk[i] = load16(from_k, row_offset(key, keys, 1u, k.ld, 16u * i + 8u * half, z.dim));
-        if constexpr (!kValuesInLds) bv[i] = load16(from_v, row_offset(key, keys, 1u, v.ld, 16u * i + 8u * half, z.dim));
-    }
+    for (unsigned i = 0; i < DP / 16; ++i) bk[i] = load16(from_k, row_offset(key, keys, 1u, k.ld, 16u * i + 8u * half, z.dim));
     landed(bk);
-    if constexpr (!kValuesInLds) landed(bv);
-    const auto run = [&](auto with_far) __attribute__((always_inline)) {
-        constexpr bool FAR = decltype(with_far)::value;
+    const auto run = [&](auto with_far, auto careful) __attribute__((always_inline)) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        const bool FAR = CAREFUL ? any_far : decltype(with_far)::value;
         for (unsigned first = 0; first < tiles; first += S) {
             wait_for_loads<0>();
             __syncthreads();
@@ -808,7 +889,7 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, DP == 64 ? 3 : 2
             const auto fetch_rows = [&](unsigned e) __attribute__((always_inline)) {
                 ring_q[e % 2u] = operand.rows(at_q, e);
                 ring_d[e % 2u] = operand.rows(at_d, e);
-                if constexpr (kValuesInLds) ring_v[e % 2u] = operand.rows(values + side * (32u * DP * 2u), e);
+                ring_v[e % 2u] = operand.rows(values + side * (32u * DP * 2u), e);
             };
             fetch_rows(0);
 #pragma unroll
@@ -816,10 +897,10 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, DP == 64 ? 3 : 2
                 if (e + 1u < DP / 16) fetch_rows(e + 1u);
                 __builtin_amdgcn_sched_barrier(0);
                 x = mfma<DT>(ring_q[e % 2u], bk[e], x);
-                y = mfma<DT>(ring_d[e % 2u], kValuesInLds ? ring_v[e % 2u] : bv[kValuesInLds ? 0 : e], y);
+                y = mfma<DT>(ring_d[e % 2u], ring_v[e % 2u], y);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if constexpr (FAR) {
+            if (FAR) {
 #pragma unroll
                 for (unsigned r = 0; r < 16; ++r) {
                     const float over = row_far[row_of(r, half)], first = row_lse[row_of(r, half)], less = x[r] - first;
@@ -833,10 +914,13 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, DP == 64 ? 3 : 2
                 ring[i % (kAhead + 1)] = operand.columns((i % 2u ? at_q : at_d) + i / (kProducts / 2u) * (16u * DP * 2u), i / 2u % (DP / 32));
             };
 #pragma unroll
-            for (unsigned i = 0; i < kAhead; ++i) fetch_columns(i);
+            for (unsigned i = 0; i < (CAREFUL ? 0u : kAhead); ++i) fetch_columns(i);
             // (every row of the tile sees every key of the wave, but for causal tiles on the border)
-            if (z.causal && first_of(key0 + side * 32u + 31u) > now) {
-                const unsigned first_row = first_of(key0 + key), hidden = first_row <= now ? 0u : group < kRows ? (first_row - now) * group : kRows;
+            unsigned hidden = 0;
+            const bool border = z.causal && first_of(key0 + side * 32u + 31u) > now;
+            if (border) {
+                const unsigned lane = lane_now(), half = lane / 32u, first_row = first_of(key0 + side * 32u + lane % 32u);
+                hidden = first_row <= now ? 0u : group < kRows ? (first_row - now) * group : kRows;
 #pragma unroll
                 for (unsigned r = 0; r < 16; ++r)
                     if (row_of(r, half) < hidden) x[r] = -kInfinity, y[r] = 0.0f;
@@ -852,17 +936,27 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, DP == 64 ? 3 : 2
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (unsigned i = 0; i < kProducts; ++i) {
-                if (i + kAhead < kProducts) fetch_columns(i + kAhead);
+                if constexpr (CAREFUL) fetch_columns(i);
+                else if (i + kAhead < kProducts) fetch_columns(i + kAhead);
                 const unsigned h = i / (kProducts / 2u), d = i / 2u % (DP / 32);
-                if (i % 2u) acc_k[d] = mfma<DT>(ring[i % (kAhead + 1)], ds[h], acc_k[d]);
+                if constexpr (CAREFUL) add_seen<DT>(i % 2u ? acc_k[d] : acc_v[d], ring[i % (kAhead + 1)], i % 2u ? ds[h] : p[h], (int)hidden - 16 * (int)h, 16);
+                else if (i % 2u) acc_k[d] = mfma<DT>(ring[i % (kAhead + 1)], ds[h], acc_k[d]);
                 else acc_v[d] = mfma<DT>(ring[i % (kAhead + 1)], p[h], acc_v[d]);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
     // (a branch for far rows within the loop costs 3 % of it, taken or not)
-    if (any_far) run(std::true_type());
-    else run(std::false_type());
+    if (any_far) run(std::true_type(), std::false_type());
+    else run(std::false_type(), std::false_type());
+    if (z.causal && any_of_group<KW * S>(any_not_finite(acc_k) || any_not_finite(acc_v), said)) {  // as in the forward pass
+        lift = Lift();
+        buffer = 0;
+#pragma unroll
+        for (unsigned d = 0; d < DP / 32; ++d) acc_k[d] = f16v{}, acc_v[d] = f16v{};
+        if (tiles) ask(stream, 0);
+        run(std::true_type(), std::true_type());
+    }
     // the streams' sums, added in their order
     const unsigned lane = lane_now(), own_key = side * 32u + lane % 32u;
     wait_for_loads<0>();
