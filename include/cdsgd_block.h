@@ -111,6 +111,8 @@ int cdsgd_block_norm_backward(const cdsgd_block_norm *norm, const void *dy, size
  * Products are summed in fp32; P and dS are rounded to the tensors' type as operands of the second products (dS of fp16 tensors times a power of two
  * of its row for dq, of its key for dk, which is divided out again: nothing overflows on the way, and what is lost of a number is below 2^-32 of the
  * largest |dS| that it is summed up with).
+ * Where a batch has too few rows of queries to fill the card, the forward pass takes their keys in parts, as many as tokens, sequences and heads of the
+ * whole batch say: out and lse of a sequence are then the same from run to run, but may be rounded otherwise in another batch (its gradients not).
  *   dtype         CDSGD_GRAD_BF16 or CDSGD_GRAD_F16
  *   dim           elements of a head: a multiple of 8, at most 128
  *   q, out, dout, dq  [tokens_q][heads][dim];  k, v, dk, dv  [tokens_k][kv_heads][dim]: the heads of a token in a row, tokens ld elements

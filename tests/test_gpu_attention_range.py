@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2106_10796_amd import binding as B
-from test_gpu_attention import SMALL, U, close as close_finite, half_step, inputs, logit_error, probabilities, reference, starts_of, tiny, tiny_p
+from test_gpu_attention import SMALL, U, check_forward, close as close_finite, half_step, inputs, logit_error, probabilities, reference, starts_of, tiny, tiny_p
 
 pytestmark = pytest.mark.gpu
 
@@ -160,3 +160,34 @@ def test_far_logits_of_ordinary_numbers_keep_their_sums():
         total = dv.double().sum(0)[:, 0]                          # of 300 queries of two heads, each a sum of probabilities: half a step each way
         assert bool(((total - 600).abs() <= 600 * 3 * 2.0 ** -8).all()), total
         assert all(bool(torch.isfinite(t).all()) for t in (dq, dk, dv))
+
+
+def test_a_sequence_in_other_batches():
+    """Where no keys are taken in parts a sequence's results are the same to the bit in any batch, dq among them."""
+    lens = [200, 77, 130]
+    q, k, v, dout = inputs(lens, lens, 8, 2, 128, "bf16", seed=41)
+    a = run(dout, q, k, v, lens, lens, True, 0.1)
+    for cut, n in ((slice(0, 200), 200), (slice(200, 277), 77), (slice(277, 407), 130)):
+        b = run(*(t[cut].contiguous() for t in (dout, q, k, v)), [n], [n], True, 0.1)
+        assert torch.equal(a[0][cut], b[0]) and torch.equal(a[1][:, cut], b[1]) and all(torch.equal(x[cut], y) for x, y in zip(a[2], b[2]))
+
+
+@pytest.mark.parametrize("others", [[], [64], [64] * 31, [4096, 1]], ids=len)
+def test_a_token_over_many_keys_beside_others(others):
+    """A new token's keys are taken in as many parts as its batch says: within the tolerances in each, the same from run to run, gradients the same in
+    any batch at the same out and lse."""
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    rnd = lambda n, h: torch.randn(n, h, 128, device="cuda", generator=gen).bfloat16()  # noqa: E731
+    q, k, v, dout, seqs = rnd(1, 8), rnd(4096, 2), rnd(4096, 2), rnd(1, 8), 1 + len(others)
+    alone = run(dout, q, k, v, [1], [4096], True, 0.1)
+    more = sum(others)
+    q, k, v, dout = (torch.cat([a, rnd(n, a.shape[1])]) for a, n in ((q, len(others)), (k, more), (v, more), (dout, len(others))))
+    lens_q, lens_k = [1] * seqs, [4096, *others]
+    out, lse, _ = run(dout, q, k, v, lens_q, lens_k, True, 0.1)
+    check_forward(q, k, v, out, lse, lens_q, lens_k, True, 0.1)
+    again = run(dout, q, k, v, lens_q, lens_k, True, 0.1)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    out[:1], lse[:, :1] = alone[0], alone[1]
+    room, grads = B.new_attention_workspace(q, k, seqs=seqs, train=True), [torch.empty_like(t) for t in (q, k, v)]
+    B.cdsgd_attention_backward(dout, q, k, v, out, lse, *grads, starts_of(lens_q), starts_of(lens_k), True, 0.1, room)
+    assert all(torch.equal(x[:n], y) for x, y, n in zip(grads, alone[2], (1, 4096, 4096)))
