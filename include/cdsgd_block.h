@@ -50,7 +50,7 @@ typedef struct {
  *   CDSGD_ACT_GELU_TANH  act(a) = a / 2 * (1 + tanh(sqrt(2 / pi) * (a + 0.044715 a^3)))
  * forward   a8_* and u8_*: where not NULL (all four or none) they receive a and u as cdsgd_mxint8_quantize would write them, for the backward pass
  * backward  da = dy * u * act'(a), du = dy * act(a), at a and u as they are or as 8 bits hold them (both the same way)
- * All matrices are rows by cols, of element type dtype.
+ * All matrices are rows by cols, of element type dtype.  An exponential below 2^-126 counts as 0.
  */
 typedef enum { CDSGD_ACT_SILU = 0, CDSGD_ACT_GELU_TANH = 1 } cdsgd_act;
 int cdsgd_gated_forward(int act, int dtype, size_t rows, size_t cols, const void *a, size_t ld_a, const void *u, size_t ld_u, void *y, size_t ld_y,

@@ -59,7 +59,9 @@ inline int check_held(const cdsgd_held *x, size_t rows, size_t cols, int dtype, 
     return CDSGD_OK;
 }
 
-// The longest row that a group holds in its registers.
+// The longest row: 16 waves of four fours to a lane.  Registers hold all of a row up to 8192 columns (of an fp32 matrix on an fp32 stream, backward, but
+// for 3 to 9 of them); beyond, with 128 to a lane, 170 to 240 bytes of a lane's share are in scratch forward and 280 to 410 backward, and every row goes
+// through them (2048 x 12288 in bf16 on an fp32 stream, us: 106, 236 of the 44 and 68 that its bytes take).
 constexpr size_t kMostCols = 16384;
 
 // Groups of the norm's backward pass, which leave their sums over rows: enough to fill the card, few enough that joining them
@@ -120,8 +122,8 @@ int check_norm(const cdsgd_block_norm *n)
 
 extern "C" {
 
-size_t cdsgd_mxint8_code_bytes(size_t rows, size_t cols) { return rows * ((cols + 31u) / 32u) * 32u; }
-size_t cdsgd_mxint8_scale_bytes(size_t rows, size_t cols) { return rows * ((cols + 31u) / 32u); }
+size_t cdsgd_mxint8_code_bytes(size_t rows, size_t cols) { return rows * held_groups(cols) * 32u; }
+size_t cdsgd_mxint8_scale_bytes(size_t rows, size_t cols) { return rows * held_groups(cols); }
 
 int cdsgd_mxint8_quantize(const void *x, int dtype, size_t rows, size_t cols, size_t ld, int8_t *codes, uint8_t *scales, void *hip_stream)
 {

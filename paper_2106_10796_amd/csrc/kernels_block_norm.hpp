@@ -1,6 +1,7 @@
 // The norms before and after a block, with its gate and residual scale (include/cdsgd_block.h), forward and backward.
 //
-// A group of WAVES waves takes a row, E elements V times to a lane, and keeps it in registers between the sums over it.
+// A group of WAVES waves takes a row, E elements V times to a lane, and keeps it in registers (of more than 8192 columns partly in scratch) between
+// the sums over it.
 #pragma once
 
 #include "device_matrix.hpp"

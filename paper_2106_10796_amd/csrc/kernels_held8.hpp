@@ -12,7 +12,12 @@ namespace {
 template <int DT>
 constexpr int kEach = DT == kGradF32 ? 4 : 8;
 
-inline unsigned held_groups(size_t cols) { return (unsigned)((cols + 31u) / 32u); }
+// Blocks of a row.
+template <typename T>
+__host__ __device__ constexpr T held_groups(T cols)
+{
+    return (cols + 31u) / 32u;
+}
 
 __device__ __forceinline__ unsigned larger_of(unsigned a, unsigned b) { return a > b ? a : b; }
 
@@ -67,7 +72,7 @@ __device__ __forceinline__ void decode(const Codes<E> &c, unsigned s, float (&x)
 template <int E>
 __device__ __forceinline__ void save(int8_t *codes, uint8_t *scales, size_t r, unsigned cols, unsigned c, const float (&x)[E])
 {
-    const unsigned groups = (cols + 31u) / 32u, s = block_scale<E>(x);
+    const unsigned groups = held_groups(cols), s = block_scale<E>(x);
     const Codes<E> w = encode<E>(x, s);
     if (c >= groups * 32u) return;
     *reinterpret_cast<Codes<E> *>(__builtin_assume_aligned(codes + r * (groups * 32u) + c, E)) = w;
@@ -83,7 +88,7 @@ struct Saved {
 template <int E>
 __device__ __forceinline__ Saved<E> load_saved(const int8_t *codes, const uint8_t *scales, size_t r, unsigned cols, unsigned c)
 {
-    const unsigned groups = (cols + 31u) / 32u;
+    const unsigned groups = held_groups(cols);
     Saved<E> x = {};
     if (c < groups * 32u) {
         x.w = *reinterpret_cast<const Codes<E> *>(__builtin_assume_aligned(codes + r * (groups * 32u) + c, E));
