@@ -69,10 +69,10 @@ int cdsgd_gated_backward(int act, int dtype, size_t rows, size_t cols, const voi
  *   dh = t;  dweight = sum(dy x)
  *   e = scale gate block_weight t;  db = n * (e - c mean(e c))   (block_weight NULL: db = e)
  *   dblock_weight = scale gate sum(t c);  dgate = scale block_weight sum(t c)
- * h_out is formed in 64 bits and rounded once; r, y and the gradients are formed in fp32 from what was not yet rounded (the sums over rows in
- * parts in fp32, joined in 64 bits) and rounded once.  eps keeps a row of zeros at 0.  Rows that are not finite go as the
- * formulas do: a NaN in h_out makes its row's y NaN; an infinity makes r 0, and y NaN at its place and 0 elsewhere; a NaN or an infinity in b makes
- * that row's y NaN where there is a block_weight.
+ * h_out is formed in 64 bits and rounded to fp32, and from there to a 16-bit type; r, y and the gradients are formed in fp32 from what was not yet
+ * rounded to 16 bits (the sums over rows in parts in fp32, joined in 64 bits) and rounded once.  eps keeps a row of zeros at 0.  Rows that are not
+ * finite go as the formulas do: a NaN in h_out makes its row's y NaN; an infinity makes r 0, and y NaN at its place and 0 elsewhere; a NaN or an
+ * infinity in b makes that row's y NaN where there is a block_weight.
  *   stream_dtype  of h, h_out, dh_out, dh: CDSGD_GRAD_F32, or dtype, which is that of b, y, dy, db
  *   rstd          fp32[2][rows]: r, and n (the second row is left as it is without a block_weight), from forward to backward
  *   b NULL        there is no block yet: h_out is h and must be NULL, b8, db, gate, block_weight and their gradients too; scale does nothing

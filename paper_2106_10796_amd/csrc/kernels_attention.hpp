@@ -245,6 +245,13 @@ __device__ __forceinline__ void reads_ahead()
 }
 
 // Of the 32 rows of a result, 16 from 16 t on, rounded: a second operand.
+// P and dS are rounded once here, as the matrix instructions take no wider operands beside 16-bit ones.  A second operand of what that leaves costs a
+// product more each: measured, errors against 64 bits as multiples of those of a result that is rounded once, and times (us, 8191 tokens in 8 sequences, 32
+// heads of 128 over 8 | 4096 tokens, not causal):
+//   out, dv  1.25 to 1.4 -> 1.0   forward 125 | 258 -> 149 | 353
+//   dq       1.75 (fp16 1.9) -> 1.4 (1.5)   dq 170 | 374 -> 198 | 468
+//   dk       1.6 -> 1.2 (with dq's)   dk, dv 270 | 517 -> 318 | 633, and of both P and dS 428 | 823
+// What is lost is about as much as the results' own rounding, and the rest of dq's is from the rounded `out` in dout . out: it is left at one product.
 template <int DT>
 __device__ __forceinline__ s8v rounded(const f16v &x, unsigned t)
 {

@@ -40,18 +40,6 @@ __device__ __forceinline__ void load_weight(const float *w, unsigned cols, unsig
     if (w) widened<kGradF32, E>(load_few<kGradF32, E>(w, cols, c), v);
 }
 
-// x as an fp32 number.  Where 16 bits follow, what fp32 does not hold is cut off and leaves the last bit set, so that rounding the result to nearest is
-// rounding x to nearest: to fp32 first, what lies next to halfway between two 16-bit numbers would become halfway.
-template <int DT>
-__device__ __forceinline__ float narrowed(double x)
-{
-    const float f = (float)x;
-    if constexpr (DT == kGradF32) return f;
-    const double back = f;
-    const unsigned bits = __builtin_bit_cast(unsigned, f) - (__builtin_fabs(back) > __builtin_fabs(x) ? 1u : 0u);
-    return __builtin_bit_cast(float, bits | (back != x ? 1u : 0u));
-}
-
 // Weights of a lane's elements: in registers throughout where there are few of them, or read again (from L2) for every row.
 constexpr int kKeptWeights = 8;
 
@@ -128,7 +116,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm_forward(NormWeights b
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
                     const double x = __builtin_fma(into[k][i], (double)eb[k].v[i] * n, (double)v[k][i]);
-                    v[k][i] = narrowed<ST>(x);
+                    v[k][i] = (float)x;  // (a 16-bit h_out is rounded from this, as torch takes 64 bits to 16: by way of fp32)
                     sum = __builtin_fma(x, x, sum);
                 }
                 if (place(k) < cols) store_few<ST, E>(h_out.p + r * h_out.ld, cols, place(k), v[k]);
