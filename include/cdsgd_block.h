@@ -108,9 +108,10 @@ int cdsgd_block_norm_backward(const cdsgd_block_norm *norm, const void *dy, size
  * Rows that belong to no sequence are neither read nor written.  A NaN or an infinity of a token reaches no other sequence, no other group of heads,
  * and, with `causal`, of its own sequence only what the formulas lead it to: a key's the queries that see it, a query's its own row and the keys
  * that it sees (and from a row that one key has made NaN all keys that the row sees).  What it does not reach is the same to the bit without it.
- * Products are summed in fp32; P and dS are rounded to the tensors' type as operands of the second products (dS of fp16 tensors times a power of two
- * of its row for dq, of its key for dk, which is divided out again: nothing overflows on the way, and what is lost of a number is below 2^-32 of the
- * largest |dS| that it is summed up with).
+ * Products are summed in fp32; P and dS are rounded to the tensors' type as operands of the second products.  Of fp16 tensors they are multiplied by
+ * powers of two first, which are divided out again: P by 2^7 over its row's largest in the forward pass (give or take 2^8) and 2^15 in the
+ * backward pass, so that what is lost of it beside its rounding is below 2^-32 and 2^-40; dS by one of its row for dq, of its key for dk, up to 2^60,
+ * so that nothing overflows on the way and what is lost is below 2^-32 of the largest |dS| that it is summed up with, or below 2^-85.
  * Where a batch has too few rows of queries to fill the card, the forward pass takes their keys in parts, as many as tokens, sequences and heads of the
  * whole batch say: out and lse of a sequence are then the same from run to run, but may be rounded otherwise in another batch (its gradients not).
  *   dtype         CDSGD_GRAD_BF16 or CDSGD_GRAD_F16

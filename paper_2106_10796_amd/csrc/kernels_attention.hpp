@@ -575,8 +575,9 @@ __global__ __launch_bounds__(256) void k_attention_join(AttentionSizes z, Heads<
 // dS of fp16 tensors is an operand times a power of two of its own, a row's in dq and a key's in dk (either is a lane's): fp16 ends at 65504, which
 // |dS| passes where values are large, and loses bits below 2^-14, where a flat row of many keys has all of it.  `fit` is given numbers that are
 // multiplied by `by` already.  The first that are not 0 bring the largest to 2^7 ... 2^8, later ones above 2^15 bring it there again, and what is summed up
-// is multiplied with them: nothing is lost of a number but below 2^-32 of the largest.  (7999 tokens in 16 sequences, 12 heads of 64, not causal, us: dq
-// 42 -> 45 and dk, dv 69 -> 62 with it in place of one power of two of dout's largest magnitude, which dk and dv's rows had to be searched for.)
+// is multiplied with them: nothing is lost of a number but below 2^-32 of the largest.  By no more than 2^60 at first: what comes later may be as
+// large as 2^39.  (7999 tokens in 16 sequences, 12 heads of 64, not causal, us: dq 42 -> 45 and dk, dv 69 -> 62 with it in place of one power of two of dout's
+// largest magnitude, which dk and dv's rows had to be searched for.)
 struct Lift {
     float by = 1.0f;
     bool begun = false;
@@ -591,7 +592,7 @@ struct Lift {
         const bool change = most > 32768.0f || (!begun && most > 0.0f);
         if (__builtin_amdgcn_ballot_w64(change) == 0) return;
         const unsigned e = __builtin_bit_cast(unsigned, most) >> 23, to = 261u - e;  // (of most's exponent field e, that of 2^7 over its power of two)
-        const float f = !change || e == 255u ? 1.0f : __builtin_bit_cast(float, (to < 227u ? to : 227u) << 23);
+        const float f = !change || e == 255u ? 1.0f : __builtin_bit_cast(float, (to < 187u ? to : 187u) << 23);
         begun = begun || change;
         by *= f;
         y *= f;

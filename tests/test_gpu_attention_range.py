@@ -80,6 +80,21 @@ def test_values_and_gradients_of_any_size(v_size, dout_size, causal, dim):
     go((dout.float() * dout_size).half(), q, k, (v.float() * v_size).clamp(-65504, 65504).half(), lens, lens, causal)
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_dS_of_one_row_and_of_one_key_from_almost_0_to_the_largest(dim):
+    """The first tile's probabilities are e^-85 and the last's ordinary, with values and gradients of 3e4: dS from 2^-87 to 2^30 and more in one sum."""
+    half = lambda *s: torch.zeros(*s, dtype=torch.float16, device="cuda")  # noqa: E731
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    small = lambda n: (torch.randint(-16, 17, (n, 1, dim), device="cuda", generator=gen) * 2.0 ** -24).half()  # noqa: E731
+    sign = lambda n: torch.where(torch.arange(n, device="cuda") % 2 == 0, 3e4, -3e4).half()[:, None, None].expand(n, 1, dim).contiguous()  # noqa: E731
+    # a row over 64 keys far below and 64 beside 0
+    q, k, v, dout = half(40, 1, dim) + 1, torch.cat([half(64, 1, dim) - 85.0 / dim, small(64)]), sign(128), half(40, 1, dim) + 3e4
+    go(dout, q, k, v, [40], [128], False, scale=1.0)
+    # keys seen by 64 queries from far below and by 64 from beside 0
+    q, k, v, dout = torch.cat([half(64, 1, dim) - 85.0 / dim, small(64)]), torch.cat([half(20, 1, dim) + 1, half(20, 1, dim)]), sign(40), half(128, 1, dim) + 3e4
+    go(dout, q, k, v, [128], [40], False, scale=1.0)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("v_size", [1.0, 0.02, 0.005])
 @pytest.mark.parametrize("keys", [16384, 40000])
