@@ -369,9 +369,9 @@ __device__ __forceinline__ void store_row(Elem<DT> *row, const f16v (&acc)[DP / 
 // forward
 // ---------------------------------------------------------------------------
 // A group takes 128 rows, 32 to a wave, and goes through the keys that they see by tiles of 64, the next tile on its way to LDS while one is worked on.
-// With the 228 registers that a wave of 128 elements a head takes there are two groups to a compute unit, and their LDS fits.  16384 tokens, 16
+// With the 222 registers that a wave of 128 elements a head takes there are two groups to a compute unit, and their LDS fits.  16384 tokens, 16
 // heads of 128 over 2, causal: 1.0 to 1.07 ms, 1.1 PFLOP/s of the 1.35 that the library's product reaches; bound by power and by the vector
-// instructions between the products (169 beside 32 products for a tile).  One group to a compute unit 1.37, tiles through registers 1.9, rows and tiles
+// instructions between the products (164 beside 32 products for a tile).  One group to a compute unit 1.37, tiles through registers 1.9, rows and tiles
 // read two reads ahead in place of six 1.10, a block's probabilities between the next one's products 1.2 to 1.6 (registers).
 //
 // parts, part_lse: where several groups share a row's keys (`splits`), each leaves its own result, [splits][row of all][DP] in fp32 and
@@ -602,7 +602,7 @@ struct Lift {
 };
 
 // dq, and with it the first kernel of the backward pass: tiles as in the forward pass, three products for its two.  4096 tokens, 32 heads of 128 over 8,
-// not causal: 370 us, 1.1 PFLOP/s, bound as the forward pass is; 8191 tokens in 8 sequences, causal: 163.
+// not causal: 374 us, 1.1 PFLOP/s, bound as the forward pass is; 8191 tokens in 8 sequences, causal: 166 to 172.
 // For the next kernel row_lse receives what S begins with in every row, (lift - lse log2 e) / c, far 0, and delta -dout . out, all
 // [kv head][token][head of the group].  A row whose lse is far from 0 leaves its largest S, and in far 2^lift over the sum of exp(scale (S - largest));
 // where a tile has such rows its first one's far is not 0 (-1 if it is not far itself).
