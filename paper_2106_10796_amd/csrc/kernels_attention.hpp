@@ -845,10 +845,11 @@ __global__ __launch_bounds__(64 * kKeyWaves<DP> * kStreams<DP>, DP == 64 ? 3 : 2
     const TileLoads<DP, kRows, KW> loads_q(side, group, q.ld, z.dim), loads_d(side, group, dout.ld, z.dim);
     // (values, not one of three variables: the compiler would keep those in memory)
     const float *const numbers = side == 0u ? +all_lse : +delta;
-    bool any_far = false;
-    for (unsigned long long i = l * (unsigned long long)kTileRows; i < (unsigned long long)s.queries * group; i += 64u * kTileRows)
-        any_far = any_far || far[((size_t)kv * z.tokens_q + s.q0) * group + i] != 0.0f;
-    any_far = __builtin_amdgcn_ballot_w64(any_far) != 0;
+    const float *const far_here = far + ((size_t)kv * z.tokens_q + s.q0) * group;
+    unsigned found = 0;
+#pragma unroll 4
+    for (unsigned long long i = l * (unsigned long long)kTileRows; i < (unsigned long long)s.queries * group; i += 64u * kTileRows) found |= far_here[i] != 0.0f;
+    const bool any_far = __builtin_amdgcn_ballot_w64(found != 0u) != 0;
     // tile `n` of all; past the last nothing is in range
     const auto ask = [&](unsigned n, unsigned b) __attribute__((always_inline)) {
         const unsigned i = from + n / parts * at_once, part = n % parts * kRows, there = n < tiles ? s.queries - i : 0u;

@@ -206,3 +206,13 @@ def test_a_token_over_many_keys_beside_others(others):
     room, grads = B.new_attention_workspace(q, k, seqs=seqs, train=True), [torch.empty_like(t) for t in (q, k, v)]
     B.cdsgd_attention_backward(dout, q, k, v, out, lse, *grads, starts_of(lens_q), starts_of(lens_k), True, 0.1, room)
     assert all(torch.equal(x[:n], y) for x, y, n in zip(grads, alone[2], (1, 4096, 4096)))
+
+
+@pytest.mark.parametrize("far", [slice(4990, 5000), slice(0, 3), slice(4200, 4201)], ids=["last", "first", "one"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_few_far_rows_of_many(far, dtype):
+    """More tiles of rows than a wave has lanes, of which one has far rows."""
+    near = [slice(0, far.start), slice(far.stop, 5000)]
+    q, k, v, dout = far_case(dtype, 64, 2.0 ** 10, 1, [5000], [100], 24, near_rows=near)
+    out, lse, grads = run(dout, q, k, v, [5000], [100], False, 2.0 ** 10)
+    check_gradients(dout, q, k, v, out, lse, grads, [5000], [100], False, 2.0 ** 10, exact_logits=True)
